@@ -41,8 +41,8 @@
  *  - Entry points keep no state but the scratch blocks and are reentrant:
  *    several jobs (say a training and a validation job) can be planned
  *    concurrently on different streams.
- *  - Every result is exact integer work and deterministic: the output is a
- *    pure function of the inputs.
+ *  - Every result is deterministic: the output is a pure function of the
+ *    inputs. The planning calls' are exact integer work.
  *
  * READINGS of points the paper leaves open (binding for every entry point):
  *  - Shuffle: epoch e orders samples by a 32-bit key, word (k mod 4) of
@@ -359,6 +359,121 @@ int nopfs_buffer_sim(const nopfs_job* job, const int32_t* R, const int32_t* next
 int nopfs_policy_sim(const nopfs_job* job, const int32_t* R, const int64_t* sizes,
                      const int16_t* src, const int32_t* fill, const nopfs_model* model,
                      int32_t policy, double* t, double* finish, double* io, void* hip_stream);
+
+/* ---- A training step on the reads that come next ----------------------- *
+ * What a worker's step needs where samples differ in length: the place of
+ * every token, attention over the packed samples, and the loss against
+ * teacher logits stored with the samples. These follow the conventions above;
+ * results of 16- and 32-bit arithmetic are rounded, and the same from call to
+ * call (no sum depends on the order in which work finishes). */
+
+/* Element types. */
+#define NOPFS_BF16 0
+#define NOPFS_FP16 1
+#define NOPFS_FP32 2
+
+/* The next n reads of G workers (groups), to be laid out in a token buffer of
+ * blocks of `block` tokens. */
+typedef struct nopfs_batch {
+  int64_t F;           /* samples (entries of `tokens` when ids is given)   */
+  int64_t ids_stride;  /* elements from a group's reads to the next group's */
+  int64_t free_stride; /* elements from a group's free list to the next's   */
+  int32_t G, n;        /* groups, reads of each; >= 1, n <= 2^30            */
+  int32_t blocks;      /* free blocks of each group, >= 0                   */
+  int32_t block;       /* tokens per block, >= 1                            */
+  int32_t width;       /* blocks a read may take (columns of `table`), >= 1 */
+  int32_t cap;         /* packed tokens a group may hold, 0 <= cap <= 2^30  */
+} nopfs_batch;
+
+/* Block tables and slot maps from the lengths of the next reads. Read r of
+ * group g has length len = tokens[ids[g*ids_stride + r]], 0 where the id is
+ * not in [0, F) (padding) or the length is negative; with ids NULL, tokens
+ * holds the lengths themselves ([G] rows of n, ids_stride apart). A read takes
+ * ceil(len / block) blocks from the group's free list, in order. Reads are
+ * admitted in order up to the first that does not fit: more than `width`
+ * blocks of its own, or more than `blocks` blocks or `cap` tokens in all.
+ *   free_blocks: int32, `blocks` block ids per group, taken front to back.
+ *   start: int32 [G][n+1], packed tokens before read r (start[n]: all).
+ *   table: int32 [G][n][width], a read's blocks, then -1.
+ *   slot:  int64 [G][cap], of packed token t at position p of its read:
+ *          table[p div block] * block + p mod block; -1 from start[n] on.
+ *   row, pos: int32 [G][cap], the token's read and its position in it, or -1.
+ *   used:  int32 [G][3], admitted reads, their tokens, their blocks.
+ * Errors: EINVAL, ERANGE, ENOMEM, EDEVICE. */
+int nopfs_batch_tables(const nopfs_batch* batch, const int32_t* ids, const int32_t* tokens,
+                       const int32_t* free_blocks, int32_t* start, int32_t* table, int64_t* slot,
+                       int32_t* row, int32_t* pos, int32_t* used, void* hip_stream);
+
+/* Causal attention over n packed samples of different lengths. Strides are in
+ * elements: [0] from token to token, [1] from head to head; the `width`
+ * elements of a head are adjacent. Pointers and strides of the 16-bit arrays
+ * are multiples of 16 bytes. */
+typedef struct nopfs_attention {
+  int64_t T;           /* rows (tokens, padding included)                    */
+  int32_t n;           /* samples, >= 0                                      */
+  int32_t heads;       /* query heads, a multiple of kv_heads                */
+  int32_t kv_heads;    /* query head h reads kv head h div (heads/kv_heads)  */
+  int32_t width;       /* elements of a head: a multiple of 8, 8..128        */
+  int32_t dtype;       /* NOPFS_BF16 or NOPFS_FP16                           */
+  float scale;         /* of the products q.k, positive and finite           */
+  int64_t q_stride[2], k_stride[2], v_stride[2], o_stride[2];
+  int64_t do_stride[2], dq_stride[2], dk_stride[2], dv_stride[2]; /* gradient only */
+} nopfs_attention;
+
+/* Forward. Sample s holds tokens start[s]..start[s+1]-1; a token sees its own
+ * sample up to itself:
+ *   S_ij = scale q_i.k_j for j <= i, lse_i = log sum_j exp S_ij,
+ *   o_i = sum_j exp(S_ij - lse_i) v_j.
+ *   start: int32 [n+1], 0 = start[0] <= ... <= start[n] <= T, as written by
+ *          nopfs_batch_tables (precondition; other contents give unspecified
+ *          but in-bounds results).
+ *   lse:   float [heads][T].
+ * Rows from start[n] on belong to no sample: o = 0 and lse = -inf, and what q,
+ * k and v hold there is not read. Errors: EINVAL, ERANGE, EDEVICE. */
+int nopfs_packed_attention(const nopfs_attention* a, const void* q, const void* k, const void* v,
+                           const int32_t* start, void* o, float* lse, void* hip_stream);
+
+/* Gradient of the forward call, from its outputs o and lse and from do, the
+ * gradient of o. With P_ij = exp(S_ij - lse_i), dP_ij = do_i.v_j and
+ * dS_ij = P_ij (dP_ij - do_i.o_i):
+ *   dq_i = scale sum_j dS_ij k_j,
+ *   dk_j = scale sum over the query heads of the group and i of dS_ij q_i,
+ *   dv_j = the same sum of P_ij do_i.
+ * Rows from start[n] on get 0. Errors: EINVAL, ERANGE, ENOMEM, EDEVICE. */
+int nopfs_packed_attention_grad(const nopfs_attention* a, const void* d_o, const void* q,
+                                const void* k, const void* v, const void* o, const float* lse,
+                                const int32_t* start, void* dq, void* dk, void* dv,
+                                void* hip_stream);
+
+/* Distillation from a teacher's K top logits per row. */
+typedef struct nopfs_distill {
+  int64_t T, V;           /* rows (tokens or samples), classes; < 2^31        */
+  int64_t logits_stride;  /* elements from row to row, >= V                   */
+  int64_t grad_stride;    /* the same of the gradient, >= V                   */
+  int64_t index_stride;   /* of index, >= K                                   */
+  int64_t teacher_stride; /* of teacher, >= K                                 */
+  int32_t K;              /* teacher entries per row, 1..1024                 */
+  int32_t dtype;          /* of logits and grad                               */
+  int32_t teacher_dtype;
+  float tau;              /* temperature, positive and finite                 */
+} nopfs_distill;
+
+/* Loss and gradient. With p the softmax of teacher / tau over a row's valid
+ * entries (0 <= index < V) and z = log sum_v exp(logits_v / tau):
+ *   loss   = weight tau^2 sum_k p_k (log p_k - logits[index_k] / tau + z),
+ *   grad_v = d loss / d logits_v
+ *          = weight tau (exp(logits_v / tau - z) - sum_{k: index_k = v} p_k).
+ * An entry of p_k = 0 adds nothing to the loss. A row of weight 0, or whose
+ * entries are all invalid or -inf, has loss 0 and gradient 0 whatever its
+ * logits hold.
+ *   weight: float [T], or NULL for 1.
+ *   loss:   float [T].
+ *   grad:   [T] rows of V of the logits' type, or NULL (loss alone); may be
+ *           logits itself with the same stride (in place).
+ * No scratch. Errors: EINVAL, ERANGE, EDEVICE. */
+int nopfs_topk_distill(const nopfs_distill* distill, const void* logits, const int32_t* index,
+                       const void* teacher, const float* weight, float* loss, void* grad,
+                       void* hip_stream);
 
 /* Static description of a status code. Never NULL. */
 const char* nopfs_strerror(int code);

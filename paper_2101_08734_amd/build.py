@@ -9,7 +9,8 @@ import sys
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 LIB = os.path.join(HERE, "libnopfs.so")
-SOURCES = sorted(glob.glob(os.path.join(HERE, "csrc", "*.hip")))
+# csrc: the planner; csrc_step: the operators of a training step on its reads
+SOURCES = [p for d in ("csrc", "csrc_step") for p in sorted(glob.glob(os.path.join(HERE, d, "*.hip")))]
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",
@@ -17,6 +18,7 @@ HIPCC_FLAGS = [
     "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
     "-Wall", "-Wno-unused-function",
     f"-I{os.path.join(ROOT, 'include')}", f"-I{os.path.join(HERE, 'csrc')}",
+    f"-I{os.path.join(HERE, 'csrc_step')}",
 ]
 
 

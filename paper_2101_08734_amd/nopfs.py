@@ -74,6 +74,27 @@ def make_model(c, beta, b_c, pfs_t, pfs_gamma, w0, p0, r, p) -> Model:
     return m
 
 
+class _Batch(ctypes.Structure):
+    _fields_ = ([(x, ctypes.c_int64) for x in ("F", "ids_stride", "free_stride")]
+                + [(x, ctypes.c_int32) for x in ("G", "n", "blocks", "block", "width", "cap")])
+
+
+class _Attention(ctypes.Structure):
+    # a stride[2] of the C struct is a pair of fields here: token, head
+    _fields_ = ([("T", ctypes.c_int64)]
+                + [(x, ctypes.c_int32) for x in ("n", "heads", "kv_heads", "width", "dtype")]
+                + [("scale", ctypes.c_float)]
+                + [(f"{x}_{y}", ctypes.c_int64)
+                   for x in ("q", "k", "v", "o", "do", "dq", "dk", "dv") for y in ("token", "head")])
+
+
+class _Distill(ctypes.Structure):
+    _fields_ = ([(x, ctypes.c_int64) for x in ("T", "V", "logits_stride", "grad_stride",
+                                               "index_stride", "teacher_stride")]
+                + [(x, ctypes.c_int32) for x in ("K", "dtype", "teacher_dtype")]
+                + [("tau", ctypes.c_float)])
+
+
 _lib = None
 
 
@@ -102,6 +123,10 @@ def lib() -> ctypes.CDLL:
             "nopfs_buffer_sim": [jp, P, P, P, I64, P, P, P],
             "nopfs_access_streams_range": [jp, ctypes.c_int32, ctypes.c_int32, P, P],
             "nopfs_policy_sim": [jp, P, P, P, P, ctypes.POINTER(Model), ctypes.c_int32, P, P, P, P],
+            "nopfs_batch_tables": [ctypes.POINTER(_Batch)] + [P] * 10,
+            "nopfs_packed_attention": [ctypes.POINTER(_Attention)] + [P] * 7,
+            "nopfs_packed_attention_grad": [ctypes.POINTER(_Attention)] + [P] * 11,
+            "nopfs_topk_distill": [ctypes.POINTER(_Distill)] + [P] * 7,
             "nopfs_profile_enable": [ctypes.c_int],
             "nopfs_profile_query": [ctypes.c_int, ctypes.POINTER(ctypes.c_char_p),
                                     ctypes.POINTER(I64), ctypes.POINTER(ctypes.c_double)],
@@ -126,7 +151,8 @@ EXPORTED = ("nopfs_stream_shape", "nopfs_access_streams", "nopfs_access_streams_
             "nopfs_reuse_next", "nopfs_tier_plan", "nopfs_plan_job", "nopfs_plan_job_noalloc",
             "nopfs_prefetch_order",
             "nopfs_staging_schedule", "nopfs_fetch_model", "nopfs_buffer_sim", "nopfs_policy_sim",
-            "nopfs_strerror",
+            "nopfs_batch_tables", "nopfs_packed_attention", "nopfs_packed_attention_grad",
+            "nopfs_topk_distill", "nopfs_strerror",
             "nopfs_last_error", "nopfs_profile_enable", "nopfs_profile_query",
             "nopfs_calibration_copy", "nopfs_scratch_release", "nopfs_debug_set")
 
@@ -400,6 +426,214 @@ def plan(job: Job, sizes, caps, stream=None):
     nxt = reuse_next(job, R, stream=stream)
     tier, used = tier_plan(job, count, first, sizes, caps, stream=stream)
     return dict(R=R, count=count, first=first, next=nxt, tier=tier, used=used)
+
+
+# -- a training step on the reads that come next ------------------------------------
+_DTYPES = {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2}  # NOPFS_BF16, _FP16, _FP32
+
+
+def _step_tensor(t, name, dtypes, ndim, device):
+    """A device tensor of one of these types and this many dimensions, adjacent
+    along the last one, on the given device (None: the current one)."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise TypeError(f"{name} must be a device tensor")
+    if t.dtype not in dtypes:
+        raise ValueError(f"{name} must be of type " + " or ".join(str(d) for d in dtypes))
+    if t.dim() != ndim or (t.shape[-1] > 1 and t.stride(-1) != 1):
+        raise ValueError(f"{name} must have {ndim} dimensions, the last one adjacent in memory")
+    if t.device.index != device:
+        raise ValueError(f"{name} must be on device {device}, where the call runs")
+    return t
+
+
+def _step_shape(t, name, shape):
+    if tuple(t.shape) != shape:
+        raise ValueError(f"{name} must have shape {shape}, not {tuple(t.shape)}")
+
+
+def _step_stream(stream, tensors):
+    """The stream's handle. Where it is not the current one, the allocator is
+    told that the call's tensors are in use there."""
+    current = torch.cuda.current_stream()
+    if stream is None or stream.cuda_stream == current.cuda_stream:
+        return current.cuda_stream
+    for t in tensors:
+        if t is not None:
+            t.record_stream(stream)
+    return stream.cuda_stream
+
+
+def _dense(t, name):
+    if not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+    return t
+
+
+def _row_stride(t):
+    """Elements from row to row; a single row's stride says nothing."""
+    return t.stride(0) if t.shape[0] > 1 else max(t.shape[1], 1)
+
+
+_I32 = (torch.int32,)
+
+
+def batch_tables(ids, tokens, free, block: int, width: int, cap: int, out=None, stream=None):
+    """Block tables and slot maps of the next reads (nopfs_batch_tables), from
+    their lengths in tokens.
+
+    ids [G][n] int32, the reads of G workers (columns of the streams R, say);
+    tokens [F] int32, every sample's length. With ids None, tokens [G][n] holds
+    the reads' lengths. free [G][blocks] int32, each worker's free blocks of
+    `block` tokens. Returns start [G][n+1], table [G][n][width], row and pos
+    [G][cap], used [G][3] (reads, tokens, blocks) as int32 and slot [G][cap] as
+    int64; `out` may hold any of them preallocated."""
+    dev = torch.cuda.current_device()
+    free = _step_tensor(free, "free", _I32, 2, dev)
+    if ids is None:
+        lead, F = _step_tensor(tokens, "tokens", _I32, 2, dev), 0
+    else:
+        lead = _step_tensor(ids, "ids", _I32, 2, dev)
+        F = _dense(_step_tensor(tokens, "tokens", _I32, 1, dev), "tokens").shape[0]
+    G, n = lead.shape
+    block, width, cap = int(block), int(width), int(cap)
+    if free.shape[0] != G:
+        raise ValueError(f"free must have {G} rows")
+    if not (0 < block < 2**31 and 0 < width < 2**31 and 0 <= cap < 2**31):
+        raise ValueError("block and width must be positive, cap not negative, all below 2^31")
+    o = dict(out or {})
+    for name, shape, dt in (("start", (G, n + 1), torch.int32), ("table", (G, n, width), torch.int32),
+                            ("slot", (G, cap), torch.int64), ("row", (G, cap), torch.int32),
+                            ("pos", (G, cap), torch.int32), ("used", (G, 3), torch.int32)):
+        t = o.get(name)
+        if t is None:
+            o[name] = torch.empty(shape, dtype=dt, device=lead.device)
+        else:
+            _dense(_step_tensor(t, name, (dt,), len(shape), dev), name)
+            _step_shape(t, name, shape)
+    b = _Batch(F, _row_stride(lead), _row_stride(free), G, n, free.shape[1], block, width, cap)
+    st = _step_stream(stream, (ids, tokens, free, *o.values()))
+    _check(lib().nopfs_batch_tables(
+        ctypes.byref(b), None if ids is None else ids.data_ptr(), tokens.data_ptr(),
+        free.data_ptr(), o["start"].data_ptr(), o["table"].data_ptr(), o["slot"].data_ptr(),
+        o["row"].data_ptr(), o["pos"].data_ptr(), o["used"].data_ptr(), st), "nopfs_batch_tables")
+    return o
+
+
+_HALVES = (torch.bfloat16, torch.float16)
+
+
+def _attention(q, k, v, start, scale, dev):
+    _step_tensor(q, "q", _HALVES, 3, dev)
+    T, heads, width = q.shape
+    same = (q.dtype,)
+    kv_heads = _step_tensor(k, "k", same, 3, dev).shape[1]
+    _step_shape(k, "k", (T, kv_heads, width))
+    _step_shape(_step_tensor(v, "v", same, 3, dev), "v", (T, kv_heads, width))
+    if _dense(_step_tensor(start, "start", _I32, 1, dev), "start").shape[0] < 1:
+        raise ValueError("start must have an entry before every sample and one behind the last")
+    if scale is None:
+        scale = width ** -0.5 if width else 0.0
+    return _Attention(T, start.shape[0] - 1, heads, kv_heads, width, _DTYPES[q.dtype], scale)
+
+
+def _set_strides(a, **tensors):
+    """Token and head strides. That of a single token or head says nothing:
+    what the array would have when dense."""
+    for name, t in tensors.items():
+        T, heads, width = t.shape
+        setattr(a, name + "_head", t.stride(1) if heads > 1 else width)
+        setattr(a, name + "_token", t.stride(0) if T > 1 else heads * width)
+
+
+def packed_attention(q, k, v, start, scale=None, o=None, lse=None, stream=None):
+    """Causal attention over packed samples (nopfs_packed_attention): q
+    [T][heads][width], k and v [T][kv_heads][width], bfloat16 or float16, any
+    token and head strides of whole 16 bytes (slices of one projection, say);
+    start [n+1] int32, a row of batch_tables' start. Returns o (as q) and lse
+    [heads][T] float32. scale: 1/sqrt(width) unless given."""
+    dev = torch.cuda.current_device()
+    a = _attention(q, k, v, start, scale, dev)
+    if o is None:
+        o = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    else:
+        _step_shape(_step_tensor(o, "o", (q.dtype,), 3, dev), "o", tuple(q.shape))
+    if lse is None:
+        lse = torch.empty((a.heads, a.T), dtype=torch.float32, device=q.device)
+    else:
+        _step_shape(_dense(_step_tensor(lse, "lse", (torch.float32,), 2, dev), "lse"), "lse",
+                    (a.heads, a.T))
+    _set_strides(a, q=q, k=k, v=v, o=o)
+    st = _step_stream(stream, (q, k, v, start, o, lse))
+    _check(lib().nopfs_packed_attention(ctypes.byref(a), q.data_ptr(), k.data_ptr(), v.data_ptr(),
+                                        start.data_ptr(), o.data_ptr(), lse.data_ptr(), st),
+           "nopfs_packed_attention")
+    return o, lse
+
+
+def packed_attention_grad(do, q, k, v, o, lse, start, scale=None, dq=None, dk=None, dv=None,
+                          stream=None):
+    """Gradient of packed_attention (nopfs_packed_attention_grad) from its
+    outputs and the gradient `do` of o. Returns dq, dk, dv (as q, k, v; slices
+    of one preallocated array, say)."""
+    dev = torch.cuda.current_device()
+    a = _attention(q, k, v, start, scale, dev)
+    same = (q.dtype,)
+    for name, t in (("do", do), ("o", o)):
+        _step_shape(_step_tensor(t, name, same, 3, dev), name, tuple(q.shape))
+    _step_shape(_dense(_step_tensor(lse, "lse", (torch.float32,), 2, dev), "lse"), "lse",
+                (a.heads, a.T))
+    grads = []
+    for name, t, like in (("dq", dq, q), ("dk", dk, k), ("dv", dv, v)):
+        if t is None:
+            t = torch.empty(like.shape, dtype=q.dtype, device=q.device)
+        else:
+            _step_shape(_step_tensor(t, name, same, 3, dev), name, tuple(like.shape))
+        grads.append(t)
+    dq, dk, dv = grads
+    _set_strides(a, q=q, k=k, v=v, o=o, do=do, dq=dq, dk=dk, dv=dv)
+    st = _step_stream(stream, (do, q, k, v, o, lse, start, dq, dk, dv))
+    _check(lib().nopfs_packed_attention_grad(
+        ctypes.byref(a), do.data_ptr(), q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(),
+        lse.data_ptr(), start.data_ptr(), dq.data_ptr(), dk.data_ptr(), dv.data_ptr(), st),
+        "nopfs_packed_attention_grad")
+    return dq, dk, dv
+
+
+def topk_distill(logits, index, teacher, tau=1.0, weight=None, grad=True, loss=None, dlogits=None,
+                 stream=None):
+    """Distillation from a teacher's top logits (nopfs_topk_distill): logits
+    [T][V], index [T][K] int32 and teacher [T][K], the teacher's K classes per
+    row and their logits; weight [T] float32 scales a row's loss (0: the row is
+    masked). Returns loss [T] float32 and, unless grad is False, its gradient
+    by the logits (in their type; dlogits may be logits itself)."""
+    dev = torch.cuda.current_device()
+    T, V = _step_tensor(logits, "logits", tuple(_DTYPES), 2, dev).shape
+    K = _step_tensor(index, "index", _I32, 2, dev).shape[1]
+    _step_shape(index, "index", (T, K))
+    _step_shape(_step_tensor(teacher, "teacher", tuple(_DTYPES), 2, dev), "teacher", (T, K))
+    if weight is not None:
+        _step_shape(_dense(_step_tensor(weight, "weight", (torch.float32,), 1, dev), "weight"),
+                    "weight", (T,))
+    if loss is None:
+        loss = torch.empty(T, dtype=torch.float32, device=logits.device)
+    else:
+        _step_shape(_dense(_step_tensor(loss, "loss", (torch.float32,), 1, dev), "loss"), "loss",
+                    (T,))
+    if not grad:
+        dlogits = None
+    elif dlogits is None:
+        dlogits = torch.empty((T, V), dtype=logits.dtype, device=logits.device)
+    else:
+        _step_shape(_step_tensor(dlogits, "dlogits", (logits.dtype,), 2, dev), "dlogits", (T, V))
+    d = _Distill(T, V, _row_stride(logits), 0 if dlogits is None else _row_stride(dlogits),
+                 _row_stride(index), _row_stride(teacher), K, _DTYPES[logits.dtype],
+                 _DTYPES[teacher.dtype], tau)
+    st = _step_stream(stream, (logits, index, teacher, weight, loss, dlogits))
+    _check(lib().nopfs_topk_distill(
+        ctypes.byref(d), logits.data_ptr(), index.data_ptr(), teacher.data_ptr(),
+        None if weight is None else weight.data_ptr(), loss.data_ptr(),
+        None if dlogits is None else dlogits.data_ptr(), st), "nopfs_topk_distill")
+    return loss, dlogits
 
 
 # -- measurement aids -----------------------------------------------------------
