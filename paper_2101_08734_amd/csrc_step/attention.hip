@@ -120,44 +120,62 @@ __device__ inline bool find_tile(const Attention& a, uint32_t tile, Tile* t) {
   return m0 >= 0 && m0 < t->len;
 }
 
-template <int DP>
 __device__ __forceinline__ int row_swizzle(int r) { return ((r & 3) << 1) | ((r >> 2) & 1); }
 // Byte offset of 16-byte chunk c of row r in an LDS tile of DP-element rows.
 template <int DP>
 __device__ __forceinline__ int lds_chunk(int r, int c) {
-  return r * (DP * 2) + ((c ^ row_swizzle<DP>(r)) << 4);
+  return r * (DP * 2) + ((c ^ row_swizzle(r)) << 4);
 }
 
-// Global -> registers -> LDS of a tile of ROWS rows by 256 threads. Rows past
-// the sample's end are its last row again (finite wherever the sample is;
-// what they give is masked or not stored), elements past the width are 0.
+// Copies of a tile of ROWS rows from global memory straight into LDS, by 256
+// threads and 16 bytes a lane. A wave's copy fills 64 consecutive chunks of
+// LDS, so a lane picks the chunk of the row that belongs in its place. Rows
+// past the sample's end are its last row again (finite wherever the sample is;
+// what they give is masked or not stored). Chunks past the width are not
+// copied: zero_pad clears them once.
 template <int DP, int ROWS>
-struct Stage {
+struct TileCopy {
   static constexpr int kChunks = DP / 8;
-  static constexpr int kPer = ROWS * kChunks / 256;
-  u32x4 r[kPer];
-  // base: the sample's first row of this head; row0: the tile's first row
-  __device__ __forceinline__ void load(const void* base, int64_t stride, int row0, int len, int width) {
+  static constexpr int kStep = 256 / kChunks;  // rows of one round of copies: a multiple of 8, so
+  static constexpr int kPer = ROWS / kStep;    // a lane's chunk is the same in every round
+  uint32_t off;     // the lane's byte offset in the first round
+  uint32_t stride;  // bytes from row to row
+  int row;          // the lane's row in the first round
+  bool in;
+  __device__ __forceinline__ TileCopy(int64_t elems, int width) : stride(uint32_t(elems * 2)) {
+    row = int(threadIdx.x) / kChunks;
+    const int chunk = int(threadIdx.x) % kChunks ^ row_swizzle(row);
+    in = chunk * 8 < width;
+    off = uint32_t(row) * stride + uint32_t(chunk) * 16;
+  }
+  // base: the tile's first row; rows: the sample's rows from there on (>= 1)
+  __device__ __forceinline__ void copy(const char* base, int rows, char* lds) const {
+    if (!in) return;
+    const int wave = __builtin_amdgcn_readfirstlane(int(threadIdx.x >> 6));
 #pragma unroll
     for (int j = 0; j < kPer; ++j) {
-      const int i = threadIdx.x + j * 256;
-      const int c = i % kChunks;
-      int row = row0 + i / kChunks;
-      row = row < len ? row : len - 1;
-      const bool in = c * 8 < width;
-      const char* p = static_cast<const char*>(base) + (int64_t(row) * stride + (in ? c * 8 : 0)) * 2;
-      u32x4 v = *reinterpret_cast<const u32x4*>(p);
-      r[j] = in ? v : u32x4{0, 0, 0, 0};
+      uint32_t o = off;
+      if (rows < ROWS) o -= uint32_t(max(row + j * kStep - (rows - 1), 0)) * stride;
+      // o wraps below 0 only together with the round's start: the sum is taken in 32 bits
+      const uint32_t at = o + uint32_t(j * kStep) * stride;
+      __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(base + at),
+                                       (__attribute__((address_space(3))) void*)(lds + j * 4096 + wave * 1024),
+                                       16, 0, 0);
     }
   }
-  __device__ __forceinline__ void store(char* lds) const {
+  __device__ __forceinline__ void zero_pad(char* lds) const {
+    if (in) return;
 #pragma unroll
-    for (int j = 0; j < kPer; ++j) {
-      const int i = threadIdx.x + j * 256;
-      *reinterpret_cast<u32x4*>(lds + lds_chunk<DP>(i / kChunks, i % kChunks)) = r[j];
-    }
+    for (int j = 0; j < kPer; ++j)
+      *reinterpret_cast<u32x4*>(lds + j * 4096 + threadIdx.x * 16) = u32x4{0, 0, 0, 0};
   }
 };
+
+// This wave's copies into LDS have landed; with the barrier, every wave's.
+__device__ __forceinline__ void copies_landed() {
+  __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0)
+  __syncthreads();
+}
 
 // A operand (32 rows x 16 elements): row `row0 + lane % 32` of an LDS tile.
 template <class M, int DP>
@@ -247,15 +265,16 @@ __device__ inline void zero_rows(void* base, const int64_t* s, int64_t head, int
 
 constexpr int kRows = 128;  // columns of a workgroup: 32 per wave
 constexpr int kKeys = 64;   // keys of a tile (forward, dq)
-constexpr int kQs = 32;     // queries of a tile (dk, dv)
+constexpr int kQs = 64;     // queries of a tile (dk, dv)
 
 // ------------------------------------------------------------------ forward --
 template <class M, int DP>
-__global__ void __launch_bounds__(256) at_forward(const Attention a) {
+__global__ void __launch_bounds__(256, 2) at_forward(const Attention a) {
   typedef typename M::T T;
   constexpr int DT = DP / 32, DC = DP / 16;
   constexpr int kTileBytes = kKeys * DP * 2;
-  __shared__ __align__(16) char lds[4 * kTileBytes];  // k, v; two buffers
+  // two buffers, apart by name so that a read waits for its own buffer's copies only
+  __shared__ __align__(16) char lk0[kTileBytes], lv0[kTileBytes], lk1[kTileBytes], lv1[kTileBytes];
   const uint32_t id = xcd_logical(blockIdx.x, gridDim.x);
   const uint32_t head = id / a.tiles;
   if (head >= uint32_t(a.heads)) return;
@@ -263,7 +282,7 @@ __global__ void __launch_bounds__(256) at_forward(const Attention a) {
   // the last tiles of the packed rows first: long samples' last rows see most keys
   if (!find_tile<kRows>(a, a.tiles - 1 - id % a.tiles, &t)) return;
   const int width = a.width;
-  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, half = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(int(threadIdx.x >> 6)), lane = threadIdx.x & 63, half = lane >> 5;
   T* o = static_cast<T*>(a.o) + t.begin * a.o_s[0] + head * a.o_s[1];
   float* lse = a.lse + int64_t(head) * a.T + t.begin;
   if (t.sample == a.n) {
@@ -292,30 +311,27 @@ __global__ void __launch_bounds__(256) at_forward(const Attention a) {
   const float c2 = a.scale * kLog2e;
 
   const int n_tiles = (min(t.len, t.m0 + kRows) + kKeys - 1) / kKeys;
-  Stage<DP, kKeys> sk, sv;
-  sk.load(kb, a.k_s[0], 0, t.len, width);
-  sv.load(vb, a.v_s[0], 0, t.len, width);
-  sk.store(lds);
-  sv.store(lds + kTileBytes);
-  if (n_tiles > 1) {
-    sk.load(kb, a.k_s[0], kKeys, t.len, width);
-    sv.load(vb, a.v_s[0], kKeys, t.len, width);
+  const TileCopy<DP, kKeys> ck(a.k_s[0], width), cv(a.v_s[0], width);
+  const char* kt = reinterpret_cast<const char*>(kb);
+  const char* vt = reinterpret_cast<const char*>(vb);
+  if (width < DP) {
+    ck.zero_pad(lk0);
+    ck.zero_pad(lk1);
+    cv.zero_pad(lv0);
+    cv.zero_pad(lv1);
   }
-  for (int j = 0; j < n_tiles; ++j) {
-    char* lk = lds + (j & 1) * 2 * kTileBytes;
-    char* lv = lk + kTileBytes;
-    __syncthreads();  // tile j is in LDS, and tile j - 1 is done with
-    if (j + 1 < n_tiles) {
-      char* next = lds + ((j + 1) & 1) * 2 * kTileBytes;
-      sk.store(next);
-      sv.store(next + kTileBytes);
-      if (j + 2 < n_tiles) {
-        sk.load(kb, a.k_s[0], (j + 2) * kKeys, t.len, width);
-        sv.load(vb, a.v_s[0], (j + 2) * kKeys, t.len, width);
-      }
-    }
+  ck.copy(kt, t.len, lk0);
+  cv.copy(vt, t.len, lv0);
+  auto step = [&](int j, const char* lk, const char* lv, char* next_k, char* next_v) {
+    copies_landed();  // tile j is in LDS, and tile j - 1 is done with
     const int k0 = j * kKeys;
-    if (k0 > q0 + 31) continue;  // all later than this wave's queries
+    if (j + 1 < n_tiles) {
+      kt += int64_t(ck.stride) * kKeys;
+      vt += int64_t(cv.stride) * kKeys;
+      ck.copy(kt, t.len - k0 - kKeys, next_k);
+      cv.copy(vt, t.len - k0 - kKeys, next_v);
+    }
+    if (k0 > q0 + 31) return;  // all later than this wave's queries
     f32x16 s[2];
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
@@ -360,6 +376,10 @@ __global__ void __launch_bounds__(256) at_forward(const Attention a) {
 #pragma unroll
         for (int i = 0; i < DT; ++i) acc[i] = M::mma(frag_col<M, DP>(lv, 32 * u + 16 * c, 32 * i), p, acc[i]);
       }
+  };
+  for (int j = 0; j < n_tiles; j += 2) {
+    step(j, lk0, lv0, lk1, lv1);
+    if (j + 1 < n_tiles) step(j + 1, lk1, lv1, lk0, lv0);
   }
   l = half_sum(l);
   if (qi < t.len) {
@@ -371,18 +391,18 @@ __global__ void __launch_bounds__(256) at_forward(const Attention a) {
 // ----------------------------------------------------------------------- dq --
 // Also writes delta_i = do_i.o_i for the dk/dv kernel.
 template <class M, int DP>
-__global__ void __launch_bounds__(256) at_dq(const Attention a) {
+__global__ void __launch_bounds__(256, 2) at_dq(const Attention a) {
   typedef typename M::T T;
   constexpr int DT = DP / 32, DC = DP / 16;
   constexpr int kTileBytes = kKeys * DP * 2;
-  __shared__ __align__(16) char lds[4 * kTileBytes];
+  __shared__ __align__(16) char lk0[kTileBytes], lv0[kTileBytes], lk1[kTileBytes], lv1[kTileBytes];
   const uint32_t id = xcd_logical(blockIdx.x, gridDim.x);
   const uint32_t head = id / a.tiles;
   if (head >= uint32_t(a.heads)) return;
   Tile t;
   if (!find_tile<kRows>(a, a.tiles - 1 - id % a.tiles, &t)) return;
   const int width = a.width;
-  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, half = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(int(threadIdx.x >> 6)), lane = threadIdx.x & 63, half = lane >> 5;
   if (t.sample == a.n) {
     zero_rows<M>(a.dq, a.dq_s, head, t.begin + t.m0, min(kRows, t.len - t.m0), width);
     return;
@@ -418,30 +438,28 @@ __global__ void __launch_bounds__(256) at_dq(const Attention a) {
     for (int e = 0; e < 16; ++e) acc[i][e] = 0.0f;
 
   const int n_tiles = (min(t.len, t.m0 + kRows) + kKeys - 1) / kKeys;
-  Stage<DP, kKeys> sk, sv;
-  sk.load(kb, a.k_s[0], 0, t.len, width);
-  sv.load(vb, a.v_s[0], 0, t.len, width);
-  sk.store(lds);
-  sv.store(lds + kTileBytes);
-  if (n_tiles > 1) {
-    sk.load(kb, a.k_s[0], kKeys, t.len, width);
-    sv.load(vb, a.v_s[0], kKeys, t.len, width);
+  const TileCopy<DP, kKeys> ck(a.k_s[0], width), cv(a.v_s[0], width);
+  const char* kt = reinterpret_cast<const char*>(kb);
+  const char* vt = reinterpret_cast<const char*>(vb);
+  if (width < DP) {
+    ck.zero_pad(lk0);
+    ck.zero_pad(lk1);
+    cv.zero_pad(lv0);
+    cv.zero_pad(lv1);
   }
-  for (int j = 0; j < n_tiles; ++j) {
-    char* lk = lds + (j & 1) * 2 * kTileBytes;
-    char* lv = lk + kTileBytes;
-    __syncthreads();
-    if (j + 1 < n_tiles) {
-      char* next = lds + ((j + 1) & 1) * 2 * kTileBytes;
-      sk.store(next);
-      sv.store(next + kTileBytes);
-      if (j + 2 < n_tiles) {
-        sk.load(kb, a.k_s[0], (j + 2) * kKeys, t.len, width);
-        sv.load(vb, a.v_s[0], (j + 2) * kKeys, t.len, width);
-      }
-    }
+  ck.copy(kt, t.len, lk0);
+  cv.copy(vt, t.len, lv0);
+  auto step = [&](int j, const char* lk, const char* lv, char* next_k, char* next_v) {
+    copies_landed();
     const int k0 = j * kKeys;
-    if (k0 > q0 + 31) continue;
+    if (j + 1 < n_tiles) {
+      kt += int64_t(ck.stride) * kKeys;
+      vt += int64_t(cv.stride) * kKeys;
+      ck.copy(kt, t.len - k0 - kKeys, next_k);
+      cv.copy(vt, t.len - k0 - kKeys, next_v);
+    }
+    if (k0 > q0 + 31) return;
+    const bool edge = k0 + kKeys - 1 > q0;
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
       f32x16 s, dp;
@@ -452,12 +470,12 @@ __global__ void __launch_bounds__(256) at_dq(const Attention a) {
         s = M::mma(frag_row<M, DP>(lk, 32 * u, 2 * c), q[c], s);
         dp = M::mma(frag_row<M, DP>(lv, 32 * u, 2 * c), d[c], dp);
       }
-      const bool edge = k0 + kKeys - 1 > q0;
 #pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        const float p = exp2_fast(fmaf(s[e], c2, -lc));
-        const float g = p * (dp[e] - delta);
-        s[e] = edge && k0 + 32 * u + acc_row(e) + 4 * half > qi ? 0.0f : g;
+      for (int e = 0; e < 16; ++e) s[e] = exp2_fast(fmaf(s[e], c2, -lc)) * (dp[e] - delta);
+      if (edge) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+          if (k0 + 32 * u + acc_row(e) + 4 * half > qi) s[e] = 0.0f;
       }
 #pragma unroll
       for (int c = 0; c < 2; ++c) {
@@ -466,6 +484,10 @@ __global__ void __launch_bounds__(256) at_dq(const Attention a) {
         for (int i = 0; i < DT; ++i) acc[i] = M::mma(frag_col<M, DP>(lk, 32 * u + 16 * c, 32 * i), p, acc[i]);
       }
     }
+  };
+  for (int j = 0; j < n_tiles; j += 2) {
+    step(j, lk0, lv0, lk1, lv1);
+    if (j + 1 < n_tiles) step(j + 1, lk1, lv1, lk0, lv0);
   }
   if (qi < t.len)
     store_columns<M, DT>(static_cast<T*>(a.dq) + qr * a.dq_s[0] + head * a.dq_s[1], acc, a.scale, width);
@@ -476,19 +498,19 @@ __global__ void __launch_bounds__(256) at_dq(const Attention a) {
 // order and over the query tiles from the diagonal on. Nothing is added to
 // memory from two places, so the sums' order never changes.
 template <class M, int DP>
-__global__ void __launch_bounds__(256) at_dkv(const Attention a) {
+__global__ void __launch_bounds__(256, 2) at_dkv(const Attention a) {
   typedef typename M::T T;
   constexpr int DT = DP / 32, DC = DP / 16;
   constexpr int kTileBytes = kQs * DP * 2;
-  constexpr int kBuf = 2 * kTileBytes + 2 * kQs * 4;  // q, do, lse, delta
-  __shared__ __align__(16) char lds[2 * kBuf];
+  __shared__ __align__(16) char lq0[kTileBytes], ld0[kTileBytes], lq1[kTileBytes], ld1[kTileBytes];
+  __shared__ __align__(16) float ls0[2 * kQs], ls1[2 * kQs];  // a tile's lse and delta
   const uint32_t id = xcd_logical(blockIdx.x, gridDim.x);
   const uint32_t kv = id / a.tiles;
   if (kv >= uint32_t(a.kv_heads)) return;
   Tile t;
   if (!find_tile<kRows>(a, id % a.tiles, &t)) return;  // a sample's first keys are seen by most queries
   const int width = a.width;
-  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, half = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(int(threadIdx.x >> 6)), lane = threadIdx.x & 63, half = lane >> 5;
   if (t.sample == a.n) {
     const int rows = min(kRows, t.len - t.m0);
     zero_rows<M>(a.dk, a.dk_s, kv, t.begin + t.m0, rows, width);
@@ -515,73 +537,86 @@ __global__ void __launch_bounds__(256) at_dkv(const Attention a) {
 
   const int group = a.heads / a.kv_heads;
   const int j0 = t.m0 / kQs;  // the first query tile that sees the tile's keys
-  const int per_head = (t.len + kQs - 1) / kQs - j0;
-  const int n_tiles = per_head * group;
-  Stage<DP, kQs> sq, sd;
-  float stat = 0.0f;  // of threads 0..31 the tile's lse, of 32..63 its delta
-  auto load = [&](int i) {
-    const int64_t h = int64_t(kv) * group + i / per_head;
-    const int row0 = (j0 + i % per_head) * kQs;
-    sq.load(static_cast<const T*>(a.q) + t.begin * a.q_s[0] + h * a.q_s[1], a.q_s[0], row0, t.len, width);
-    sd.load(static_cast<const T*>(a.d_o) + t.begin * a.do_s[0] + h * a.do_s[1], a.do_s[0], row0, t.len, width);
+  const int j1 = (t.len + kQs - 1) / kQs;
+  const int n_tiles = (j1 - j0) * group;
+  const TileCopy<DP, kQs> cq(a.q_s[0], width), cd(a.do_s[0], width);
+  // the tile copied next: query head and tile of the sample
+  int64_t h_next = int64_t(kv) * group;
+  int j_next = j0;
+  float stat = 0.0f;
+  auto copy = [&](char* lq, char* ld) {
+    const int row0 = j_next * kQs;
+    cq.copy(reinterpret_cast<const char*>(static_cast<const T*>(a.q) + (t.begin + row0) * a.q_s[0] + h_next * a.q_s[1]),
+            t.len - row0, lq);
+    cd.copy(reinterpret_cast<const char*>(static_cast<const T*>(a.d_o) + (t.begin + row0) * a.do_s[0] + h_next * a.do_s[1]),
+            t.len - row0, ld);
     if (threadIdx.x < 2 * kQs) {
       const int row = row0 + int(threadIdx.x % kQs);
-      const int64_t at = h * a.T + t.begin + min(row, t.len - 1);
+      const int64_t at = h_next * a.T + t.begin + min(row, t.len - 1);
       // past the end: an infinite lse makes P and dS exactly 0
       stat = threadIdx.x < kQs ? (row < t.len ? a.lse[at] * kLog2e : INFINITY) : a.delta[at];
     }
-  };
-  auto store = [&](char* buf) {
-    sq.store(buf);
-    sd.store(buf + kTileBytes);
-    if (threadIdx.x < 2 * kQs) reinterpret_cast<float*>(buf + 2 * kTileBytes)[threadIdx.x] = stat;
-  };
-  load(0);
-  store(lds);
-  if (n_tiles > 1) load(1);
-  for (int i = 0; i < n_tiles; ++i) {
-    const char* lq = lds + (i & 1) * kBuf;
-    const char* ld = lq + kTileBytes;
-    const float* ls = reinterpret_cast<const float*>(lq + 2 * kTileBytes);
-    __syncthreads();
-    if (i + 1 < n_tiles) {
-      store(lds + ((i + 1) & 1) * kBuf);
-      if (i + 2 < n_tiles) load(i + 2);
+    if (++j_next == j1) {
+      j_next = j0;
+      ++h_next;
     }
-    const int q0 = (j0 + i % per_head) * kQs;
-    if (q0 + kQs - 1 < k0) continue;  // all earlier than this wave's keys
-    f32x16 s, dp;
+  };
+  if (width < DP) {
+    cq.zero_pad(lq0);
+    cq.zero_pad(lq1);
+    cd.zero_pad(ld0);
+    cd.zero_pad(ld1);
+  }
+  copy(lq0, ld0);
+  int q0 = t.m0;
+  auto step = [&](int i, const char* lq, const char* ld, float* ls, char* next_q, char* next_d) {
+    if (threadIdx.x < 2 * kQs) ls[threadIdx.x] = stat;
+    copies_landed();
+    if (i + 1 < n_tiles) copy(next_q, next_d);
+    const int row0 = q0;
+    q0 = q0 + kQs < t.len ? q0 + kQs : t.m0;
+    if (row0 + kQs - 1 < k0) return;  // all earlier than this wave's keys
+#pragma unroll 1
+    for (int u = 0; u < kQs / 32; ++u) {
+      f32x16 s, dp;
 #pragma unroll
-    for (int e = 0; e < 16; ++e) s[e] = dp[e] = 0.0f;
+      for (int e = 0; e < 16; ++e) s[e] = dp[e] = 0.0f;
 #pragma unroll
-    for (int c = 0; c < DC; ++c) {
-      s = M::mma(frag_row<M, DP>(lq, 0, 2 * c), k[c], s);
-      dp = M::mma(frag_row<M, DP>(ld, 0, 2 * c), v[c], dp);
-    }
-    const bool edge = q0 < k0 + 31;
+      for (int c = 0; c < DC; ++c) {
+        s = M::mma(frag_row<M, DP>(lq, 32 * u, 2 * c), k[c], s);
+        dp = M::mma(frag_row<M, DP>(ld, 32 * u, 2 * c), v[c], dp);
+      }
 #pragma unroll
-    for (int b = 0; b < 4; ++b) {
-      const f32x4 lc = *reinterpret_cast<const f32x4*>(ls + 8 * b + 4 * half);
-      const f32x4 de = *reinterpret_cast<const f32x4*>(ls + kQs + 8 * b + 4 * half);
+      for (int b = 0; b < 4; ++b) {
+        const f32x4 lc = *reinterpret_cast<const f32x4*>(ls + 32 * u + 8 * b + 4 * half);
+        const f32x4 de = *reinterpret_cast<const f32x4*>(ls + kQs + 32 * u + 8 * b + 4 * half);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const int r = 4 * b + e;
-        float p = exp2_fast(fmaf(s[r], c2, -lc[e]));
-        if (edge && q0 + acc_row(r) + 4 * half < ki) p = 0.0f;
-        s[r] = p;
-        dp[r] = p * (dp[r] - de[e]);
+        for (int e = 0; e < 4; ++e) {
+          const int r = 4 * b + e;
+          s[r] = exp2_fast(fmaf(s[r], c2, -lc[e]));
+          dp[r] = s[r] * (dp[r] - de[e]);
+        }
+      }
+      if (row0 < k0 + 31) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+          if (row0 + 32 * u + acc_row(r) + 4 * half < ki) s[r] = dp[r] = 0.0f;
+      }
+#pragma unroll
+      for (int c = 0; c < 2; ++c) {
+        const typename M::V8 p = pack8<M>(s, c);
+        const typename M::V8 g = pack8<M>(dp, c);
+#pragma unroll
+        for (int x = 0; x < DT; ++x) {
+          dv[x] = M::mma(frag_col<M, DP>(ld, 32 * u + 16 * c, 32 * x), p, dv[x]);
+          dk[x] = M::mma(frag_col<M, DP>(lq, 32 * u + 16 * c, 32 * x), g, dk[x]);
+        }
       }
     }
-#pragma unroll
-    for (int c = 0; c < 2; ++c) {
-      const typename M::V8 p = pack8<M>(s, c);
-      const typename M::V8 g = pack8<M>(dp, c);
-#pragma unroll
-      for (int x = 0; x < DT; ++x) {
-        dv[x] = M::mma(frag_col<M, DP>(ld, 16 * c, 32 * x), p, dv[x]);
-        dk[x] = M::mma(frag_col<M, DP>(lq, 16 * c, 32 * x), g, dk[x]);
-      }
-    }
+  };
+  for (int i = 0; i < n_tiles; i += 2) {
+    step(i, lq0, ld0, ls0, lq1, ld1);
+    if (i + 1 < n_tiles) step(i + 1, lq1, ld1, ls1, lq0, ld0);
   }
   if (ki < t.len) {
     store_columns<M, DT>(static_cast<T*>(a.dk) + kr * a.dk_s[0] + kv * a.dk_s[1], dk, a.scale, width);
@@ -598,8 +633,8 @@ int check_array(const char* name, const void* p, const int64_t* s, int64_t heads
     return fail(NOPFS_EINVAL, std::string(name) + " and its strides must be multiples of 16 bytes");
   if (s[0] < width || (heads > 1 && s[1] < width))
     return fail(NOPFS_EINVAL, std::string(name) + ": strides smaller than a head");
-  if (s[0] > (int64_t(1) << 40) || s[1] > (int64_t(1) << 40))
-    return fail(NOPFS_ERANGE, std::string(name) + ": strides must be <= 2^40");
+  if (s[0] > (int64_t(1) << 23) || s[1] > (int64_t(1) << 40))
+    return fail(NOPFS_ERANGE, std::string(name) + ": the token stride must be <= 2^23, the head stride <= 2^40");
   return NOPFS_OK;
 }
 
