@@ -429,7 +429,7 @@ typedef struct nopfs_attention {
  *          but in-bounds results).
  *   lse:   float [heads][T].
  * Rows from start[n] on belong to no sample: o = 0 and lse = -inf, and what q,
- * k and v hold there is not read. Errors: EINVAL, ERANGE, EDEVICE. */
+ * k and v hold there is not read. Errors: EINVAL, ERANGE, ENOMEM, EDEVICE. */
 int nopfs_packed_attention(const nopfs_attention* a, const void* q, const void* k, const void* v,
                            const int32_t* start, void* o, float* lse, void* hip_stream);
 

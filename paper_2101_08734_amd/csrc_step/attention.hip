@@ -67,9 +67,14 @@ struct Attention {
   float* delta;  // [heads][T] (scratch)
   const int32_t* start;
   uint32_t tiles;  // an upper bound of the row tiles
+  const int2* order;  // the tiles' (sample, first row), costliest first, or NULL
 };
 
 constexpr float kLog2e = 1.4426950408889634f;
+// The running maximum follows a row's scores only when they pass it by more
+// than this (base 2): until then exponentials up to 2^8 are summed, exact to
+// the same relative error, and the sums need no rescaling.
+constexpr float kSlack = 8.0f;
 
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 
@@ -87,37 +92,119 @@ __device__ __forceinline__ float half_sum(float v) {
 // start[s] / BM + s: consecutive samples' numbers never overlap, since
 // ceil((b - a) / BM) <= b / BM - a / BM + 1, and no pass over the lengths is
 // needed before the launch. The rows behind the last sample count as one more
-// sample. Returns false where the tile's number belongs to no row.
+// sample.
 struct Tile {
   int32_t sample;   // n: the rows of no sample
   int64_t begin;    // the sample's first row
   int32_t len, m0;  // its rows, and the tile's first row in it
 };
+
+// start[s], within the rows whatever the array holds; 0 before the first.
+__device__ __forceinline__ int64_t sample_begin(const Attention& a, int32_t s) {
+  const int64_t v = s <= 0 ? 0 : a.start[s];
+  return v < 0 ? 0 : (v > a.T ? a.T : v);
+}
+
+// Completes a tile whose sample and first row are known; false where the row
+// is none of the sample's.
+__device__ __forceinline__ bool finish_tile(const Attention& a, Tile* t) {
+  t->begin = sample_begin(a, t->sample);
+  const int64_t end = t->sample < a.n ? sample_begin(a, t->sample + 1) : a.T;
+  t->len = int32_t(end > t->begin ? end - t->begin : 0);
+  return t->m0 >= 0 && t->m0 < t->len;
+}
+
 template <int BM>
 __device__ inline bool find_tile(const Attention& a, uint32_t tile, Tile* t) {
   const int lane = __lane_id();
-  auto at = [&](int32_t s) -> int64_t {
-    int64_t v = s <= 0 ? 0 : a.start[s];
-    return v < 0 ? 0 : (v > a.T ? a.T : v);
-  };
   // the last s in [lo, hi] whose number is <= tile, 64 candidates at a time
   int32_t lo = 0, hi = a.n;
   while (hi > lo) {
     const int32_t step = (hi - lo + 63) >> 6;  // candidates lo + step * (lane + 1)
     const int64_t cand = int64_t(lo) + int64_t(step) * (lane + 1);
-    const bool le = cand <= hi && at(int32_t(cand)) / BM + cand <= int64_t(tile);
+    const bool le = cand <= hi && sample_begin(a, int32_t(cand)) / BM + cand <= int64_t(tile);
     const int k = __popcll(__ballot(le));  // monotone: the first k hold
     const int64_t top = int64_t(lo) + int64_t(step) * (k + 1) - 1;
     lo += step * k;
     hi = top < hi ? int32_t(top) : hi;
   }
   t->sample = lo;
-  t->begin = at(lo);
-  const int64_t end = lo < a.n ? at(lo + 1) : a.T;
-  t->len = int32_t(end > t->begin ? end - t->begin : 0);
-  const int64_t m0 = (int64_t(tile) - (t->begin / BM + lo)) * BM;
-  t->m0 = int32_t(m0);
-  return m0 >= 0 && m0 < t->len;
+  t->m0 = int32_t((int64_t(tile) - (sample_begin(a, lo) / BM + lo)) * BM);
+  return finish_tile(a, t);
+}
+
+// The workgroup's tile: the rank-th of the order, or without one the tiles as
+// packed, from the last (kLast) or from the first.
+template <int BM, bool kLast>
+__device__ __forceinline__ bool pick_tile(const Attention& a, uint32_t rank, Tile* t) {
+  if (a.order) {
+    const int2 e = a.order[rank];
+    t->sample = e.x;
+    t->m0 = e.y;
+    return e.x >= 0 && finish_tile(a, t);
+  }
+  return find_tile<BM>(a, kLast ? a.tiles - 1 - rank : rank, t);
+}
+
+// Orders the tiles by what they cost, so that the longest work starts first:
+// by their first row (a query tile sees the keys up to itself, kByRow), or by
+// the rows from there to the sample's end (a key tile). A counting sort by one
+// workgroup; which of two tiles of one class comes first is left open (no
+// result depends on it).
+constexpr int kClasses = 1024;
+struct OrderJob {
+  int2* order;
+  uint32_t tiles;
+  int32_t rows;  // of a tile
+  bool by_row;
+};
+__global__ void __launch_bounds__(1024) at_order(const Attention a, const OrderJob j0, const OrderJob j1) {
+  __shared__ uint32_t count[kClasses];
+  __shared__ uint32_t tmp[65];
+  const OrderJob& j = blockIdx.x == 0 ? j0 : j1;
+  int shift = 0;
+  while ((a.T / j.rows) >> shift >= kClasses) ++shift;
+  count[threadIdx.x] = 0;
+  auto tile = [&](uint32_t i, Tile* t) {
+    int32_t lo = 0, hi = a.n;
+    while (hi > lo) {
+      const int32_t mid = lo + (hi - lo + 1) / 2;
+      if (sample_begin(a, mid) / j.rows + mid <= int64_t(i)) lo = mid;
+      else hi = mid - 1;
+    }
+    t->sample = lo;
+    t->m0 = int32_t((int64_t(i) - (sample_begin(a, lo) / j.rows + lo)) * j.rows);
+    if (!finish_tile(a, t)) return -1;
+    const int cost = (j.by_row ? t->m0 : t->len - t->m0 - 1) / j.rows;
+    return kClasses - 1 - min(lo == a.n ? 0 : cost >> shift, kClasses - 1);
+  };
+  __syncthreads();
+  for (uint32_t i = threadIdx.x; i < j.tiles; i += 1024) {
+    Tile t;
+    const int c = tile(i, &t);
+    if (c >= 0) atomicAdd(&count[c], 1u);
+  }
+  __syncthreads();
+  uint32_t total;
+  const uint32_t first = block_exclusive_scan(count[threadIdx.x], tmp, &total);
+  count[threadIdx.x] = first;
+  __syncthreads();
+  for (uint32_t i = threadIdx.x; i < j.tiles; i += 1024) {
+    Tile t;
+    const int c = tile(i, &t);
+    if (c >= 0) j.order[atomicAdd(&count[c], 1u)] = int2{t.sample, t.m0};
+  }
+  for (uint32_t i = total + threadIdx.x; i < j.tiles; i += 1024) j.order[i] = int2{-1, 0};
+}
+
+// Workgroup -> (tile, head): all heads of a tile are neighbours, so every die
+// (workgroup b runs on die b mod 8) gets the same share of each sample; where
+// the heads divide by 8, a die has neighbouring heads, which share kv heads in
+// its L2.
+__device__ __forceinline__ void tile_and_head(uint32_t b, uint32_t heads, uint32_t* tile, uint32_t* head) {
+  *tile = b / heads;
+  const uint32_t h = b % heads;
+  *head = heads % 8 == 0 ? (h % 8) * (heads / 8) + h / 8 : h;
 }
 
 __device__ __forceinline__ int row_swizzle(int r) { return ((r & 3) << 1) | ((r >> 2) & 1); }
@@ -171,9 +258,12 @@ struct TileCopy {
   }
 };
 
-// This wave's copies into LDS have landed; with the barrier, every wave's.
+// This wave's copies into LDS have landed, all but the last kBehind; with the
+// barrier, every wave's.
+template <int kBehind>
 __device__ __forceinline__ void copies_landed() {
-  __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0)
+  static_assert(kBehind < 64, "vmcnt has 6 bits");
+  __builtin_amdgcn_s_waitcnt(0x0f70 | (kBehind & 15) | (kBehind >> 4) << 14);  // vmcnt(kBehind)
   __syncthreads();
 }
 
@@ -254,6 +344,32 @@ __device__ __forceinline__ void store_columns(typename M::T* row, const f32x16* 
     }
 }
 
+// A wave's accumulators through LDS to the wave that owns the same columns,
+// which adds them: acc = acc * f0 + theirs * f1.
+template <int DT>
+__device__ __forceinline__ void give_columns(char* lds, const f32x16* acc) {
+  const int lane = threadIdx.x & 63;
+#pragma unroll
+  for (int t = 0; t < DT; ++t)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const f32x4 v = {acc[t][4 * i], acc[t][4 * i + 1], acc[t][4 * i + 2], acc[t][4 * i + 3]};
+      *reinterpret_cast<f32x4*>(lds + ((t * 4 + i) * 64 + lane) * 16) = v;
+    }
+}
+template <int DT>
+__device__ __forceinline__ void take_columns(const char* lds, f32x16* acc, float f0, float f1) {
+  const int lane = threadIdx.x & 63;
+#pragma unroll
+  for (int t = 0; t < DT; ++t)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const f32x4 v = *reinterpret_cast<const f32x4*>(lds + ((t * 4 + i) * 64 + lane) * 16);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) acc[t][4 * i + e] = acc[t][4 * i + e] * f0 + v[e] * f1;
+    }
+}
+
 template <class M>
 __device__ inline void zero_rows(void* base, const int64_t* s, int64_t head, int64_t row0, int rows, int width) {
   const int per = width / 8;
@@ -263,26 +379,28 @@ __device__ inline void zero_rows(void* base, const int64_t* s, int64_t head, int
   }
 }
 
-constexpr int kRows = 128;  // columns of a workgroup: 32 per wave
-constexpr int kKeys = 64;   // keys of a tile (forward, dq)
-constexpr int kQs = 64;     // queries of a tile (dk, dv)
+// A workgroup's 4 waves are strips of 32 columns, times splits of the other
+// side: with two splits, two waves share a strip's columns, each takes every
+// other block of the tiles, and their sums are joined through LDS at the end.
+constexpr int kKeys = 64;  // keys of a tile (forward, dq)
 
 // ------------------------------------------------------------------ forward --
-template <class M, int DP>
+template <class M, int DP, int kSplits>
 __global__ void __launch_bounds__(256, 2) at_forward(const Attention a) {
   typedef typename M::T T;
   constexpr int DT = DP / 32, DC = DP / 16;
+  constexpr int kStrips = 4 / kSplits, kRows = 32 * kStrips, NU = 2 / kSplits;
   constexpr int kTileBytes = kKeys * DP * 2;
   // two buffers, apart by name so that a read waits for its own buffer's copies only
   __shared__ __align__(16) char lk0[kTileBytes], lv0[kTileBytes], lk1[kTileBytes], lv1[kTileBytes];
-  const uint32_t id = xcd_logical(blockIdx.x, gridDim.x);
-  const uint32_t head = id / a.tiles;
-  if (head >= uint32_t(a.heads)) return;
+  uint32_t tile, head;
+  tile_and_head(blockIdx.x, uint32_t(a.heads), &tile, &head);
   Tile t;
   // the last tiles of the packed rows first: long samples' last rows see most keys
-  if (!find_tile<kRows>(a, a.tiles - 1 - id % a.tiles, &t)) return;
+  if (!pick_tile<kRows, true>(a, tile, &t)) return;
   const int width = a.width;
   const int wave = __builtin_amdgcn_readfirstlane(int(threadIdx.x >> 6)), lane = threadIdx.x & 63, half = lane >> 5;
+  const int strip = wave % kStrips, split = kSplits == 1 ? 0 : wave / kStrips;
   T* o = static_cast<T*>(a.o) + t.begin * a.o_s[0] + head * a.o_s[1];
   float* lse = a.lse + int64_t(head) * a.T + t.begin;
   if (t.sample == a.n) {
@@ -294,7 +412,7 @@ __global__ void __launch_bounds__(256, 2) at_forward(const Attention a) {
   const int64_t kv = head / (a.heads / a.kv_heads);
   const T* kb = static_cast<const T*>(a.k) + t.begin * a.k_s[0] + kv * a.k_s[1];
   const T* vb = static_cast<const T*>(a.v) + t.begin * a.v_s[0] + kv * a.v_s[1];
-  const int q0 = t.m0 + 32 * wave;  // the wave's first query
+  const int q0 = t.m0 + 32 * strip;  // the wave's first query
   const int qi = q0 + (lane & 31);  // the lane's query
   const int qr = min(qi, t.len - 1);
   const T* qrow = static_cast<const T*>(a.q) + (t.begin + qr) * a.q_s[0] + head * a.q_s[1];
@@ -308,7 +426,7 @@ __global__ void __launch_bounds__(256, 2) at_forward(const Attention a) {
 #pragma unroll
     for (int e = 0; e < 16; ++e) acc[i][e] = 0.0f;
   float m = -INFINITY, l = 0.0f;  // l: over the lane's own keys
-  const float c2 = a.scale * kLog2e;
+  const float c2 = a.scale * kLog2e, slack = kSlack / c2;
 
   const int n_tiles = (min(t.len, t.m0 + kRows) + kKeys - 1) / kKeys;
   const TileCopy<DP, kKeys> ck(a.k_s[0], width), cv(a.v_s[0], width);
@@ -323,7 +441,7 @@ __global__ void __launch_bounds__(256, 2) at_forward(const Attention a) {
   ck.copy(kt, t.len, lk0);
   cv.copy(vt, t.len, lv0);
   auto step = [&](int j, const char* lk, const char* lv, char* next_k, char* next_v) {
-    copies_landed();  // tile j is in LDS, and tile j - 1 is done with
+    copies_landed<0>();  // tile j is in LDS, and tile j - 1 is done with
     const int k0 = j * kKeys;
     if (j + 1 < n_tiles) {
       kt += int64_t(ck.stride) * kKeys;
@@ -331,55 +449,79 @@ __global__ void __launch_bounds__(256, 2) at_forward(const Attention a) {
       ck.copy(kt, t.len - k0 - kKeys, next_k);
       cv.copy(vt, t.len - k0 - kKeys, next_v);
     }
-    if (k0 > q0 + 31) return;  // all later than this wave's queries
-    f32x16 s[2];
+    const int kb = k0 + 32 * NU * split;  // the wave's keys of the tile
+    if (kb > q0 + 31) return;  // all later than this wave's queries
+    f32x16 s[NU];
 #pragma unroll
-    for (int u = 0; u < 2; ++u) {
+    for (int u = 0; u < NU; ++u) {
 #pragma unroll
       for (int e = 0; e < 16; ++e) s[u][e] = 0.0f;
 #pragma unroll
-      for (int c = 0; c < DC; ++c) s[u] = M::mma(frag_row<M, DP>(lk, 32 * u, 2 * c), q[c], s[u]);
+      for (int c = 0; c < DC; ++c)
+        s[u] = M::mma(frag_row<M, DP>(lk, 32 * (NU * split + u), 2 * c), q[c], s[u]);
     }
-    if (k0 + kKeys - 1 > q0) {
+    if (kb + 32 * NU - 1 > q0) {
 #pragma unroll
-      for (int u = 0; u < 2; ++u)
+      for (int u = 0; u < NU; ++u)
 #pragma unroll
         for (int e = 0; e < 16; ++e)
-          if (k0 + 32 * u + acc_row(e) + 4 * half > qi) s[u][e] = -INFINITY;
+          if (kb + 32 * u + acc_row(e) + 4 * half > qi) s[u][e] = -INFINITY;
     }
     float top = s[0][0];
 #pragma unroll
-    for (int u = 0; u < 2; ++u)
+    for (int u = 0; u < NU; ++u)
 #pragma unroll
       for (int e = 0; e < 16; ++e) top = fmaxf(top, s[u][e]);
-    top = fmaxf(m, half_max(top));
-    const float f = exp2_fast((m - top) * c2);
-    m = top;
-    l *= f;
+    top = half_max(top);
+    if (__any(top > m + slack)) {  // rare: see kSlack
+      top = fmaxf(m, top);
+      const float f = exp2_fast((m - top) * c2);
+      m = top;
+      l *= f;
 #pragma unroll
-    for (int i = 0; i < DT; ++i)
+      for (int i = 0; i < DT; ++i)
 #pragma unroll
-      for (int e = 0; e < 16; ++e) acc[i][e] *= f;
+        for (int e = 0; e < 16; ++e) acc[i][e] *= f;
+    }
     const float mc = m * c2;
 #pragma unroll
-    for (int u = 0; u < 2; ++u)
+    for (int u = 0; u < NU; ++u)
 #pragma unroll
       for (int e = 0; e < 16; ++e) {
         s[u][e] = exp2_fast(fmaf(s[u][e], c2, -mc));
         l += s[u][e];
       }
 #pragma unroll
-    for (int u = 0; u < 2; ++u)
+    for (int u = 0; u < NU; ++u)
 #pragma unroll
       for (int c = 0; c < 2; ++c) {
         const typename M::V8 p = pack8<M>(s[u], c);
 #pragma unroll
-        for (int i = 0; i < DT; ++i) acc[i] = M::mma(frag_col<M, DP>(lv, 32 * u + 16 * c, 32 * i), p, acc[i]);
+        for (int i = 0; i < DT; ++i)
+          acc[i] = M::mma(frag_col<M, DP>(lv, 32 * (NU * split + u) + 16 * c, 32 * i), p, acc[i]);
       }
   };
   for (int j = 0; j < n_tiles; j += 2) {
     step(j, lk0, lv0, lk1, lv1);
     if (j + 1 < n_tiles) step(j + 1, lk1, lv1, lk0, lv0);
+  }
+  if constexpr (kSplits == 2) {
+    // the second split's sums join the first's, rescaled to the larger maximum
+    __syncthreads();
+    float* st = reinterpret_cast<float*>(lk1) + strip * 128 + lane;
+    char* part = strip ? lv0 : lk0;
+    if (split) {
+      give_columns<DT>(part, acc);
+      st[0] = m;
+      st[64] = l;
+    }
+    __syncthreads();
+    if (split) return;
+    const float m1 = st[0], top = fmaxf(m, m1);
+    const float f0 = exp2_fast((m - top) * c2), f1 = exp2_fast((m1 - top) * c2);
+    take_columns<DT>(part, acc, f0, f1);
+    l = l * f0 + st[64] * f1;
+    m = top;
   }
   l = half_sum(l);
   if (qi < t.len) {
@@ -390,19 +532,20 @@ __global__ void __launch_bounds__(256, 2) at_forward(const Attention a) {
 
 // ----------------------------------------------------------------------- dq --
 // Also writes delta_i = do_i.o_i for the dk/dv kernel.
-template <class M, int DP>
+template <class M, int DP, int kSplits>
 __global__ void __launch_bounds__(256, 2) at_dq(const Attention a) {
   typedef typename M::T T;
   constexpr int DT = DP / 32, DC = DP / 16;
+  constexpr int kStrips = 4 / kSplits, kRows = 32 * kStrips, NU = 2 / kSplits;
   constexpr int kTileBytes = kKeys * DP * 2;
   __shared__ __align__(16) char lk0[kTileBytes], lv0[kTileBytes], lk1[kTileBytes], lv1[kTileBytes];
-  const uint32_t id = xcd_logical(blockIdx.x, gridDim.x);
-  const uint32_t head = id / a.tiles;
-  if (head >= uint32_t(a.heads)) return;
+  uint32_t tile, head;
+  tile_and_head(blockIdx.x, uint32_t(a.heads), &tile, &head);
   Tile t;
-  if (!find_tile<kRows>(a, a.tiles - 1 - id % a.tiles, &t)) return;
+  if (!pick_tile<kRows, true>(a, tile, &t)) return;
   const int width = a.width;
   const int wave = __builtin_amdgcn_readfirstlane(int(threadIdx.x >> 6)), lane = threadIdx.x & 63, half = lane >> 5;
+  const int strip = wave % kStrips, split = kSplits == 1 ? 0 : wave / kStrips;
   if (t.sample == a.n) {
     zero_rows<M>(a.dq, a.dq_s, head, t.begin + t.m0, min(kRows, t.len - t.m0), width);
     return;
@@ -410,7 +553,7 @@ __global__ void __launch_bounds__(256, 2) at_dq(const Attention a) {
   const int64_t kv = head / (a.heads / a.kv_heads);
   const T* kb = static_cast<const T*>(a.k) + t.begin * a.k_s[0] + kv * a.k_s[1];
   const T* vb = static_cast<const T*>(a.v) + t.begin * a.v_s[0] + kv * a.v_s[1];
-  const int q0 = t.m0 + 32 * wave;
+  const int q0 = t.m0 + 32 * strip;
   const int qi = q0 + (lane & 31);
   const int64_t qr = t.begin + min(qi, t.len - 1);
   const T* qrow = static_cast<const T*>(a.q) + qr * a.q_s[0] + head * a.q_s[1];
@@ -429,7 +572,7 @@ __global__ void __launch_bounds__(256, 2) at_dq(const Attention a) {
   delta = half_sum(delta);
   const int64_t stat = int64_t(head) * a.T + qr;
   const float c2 = a.scale * kLog2e, lc = a.lse[stat] * kLog2e;
-  if (half == 0 && qi < t.len) a.delta[stat] = delta;
+  if (half == 0 && split == 0 && qi < t.len) a.delta[stat] = delta;
 
   f32x16 acc[DT];
 #pragma unroll
@@ -450,7 +593,7 @@ __global__ void __launch_bounds__(256, 2) at_dq(const Attention a) {
   ck.copy(kt, t.len, lk0);
   cv.copy(vt, t.len, lv0);
   auto step = [&](int j, const char* lk, const char* lv, char* next_k, char* next_v) {
-    copies_landed();
+    copies_landed<0>();
     const int k0 = j * kKeys;
     if (j + 1 < n_tiles) {
       kt += int64_t(ck.stride) * kKeys;
@@ -458,10 +601,10 @@ __global__ void __launch_bounds__(256, 2) at_dq(const Attention a) {
       ck.copy(kt, t.len - k0 - kKeys, next_k);
       cv.copy(vt, t.len - k0 - kKeys, next_v);
     }
-    if (k0 > q0 + 31) return;
-    const bool edge = k0 + kKeys - 1 > q0;
 #pragma unroll
-    for (int u = 0; u < 2; ++u) {
+    for (int x = 0; x < NU; ++x) {
+      const int u = NU * split + x, kb = k0 + 32 * u;
+      if (kb > q0) break;  // all later than this wave's queries
       f32x16 s, dp;
 #pragma unroll
       for (int e = 0; e < 16; ++e) s[e] = dp[e] = 0.0f;
@@ -472,10 +615,10 @@ __global__ void __launch_bounds__(256, 2) at_dq(const Attention a) {
       }
 #pragma unroll
       for (int e = 0; e < 16; ++e) s[e] = exp2_fast(fmaf(s[e], c2, -lc)) * (dp[e] - delta);
-      if (edge) {
-#pragma unroll
+      if (kb == q0) {  // the diagonal: both are multiples of 32
+  #pragma unroll
         for (int e = 0; e < 16; ++e)
-          if (k0 + 32 * u + acc_row(e) + 4 * half > qi) s[e] = 0.0f;
+          if (acc_row(e) + 4 * half > (lane & 31)) s[e] = 0.0f;
       }
 #pragma unroll
       for (int c = 0; c < 2; ++c) {
@@ -489,6 +632,14 @@ __global__ void __launch_bounds__(256, 2) at_dq(const Attention a) {
     step(j, lk0, lv0, lk1, lv1);
     if (j + 1 < n_tiles) step(j + 1, lk1, lv1, lk0, lv0);
   }
+  if constexpr (kSplits == 2) {
+    __syncthreads();
+    char* part = strip ? lv0 : lk0;
+    if (split) give_columns<DT>(part, acc);
+    __syncthreads();
+    if (split) return;
+    take_columns<DT>(part, acc, 1.0f, 1.0f);
+  }
   if (qi < t.len)
     store_columns<M, DT>(static_cast<T*>(a.dq) + qr * a.dq_s[0] + head * a.dq_s[1], acc, a.scale, width);
 }
@@ -497,27 +648,31 @@ __global__ void __launch_bounds__(256, 2) at_dq(const Attention a) {
 // One workgroup: 128 keys of one kv head, over the query heads of its group in
 // order and over the query tiles from the diagonal on. Nothing is added to
 // memory from two places, so the sums' order never changes.
-template <class M, int DP>
-__global__ void __launch_bounds__(256, 2) at_dkv(const Attention a) {
+template <class M, int DP, int kSplits, int kQs, int kStages, int kWaves>
+__global__ void __launch_bounds__(256, kWaves) at_dkv(const Attention a) {
   typedef typename M::T T;
   constexpr int DT = DP / 32, DC = DP / 16;
+  constexpr int kStrips = 4 / kSplits, kRows = 32 * kStrips;
   constexpr int kTileBytes = kQs * DP * 2;
+  // buffers, apart by name so that a read waits for its own buffer's copies only
   __shared__ __align__(16) char lq0[kTileBytes], ld0[kTileBytes], lq1[kTileBytes], ld1[kTileBytes];
-  __shared__ __align__(16) float ls0[2 * kQs], ls1[2 * kQs];  // a tile's lse and delta
-  const uint32_t id = xcd_logical(blockIdx.x, gridDim.x);
-  const uint32_t kv = id / a.tiles;
-  if (kv >= uint32_t(a.kv_heads)) return;
+  __shared__ __align__(16) char lq2[kStages > 2 ? kTileBytes : 1], ld2[kStages > 2 ? kTileBytes : 1];
+  __shared__ __align__(16) char lq3[kStages > 3 ? kTileBytes : 1], ld3[kStages > 3 ? kTileBytes : 1];
+  __shared__ __align__(16) float ls0[2 * kQs], ls1[2 * kQs], ls2[2 * kQs], ls3[2 * kQs];  // lse, delta
+  uint32_t tile, kv;
+  tile_and_head(blockIdx.x, uint32_t(a.kv_heads), &tile, &kv);
   Tile t;
-  if (!find_tile<kRows>(a, id % a.tiles, &t)) return;  // a sample's first keys are seen by most queries
+  if (!pick_tile<kRows, false>(a, tile, &t)) return;  // a sample's first keys are seen by most queries
   const int width = a.width;
   const int wave = __builtin_amdgcn_readfirstlane(int(threadIdx.x >> 6)), lane = threadIdx.x & 63, half = lane >> 5;
+  const int strip = wave % kStrips, split = kSplits == 1 ? 0 : wave / kStrips;
   if (t.sample == a.n) {
     const int rows = min(kRows, t.len - t.m0);
     zero_rows<M>(a.dk, a.dk_s, kv, t.begin + t.m0, rows, width);
     zero_rows<M>(a.dv, a.dv_s, kv, t.begin + t.m0, rows, width);
     return;
   }
-  const int k0 = t.m0 + 32 * wave;
+  const int k0 = t.m0 + 32 * strip;
   const int ki = k0 + (lane & 31);  // the lane's key
   const int64_t kr = t.begin + min(ki, t.len - 1);
   const T* krow = static_cast<const T*>(a.k) + kr * a.k_s[0] + kv * a.k_s[1];
@@ -543,41 +698,50 @@ __global__ void __launch_bounds__(256, 2) at_dkv(const Attention a) {
   // the tile copied next: query head and tile of the sample
   int64_t h_next = int64_t(kv) * group;
   int j_next = j0;
-  float stat = 0.0f;
-  auto copy = [&](char* lq, char* ld) {
+  // lse and delta go with the tile: a wave copies 64 of the 2 kQs values
+  constexpr int kStatWaves = 2 * kQs / 64;
+  auto copy = [&](char* lq, char* ld, float* ls) {
     const int row0 = j_next * kQs;
     cq.copy(reinterpret_cast<const char*>(static_cast<const T*>(a.q) + (t.begin + row0) * a.q_s[0] + h_next * a.q_s[1]),
             t.len - row0, lq);
     cd.copy(reinterpret_cast<const char*>(static_cast<const T*>(a.d_o) + (t.begin + row0) * a.do_s[0] + h_next * a.do_s[1]),
             t.len - row0, ld);
-    if (threadIdx.x < 2 * kQs) {
-      const int row = row0 + int(threadIdx.x % kQs);
-      const int64_t at = h_next * a.T + t.begin + min(row, t.len - 1);
-      // past the end: an infinite lse makes P and dS exactly 0
-      stat = threadIdx.x < kQs ? (row < t.len ? a.lse[at] * kLog2e : INFINITY) : a.delta[at];
-    }
+    const int part = wave % kStatWaves;  // waves beyond them copy the same again: all issue alike
+    const int at = part * 64 % kQs;
+    const float* from = (part * 64 < kQs ? a.lse : a.delta) + h_next * a.T + t.begin;
+    __builtin_amdgcn_global_load_lds(
+        (const __attribute__((address_space(1))) void*)(from + min(row0 + at + lane, t.len - 1)),
+        (__attribute__((address_space(3))) void*)(ls + part * 64), 4, 0, 0);
     if (++j_next == j1) {
       j_next = j0;
       ++h_next;
     }
   };
+  constexpr int kCopies = cq.kPer + cd.kPer + 1;  // of a tile, by each wave
   if (width < DP) {
     cq.zero_pad(lq0);
     cq.zero_pad(lq1);
     cd.zero_pad(ld0);
     cd.zero_pad(ld1);
+    if (kStages > 2) cq.zero_pad(lq2), cd.zero_pad(ld2);
+    if (kStages > 3) cq.zero_pad(lq3), cd.zero_pad(ld3);
   }
-  copy(lq0, ld0);
-  int q0 = t.m0;
-  auto step = [&](int i, const char* lq, const char* ld, float* ls, char* next_q, char* next_d) {
-    if (threadIdx.x < 2 * kQs) ls[threadIdx.x] = stat;
-    copies_landed();
-    if (i + 1 < n_tiles) copy(next_q, next_d);
+  copy(lq0, ld0, ls0);
+  if (kStages > 2 && n_tiles > 1) copy(lq1, ld1, ls1);
+  if (kStages > 3 && n_tiles > 2) copy(lq2, ld2, ls2);
+  int q0 = j0 * kQs;
+  auto step = [&](int i, const char* lq, const char* ld, const float* ls, char* next_q, char* next_d, float* next_s) {
+    // tile i is in LDS, and tile i - 1 is done with
+    const int behind = min(n_tiles - 1 - i, kStages - 2);
+    if (behind == 2) copies_landed<2 * kCopies>();
+    else if (behind == 1) copies_landed<kCopies>();
+    else copies_landed<0>();
+    if (i + kStages - 1 < n_tiles) copy(next_q, next_d, next_s);
     const int row0 = q0;
-    q0 = q0 + kQs < t.len ? q0 + kQs : t.m0;
-    if (row0 + kQs - 1 < k0) return;  // all earlier than this wave's keys
+    q0 = q0 + kQs < t.len ? q0 + kQs : j0 * kQs;
 #pragma unroll 1
-    for (int u = 0; u < kQs / 32; ++u) {
+    for (int u = split; u < kQs / 32; u += kSplits) {
+      if (row0 + 32 * u < k0) continue;  // all earlier than this wave's keys
       f32x16 s, dp;
 #pragma unroll
       for (int e = 0; e < 16; ++e) s[e] = dp[e] = 0.0f;
@@ -593,14 +757,19 @@ __global__ void __launch_bounds__(256, 2) at_dkv(const Attention a) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           const int r = 4 * b + e;
-          s[r] = exp2_fast(fmaf(s[r], c2, -lc[e]));
+          s[r] = exp2_fast(fmaf(s[r], c2, -lc[e] * kLog2e));
           dp[r] = s[r] * (dp[r] - de[e]);
         }
       }
-      if (row0 < k0 + 31) {
+      if (row0 + 32 * u == k0) {  // the diagonal: both are multiples of 32
+  #pragma unroll
+        for (int r = 0; r < 16; ++r)
+          if (acc_row(r) + 4 * half < (lane & 31)) s[r] = dp[r] = 0.0f;
+      }
+      if (row0 + 32 * u + 32 > t.len) {  // rows past the end
 #pragma unroll
         for (int r = 0; r < 16; ++r)
-          if (row0 + 32 * u + acc_row(r) + 4 * half < ki) s[r] = dp[r] = 0.0f;
+          if (row0 + 32 * u + acc_row(r) + 4 * half >= t.len) s[r] = dp[r] = 0.0f;
       }
 #pragma unroll
       for (int c = 0; c < 2; ++c) {
@@ -614,9 +783,33 @@ __global__ void __launch_bounds__(256, 2) at_dkv(const Attention a) {
       }
     }
   };
-  for (int i = 0; i < n_tiles; i += 2) {
-    step(i, lq0, ld0, ls0, lq1, ld1);
-    if (i + 1 < n_tiles) step(i + 1, lq1, ld1, ls1, lq0, ld0);
+  for (int i = 0; i < n_tiles; i += kStages) {
+    if constexpr (kStages == 2) {
+      step(i, lq0, ld0, ls0, lq1, ld1, ls1);
+      if (i + 1 < n_tiles) step(i + 1, lq1, ld1, ls1, lq0, ld0, ls0);
+    } else if constexpr (kStages == 3) {
+      step(i, lq0, ld0, ls0, lq2, ld2, ls2);
+      if (i + 1 < n_tiles) step(i + 1, lq1, ld1, ls1, lq0, ld0, ls0);
+      if (i + 2 < n_tiles) step(i + 2, lq2, ld2, ls2, lq1, ld1, ls1);
+    } else {
+      step(i, lq0, ld0, ls0, lq3, ld3, ls3);
+      if (i + 1 < n_tiles) step(i + 1, lq1, ld1, ls1, lq0, ld0, ls0);
+      if (i + 2 < n_tiles) step(i + 2, lq2, ld2, ls2, lq1, ld1, ls1);
+      if (i + 3 < n_tiles) step(i + 3, lq3, ld3, ls3, lq2, ld2, ls2);
+    }
+  }
+  if constexpr (kSplits == 2) {
+    __syncthreads();
+    char* pk = strip ? lq1 : lq0;
+    char* pv = strip ? ld1 : ld0;
+    if (split) {
+      give_columns<DT>(pk, dk);
+      give_columns<DT>(pv, dv);
+    }
+    __syncthreads();
+    if (split) return;
+    take_columns<DT>(pk, dk, 1.0f, 1.0f);
+    take_columns<DT>(pv, dv, 1.0f, 1.0f);
   }
   if (ki < t.len) {
     store_columns<M, DT>(static_cast<T*>(a.dk) + kr * a.dk_s[0] + kv * a.dk_s[1], dk, a.scale, width);
@@ -638,6 +831,16 @@ int check_array(const char* name, const void* p, const int64_t* s, int64_t heads
   return NOPFS_OK;
 }
 
+// Row tiles of `rows` rows at most, and the grid over them and the heads.
+int tile_grid(Attention* a, int rows, int32_t heads, dim3* grid) {
+  const int64_t tiles = a->T / rows + a->n + 1;
+  if (tiles * heads > (int64_t(1) << 31) - 16)
+    return fail(NOPFS_ERANGE, "too many rows, samples and heads for one call");
+  a->tiles = uint32_t(tiles);
+  *grid = dim3(uint32_t(tiles * heads));
+  return NOPFS_OK;
+}
+
 int make_attention(const nopfs_attention* p, Attention* a) {
   if (!p) return fail(NOPFS_EINVAL, "attention is NULL");
   if (p->T < 0 || p->n < 0) return fail(NOPFS_EINVAL, "T and n must be >= 0");
@@ -649,7 +852,7 @@ int make_attention(const nopfs_attention* p, Attention* a) {
   if (p->width > 128) return fail(NOPFS_ERANGE, "width must be <= 128");
   if (!(p->scale > 0.0f) || !isfinite(p->scale))
     return fail(NOPFS_EINVAL, "scale must be positive and finite");
-  if (p->T >= (int64_t(1) << 31) - kRows || p->n > (1 << 30))
+  if (p->T >= (int64_t(1) << 31) - 128 || p->n > (1 << 30))
     return fail(NOPFS_ERANGE, "T must be < 2^31 - 128, n <= 2^30");
   a->T = p->T;
   a->n = p->n;
@@ -667,11 +870,36 @@ int make_attention(const nopfs_attention* p, Attention* a) {
     a->dk_s[i] = p->dk_stride[i];
     a->dv_s[i] = p->dv_stride[i];
   }
-  const int64_t tiles = p->T / kRows + p->n + 1;
-  if (tiles * p->heads > (int64_t(1) << 31) - 16)
-    return fail(NOPFS_ERANGE, "too many rows, samples and heads for one call");
-  a->tiles = uint32_t(tiles);
   return NOPFS_OK;
+}
+
+// Two splits where one leaves compute units without a second workgroup to
+// overlap with: 5,003 tokens x 6 heads forward 26.2 -> 20.6 us with two, 16,384
+// x 16 heads 99 -> 131.
+constexpr int64_t kSlots = 512;
+bool two_splits(const Attention& a, int32_t heads) { return (a.T / 128 + 1) * heads < kSlots; }
+
+// An order by cost is worth its launch (4 us) where samples of several tiles
+// differ: 32 documents of 16,384 tokens, forward 127 -> 99 us. A single sample
+// is in order by itself, and samples below a tile all cost the same.
+bool needs_order(const Attention& a) { return a.n > 1 && a.T >= 4096 && a.T / a.n >= 64; }
+
+template <class M, int DP>
+int launch_forward(Attention a, hipStream_t st) {
+  const bool two = two_splits(a, a.heads);
+  const int32_t rows = two ? 64 : 128;
+  dim3 grid;
+  int rc = tile_grid(&a, rows, a.heads, &grid);
+  if (rc) return rc;
+  Scratch sc(st);
+  if (needs_order(a)) {
+    OrderJob j{nullptr, a.tiles, rows, true};
+    if ((rc = sc.alloc_n(&j.order, a.tiles))) return rc;
+    if ((rc = launch("at_order", at_order, dim3(1), dim3(1024), 0, st, a, j, j))) return rc;
+    a.order = j.order;
+  }
+  return two ? launch("at_forward", at_forward<M, DP, 2>, grid, dim3(256), 0, st, a)
+             : launch("at_forward", at_forward<M, DP, 1>, grid, dim3(256), 0, st, a);
 }
 
 int attention_impl(const nopfs_attention* p, const void* q, const void* k, const void* v,
@@ -691,20 +919,39 @@ int attention_impl(const nopfs_attention* p, const void* q, const void* k, const
   a.o = o;
   a.lse = lse;
   a.start = start;
-  const dim3 grid(xcd_padded(a.tiles * uint32_t(a.heads)));
-  const bool bf = p->dtype == NOPFS_BF16;
   if (a.width <= 64)
-    return bf ? launch("at_forward", at_forward<MBf16, 64>, grid, dim3(256), 0, st, a)
-              : launch("at_forward", at_forward<MFp16, 64>, grid, dim3(256), 0, st, a);
-  return bf ? launch("at_forward", at_forward<MBf16, 128>, grid, dim3(256), 0, st, a)
-            : launch("at_forward", at_forward<MFp16, 128>, grid, dim3(256), 0, st, a);
+    return p->dtype == NOPFS_BF16 ? launch_forward<MBf16, 64>(a, st) : launch_forward<MFp16, 64>(a, st);
+  return p->dtype == NOPFS_BF16 ? launch_forward<MBf16, 128>(a, st) : launch_forward<MFp16, 128>(a, st);
 }
 
 template <class M, int DP>
-int launch_grad(const Attention& a, hipStream_t st) {
-  int rc = launch("at_dq", at_dq<M, DP>, dim3(xcd_padded(a.tiles * uint32_t(a.heads))), dim3(256), 0, st, a);
+int launch_grad(Attention a, hipStream_t st) {
+  // dk, dv: 128 elements a head leave one wave per SIMD its registers, and two
+  // splits then halve the longest workgroup
+  const bool two_q = two_splits(a, a.heads), two_k = DP == 128 || two_splits(a, a.kv_heads);
+  Attention ak = a;
+  dim3 gq, gk;
+  int rc = tile_grid(&a, two_q ? 64 : 128, a.heads, &gq);
   if (rc) return rc;
-  return launch("at_dkv", at_dkv<M, DP>, dim3(xcd_padded(a.tiles * uint32_t(a.kv_heads))), dim3(256), 0, st, a);
+  if ((rc = tile_grid(&ak, two_k ? 64 : 128, a.kv_heads, &gk))) return rc;
+  Scratch sc(st);
+  if (needs_order(a)) {
+    OrderJob jq{nullptr, a.tiles, two_q ? 64 : 128, true}, jk{nullptr, ak.tiles, two_k ? 64 : 128, false};
+    if ((rc = sc.alloc_n(&jq.order, a.tiles))) return rc;
+    if ((rc = sc.alloc_n(&jk.order, ak.tiles))) return rc;
+    if ((rc = launch("at_order", at_order, dim3(2), dim3(1024), 0, st, a, jq, jk))) return rc;
+    a.order = jq.order;
+    ak.order = jk.order;
+  }
+  rc = two_q ? launch("at_dq", at_dq<M, DP, 2>, gq, dim3(256), 0, st, a)
+             : launch("at_dq", at_dq<M, DP, 1>, gq, dim3(256), 0, st, a);
+  if (rc) return rc;
+  if constexpr (DP == 128) {
+    return launch("at_dkv", at_dkv<M, DP, 2, 64, 3, 1>, gk, dim3(256), 0, st, ak);
+  } else {
+    return two_k ? launch("at_dkv", at_dkv<M, DP, 2, 64, 2, 2>, gk, dim3(256), 0, st, ak)
+                 : launch("at_dkv", at_dkv<M, DP, 1, 64, 3, 2>, gk, dim3(256), 0, st, ak);
+  }
 }
 
 int attention_grad_impl(const nopfs_attention* p, const void* d_o, const void* q, const void* k,

@@ -2,6 +2,7 @@
 #pragma once
 
 #include <limits.h>
+#include <type_traits>
 #include <math.h>
 
 #include "common.hpp"

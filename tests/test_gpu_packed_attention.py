@@ -101,6 +101,26 @@ def test_many_short_samples(n):
     _run_and_check(q, k, v, do, _starts(lengths))
 
 
+@pytest.mark.parametrize("width", [64, 128])
+@pytest.mark.parametrize("kv_heads", [200, 520])
+def test_many_heads(width, kv_heads):
+    """Enough workgroups for one split: 128 columns each."""
+    lengths = [3, 129, 0, 100]
+    q, k, v, do = _inputs(lengths, 7, 520, 520, width, BF, 11)
+    if kv_heads < 520:
+        q, do, k, v = q[:, :400], do[:, :400], k[:, :200], v[:, :200]
+    _run_and_check(q, k, v, do, _starts(lengths))
+
+
+@pytest.mark.parametrize("heads,kv_heads", [(1, 1), (18, 6)])
+@pytest.mark.parametrize("width", [64, 128])
+def test_order_by_cost(heads, kv_heads, width):
+    """Enough rows and samples for the tiles to be ordered."""
+    lengths = [700, 1, 0, 64, 1_500, 130, 128, 900, 0, 33, 620, 200]
+    q, k, v, do = _inputs(lengths, 90, heads, kv_heads, width, BF, 12)
+    _run_and_check(q, k, v, do, _starts(lengths))
+
+
 def test_no_sample_and_no_row():
     q, k, v, do = _inputs([], 150, 2, 1, 64, BF, 1)
     for start in ([0], [0, 0, 0]):
