@@ -434,29 +434,29 @@ _DTYPES = {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2}  # NOPFS_BF16,
 
 def _step_tensor(t, name, dtypes, ndim, device):
     """A device tensor of one of these types and this many dimensions, adjacent
-    along the last one, on the given device (None: the current one)."""
+    along the last one, on the current device."""
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise TypeError(f"{name} must be a device tensor")
     if t.dtype not in dtypes:
         raise ValueError(f"{name} must be of type " + " or ".join(str(d) for d in dtypes))
-    if t.dim() != ndim or (t.shape[-1] > 1 and t.stride(-1) != 1):
+    if t.dim() != ndim or (t.stride(-1) != 1 and t.shape[-1] > 1):
         raise ValueError(f"{name} must have {ndim} dimensions, the last one adjacent in memory")
-    if t.device.index != device:
+    if t.get_device() != device:
         raise ValueError(f"{name} must be on device {device}, where the call runs")
     return t
 
 
 def _step_shape(t, name, shape):
-    if tuple(t.shape) != shape:
-        raise ValueError(f"{name} must have shape {shape}, not {tuple(t.shape)}")
+    if t.shape != shape:
+        raise ValueError(f"{name} must have shape {tuple(shape)}, not {tuple(t.shape)}")
 
 
-def _step_stream(stream, tensors):
+def _step_stream(stream, device, tensors):
     """The stream's handle. Where it is not the current one, the allocator is
     told that the call's tensors are in use there."""
-    current = torch.cuda.current_stream()
-    if stream is None or stream.cuda_stream == current.cuda_stream:
-        return current.cuda_stream
+    current = torch.cuda.current_stream(device).cuda_stream
+    if stream is None or stream.cuda_stream == current:
+        return current
     for t in tensors:
         if t is not None:
             t.record_stream(stream)
@@ -506,12 +506,12 @@ def batch_tables(ids, tokens, free, block: int, width: int, cap: int, out=None, 
                             ("pos", (G, cap), torch.int32), ("used", (G, 3), torch.int32)):
         t = o.get(name)
         if t is None:
-            o[name] = torch.empty(shape, dtype=dt, device=lead.device)
+            o[name] = lead.new_empty(shape, dtype=dt)
         else:
             _dense(_step_tensor(t, name, (dt,), len(shape), dev), name)
             _step_shape(t, name, shape)
     b = _Batch(F, _row_stride(lead), _row_stride(free), G, n, free.shape[1], block, width, cap)
-    st = _step_stream(stream, (ids, tokens, free, *o.values()))
+    st = _step_stream(stream, dev, (ids, tokens, free, *o.values()))
     _check(lib().nopfs_batch_tables(
         ctypes.byref(b), None if ids is None else ids.data_ptr(), tokens.data_ptr(),
         free.data_ptr(), o["start"].data_ptr(), o["table"].data_ptr(), o["slot"].data_ptr(),
@@ -533,16 +533,18 @@ def _attention(q, k, v, start, scale, dev):
         raise ValueError("start must have an entry before every sample and one behind the last")
     if scale is None:
         scale = width ** -0.5 if width else 0.0
-    return _Attention(T, start.shape[0] - 1, heads, kv_heads, width, _DTYPES[q.dtype], scale)
+    return T, start.shape[0] - 1, heads, kv_heads, width, _DTYPES[q.dtype], scale
 
 
-def _set_strides(a, **tensors):
-    """Token and head strides. That of a single token or head says nothing:
-    what the array would have when dense."""
-    for name, t in tensors.items():
+def _strides(*tensors):
+    """Token and head strides of each. That of a single token or head says
+    nothing: what the array would have when dense."""
+    out = []
+    for t in tensors:
         T, heads, width = t.shape
-        setattr(a, name + "_head", t.stride(1) if heads > 1 else width)
-        setattr(a, name + "_token", t.stride(0) if T > 1 else heads * width)
+        token, head, _ = t.stride()
+        out += (token if T > 1 else heads * width, head if heads > 1 else width)
+    return out
 
 
 def packed_attention(q, k, v, start, scale=None, o=None, lse=None, stream=None):
@@ -554,16 +556,16 @@ def packed_attention(q, k, v, start, scale=None, o=None, lse=None, stream=None):
     dev = torch.cuda.current_device()
     a = _attention(q, k, v, start, scale, dev)
     if o is None:
-        o = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        o = q.new_empty(q.shape)
     else:
-        _step_shape(_step_tensor(o, "o", (q.dtype,), 3, dev), "o", tuple(q.shape))
+        _step_shape(_step_tensor(o, "o", (q.dtype,), 3, dev), "o", q.shape)
     if lse is None:
-        lse = torch.empty((a.heads, a.T), dtype=torch.float32, device=q.device)
+        lse = q.new_empty((a[2], a[0]), dtype=torch.float32)
     else:
         _step_shape(_dense(_step_tensor(lse, "lse", (torch.float32,), 2, dev), "lse"), "lse",
-                    (a.heads, a.T))
-    _set_strides(a, q=q, k=k, v=v, o=o)
-    st = _step_stream(stream, (q, k, v, start, o, lse))
+                    (a[2], a[0]))
+    a = _Attention(*a, *_strides(q, k, v, o))
+    st = _step_stream(stream, dev, (q, k, v, start, o, lse))
     _check(lib().nopfs_packed_attention(ctypes.byref(a), q.data_ptr(), k.data_ptr(), v.data_ptr(),
                                         start.data_ptr(), o.data_ptr(), lse.data_ptr(), st),
            "nopfs_packed_attention")
@@ -579,19 +581,19 @@ def packed_attention_grad(do, q, k, v, o, lse, start, scale=None, dq=None, dk=No
     a = _attention(q, k, v, start, scale, dev)
     same = (q.dtype,)
     for name, t in (("do", do), ("o", o)):
-        _step_shape(_step_tensor(t, name, same, 3, dev), name, tuple(q.shape))
+        _step_shape(_step_tensor(t, name, same, 3, dev), name, q.shape)
     _step_shape(_dense(_step_tensor(lse, "lse", (torch.float32,), 2, dev), "lse"), "lse",
-                (a.heads, a.T))
+                (a[2], a[0]))
     grads = []
     for name, t, like in (("dq", dq, q), ("dk", dk, k), ("dv", dv, v)):
         if t is None:
-            t = torch.empty(like.shape, dtype=q.dtype, device=q.device)
+            t = q.new_empty(like.shape)
         else:
-            _step_shape(_step_tensor(t, name, same, 3, dev), name, tuple(like.shape))
+            _step_shape(_step_tensor(t, name, same, 3, dev), name, like.shape)
         grads.append(t)
     dq, dk, dv = grads
-    _set_strides(a, q=q, k=k, v=v, o=o, do=do, dq=dq, dk=dk, dv=dv)
-    st = _step_stream(stream, (do, q, k, v, o, lse, start, dq, dk, dv))
+    a = _Attention(*a, *_strides(q, k, v, o, do, dq, dk, dv))
+    st = _step_stream(stream, dev, (do, q, k, v, o, lse, start, dq, dk, dv))
     _check(lib().nopfs_packed_attention_grad(
         ctypes.byref(a), do.data_ptr(), q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(),
         lse.data_ptr(), start.data_ptr(), dq.data_ptr(), dk.data_ptr(), dv.data_ptr(), st),
@@ -615,20 +617,20 @@ def topk_distill(logits, index, teacher, tau=1.0, weight=None, grad=True, loss=N
         _step_shape(_dense(_step_tensor(weight, "weight", (torch.float32,), 1, dev), "weight"),
                     "weight", (T,))
     if loss is None:
-        loss = torch.empty(T, dtype=torch.float32, device=logits.device)
+        loss = logits.new_empty(T, dtype=torch.float32)
     else:
         _step_shape(_dense(_step_tensor(loss, "loss", (torch.float32,), 1, dev), "loss"), "loss",
                     (T,))
     if not grad:
         dlogits = None
     elif dlogits is None:
-        dlogits = torch.empty((T, V), dtype=logits.dtype, device=logits.device)
+        dlogits = logits.new_empty((T, V))
     else:
         _step_shape(_step_tensor(dlogits, "dlogits", (logits.dtype,), 2, dev), "dlogits", (T, V))
     d = _Distill(T, V, _row_stride(logits), 0 if dlogits is None else _row_stride(dlogits),
                  _row_stride(index), _row_stride(teacher), K, _DTYPES[logits.dtype],
                  _DTYPES[teacher.dtype], tau)
-    st = _step_stream(stream, (logits, index, teacher, weight, loss, dlogits))
+    st = _step_stream(stream, dev, (logits, index, teacher, weight, loss, dlogits))
     _check(lib().nopfs_topk_distill(
         ctypes.byref(d), logits.data_ptr(), index.data_ptr(), teacher.data_ptr(),
         None if weight is None else weight.data_ptr(), loss.data_ptr(),
