@@ -65,6 +65,11 @@ struct Attention {
   void *o, *dq, *dk, *dv;  // o: output of the forward call, input of the gradient
   float* lse;
   float* delta;  // [heads][T] (scratch)
+  // dk, dv: parts of a group's query heads that workgroups of their own sum;
+  // with more than one, their sums [part][dk, dv][T][kv_heads][width] in 32
+  // bits (scratch), added in order afterwards
+  int32_t parts;
+  float* partial;
   const int32_t* start;
   uint32_t tiles;  // an upper bound of the row tiles
   const int2* order;  // the tiles' (sample, first row), costliest first, or NULL
@@ -258,13 +263,16 @@ struct TileCopy {
   }
 };
 
-// This wave's copies into LDS have landed, all but the last kBehind; with the
-// barrier, every wave's.
+// Every wave is here and has what it read from or wrote to LDS behind it, and
+// its copies into LDS have landed, all but the last kBehind. (A __syncthreads
+// would wait for all of them: the next tile's too.)
 template <int kBehind>
-__device__ __forceinline__ void copies_landed() {
+__device__ __forceinline__ void meet() {
   static_assert(kBehind < 64, "vmcnt has 6 bits");
-  __builtin_amdgcn_s_waitcnt(0x0f70 | (kBehind & 15) | (kBehind >> 4) << 14);  // vmcnt(kBehind)
-  __syncthreads();
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt(0x0070 | (kBehind & 15) | (kBehind >> 4) << 14);  // vmcnt(kBehind) lgkmcnt(0)
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
 }
 
 // A operand (32 rows x 16 elements): row `row0 + lane % 32` of an LDS tile.
@@ -342,6 +350,36 @@ __device__ __forceinline__ void store_columns(typename M::T* row, const f32x16* 
       for (int e = 0; e < 4; ++e) v[e] = typename M::T(acc[t][4 * i + e] * f);
       *reinterpret_cast<typename M::V4*>(row + d) = v;
     }
+}
+template <int DT>
+__device__ __forceinline__ void store_sums(float* row, const f32x16* acc, int width) {
+  const int half = (threadIdx.x & 63) >> 5;
+#pragma unroll
+  for (int t = 0; t < DT; ++t)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int d = 32 * t + 8 * i + 4 * half;
+      if (d < width)
+        *reinterpret_cast<f32x4*>(row + d) =
+            f32x4{acc[t][4 * i], acc[t][4 * i + 1], acc[t][4 * i + 2], acc[t][4 * i + 3]};
+    }
+}
+
+// dk and dv of the lane's key (row kr of all), elements d0 on: rounded where a
+// workgroup has the whole group's sums, else its part of them.
+template <class M, int DT>
+__device__ __forceinline__ void store_dkv(const Attention& a, int64_t kr, int64_t kv, int part, int d0,
+                                          const f32x16* dk, const f32x16* dv) {
+  typedef typename M::T T;
+  if (a.parts == 1) {
+    store_columns<M, DT>(static_cast<T*>(a.dk) + kr * a.dk_s[0] + kv * a.dk_s[1] + d0, dk, a.scale, a.width - d0);
+    store_columns<M, DT>(static_cast<T*>(a.dv) + kr * a.dv_s[0] + kv * a.dv_s[1] + d0, dv, 1.0f, a.width - d0);
+    return;
+  }
+  const int64_t size = a.T * a.kv_heads * a.width;
+  float* row = a.partial + 2 * part * size + (kr * a.kv_heads + kv) * a.width + d0;
+  store_sums<DT>(row, dk, a.width - d0);
+  store_sums<DT>(row + size, dv, a.width - d0);
 }
 
 // A wave's accumulators through LDS to the wave that owns the same columns,
@@ -441,7 +479,7 @@ __global__ void __launch_bounds__(256, 2) at_forward(const Attention a) {
   ck.copy(kt, t.len, lk0);
   cv.copy(vt, t.len, lv0);
   auto step = [&](int j, const char* lk, const char* lv, char* next_k, char* next_v) {
-    copies_landed<0>();  // tile j is in LDS, and tile j - 1 is done with
+    meet<0>();  // tile j is in LDS, and tile j - 1 is done with
     const int k0 = j * kKeys;
     if (j + 1 < n_tiles) {
       kt += int64_t(ck.stride) * kKeys;
@@ -593,7 +631,7 @@ __global__ void __launch_bounds__(256, 2) at_dq(const Attention a) {
   ck.copy(kt, t.len, lk0);
   cv.copy(vt, t.len, lv0);
   auto step = [&](int j, const char* lk, const char* lv, char* next_k, char* next_v) {
-    copies_landed<0>();
+    meet<0>();
     const int k0 = j * kKeys;
     if (j + 1 < n_tiles) {
       kt += int64_t(ck.stride) * kKeys;
@@ -660,13 +698,16 @@ __global__ void __launch_bounds__(256, kWaves) at_dkv(const Attention a) {
   __shared__ __align__(16) char lq3[kStages > 3 ? kTileBytes : 1], ld3[kStages > 3 ? kTileBytes : 1];
   __shared__ __align__(16) float ls0[2 * kQs], ls1[2 * kQs], ls2[2 * kQs], ls3[2 * kQs];  // lse, delta
   uint32_t tile, kv;
-  tile_and_head(blockIdx.x, uint32_t(a.kv_heads), &tile, &kv);
+  tile_and_head(blockIdx.x, uint32_t(a.kv_heads * a.parts), &tile, &kv);
+  const int head_part = int(kv) % a.parts;  // neighbours: the parts of a kv head
+  kv /= uint32_t(a.parts);
   Tile t;
   if (!pick_tile<kRows, false>(a, tile, &t)) return;  // a sample's first keys are seen by most queries
   const int width = a.width;
   const int wave = __builtin_amdgcn_readfirstlane(int(threadIdx.x >> 6)), lane = threadIdx.x & 63, half = lane >> 5;
   const int strip = wave % kStrips, split = kSplits == 1 ? 0 : wave / kStrips;
   if (t.sample == a.n) {
+    if (a.parts > 1) return;  // the sum of the parts has these rows
     const int rows = min(kRows, t.len - t.m0);
     zero_rows<M>(a.dk, a.dk_s, kv, t.begin + t.m0, rows, width);
     zero_rows<M>(a.dv, a.dv_s, kv, t.begin + t.m0, rows, width);
@@ -690,13 +731,13 @@ __global__ void __launch_bounds__(256, kWaves) at_dkv(const Attention a) {
     for (int e = 0; e < 16; ++e) dk[i][e] = dv[i][e] = 0.0f;
   const float c2 = a.scale * kLog2e;
 
-  const int group = a.heads / a.kv_heads;
+  const int group = a.heads / a.kv_heads / a.parts;  // query heads of this part
   const int j0 = t.m0 / kQs;  // the first query tile that sees the tile's keys
   const int j1 = (t.len + kQs - 1) / kQs;
   const int n_tiles = (j1 - j0) * group;
   const TileCopy<DP, kQs> cq(a.q_s[0], width), cd(a.do_s[0], width);
   // the tile copied next: query head and tile of the sample
-  int64_t h_next = int64_t(kv) * group;
+  int64_t h_next = (int64_t(kv) * a.parts + head_part) * group;
   int j_next = j0;
   // lse and delta go with the tile: a wave copies 64 of the 2 kQs values
   constexpr int kStatWaves = 2 * kQs / 64;
@@ -733,9 +774,9 @@ __global__ void __launch_bounds__(256, kWaves) at_dkv(const Attention a) {
   auto step = [&](int i, const char* lq, const char* ld, const float* ls, char* next_q, char* next_d, float* next_s) {
     // tile i is in LDS, and tile i - 1 is done with
     const int behind = min(n_tiles - 1 - i, kStages - 2);
-    if (behind == 2) copies_landed<2 * kCopies>();
-    else if (behind == 1) copies_landed<kCopies>();
-    else copies_landed<0>();
+    if (behind == 2) meet<2 * kCopies>();
+    else if (behind == 1) meet<kCopies>();
+    else meet<0>();
     if (i + kStages - 1 < n_tiles) copy(next_q, next_d, next_s);
     const int row0 = q0;
     q0 = q0 + kQs < t.len ? q0 + kQs : j0 * kQs;
@@ -811,10 +852,185 @@ __global__ void __launch_bounds__(256, kWaves) at_dkv(const Attention a) {
     take_columns<DT>(pk, dk, 1.0f, 1.0f);
     take_columns<DT>(pv, dv, 1.0f, 1.0f);
   }
-  if (ki < t.len) {
-    store_columns<M, DT>(static_cast<T*>(a.dk) + kr * a.dk_s[0] + kv * a.dk_s[1], dk, a.scale, width);
-    store_columns<M, DT>(static_cast<T*>(a.dv) + kr * a.dv_s[0] + kv * a.dv_s[1], dv, 1.0f, width);
+  if (ki < t.len) store_dkv<M, DT>(a, kr, kv, head_part, 0, dk, dv);
+}
+
+// The same for heads of more than 64 elements, where a wave's own rows and
+// sums of 32 keys (K, V: 64 registers, dk, dv: 128) leave no room for a second
+// wave on the SIMD. One workgroup: 64 keys, in two strips of 32; two waves
+// share a strip. In a tile of 64 queries each makes P and dS of 32 of them,
+// hands them to the other through LDS (as the operands they are, 16 bytes a
+// lane), and then sums one half of the head's elements over all 64: half the
+// sums per wave, and two workgroups share a compute unit. Their LDS is exactly
+// half of it, so lse and delta stay in registers, one row per lane.
+template <class M>
+__global__ void __launch_bounds__(256, 2) at_dkv_wide(const Attention a) {
+  typedef typename M::T T;
+  typedef typename M::V8 V8;
+  constexpr int DP = 128, DC = DP / 16, kRows = 64, kQs = 64;
+  constexpr int kTileBytes = kQs * DP * 2;
+  __shared__ __align__(16) char lq0[kTileBytes], ld0[kTileBytes], lq1[kTileBytes], ld1[kTileBytes];
+  __shared__ __align__(16) char lx[4 * 4096];  // P and dS: 4 operands of every wave
+  uint32_t tile, kv;
+  tile_and_head(blockIdx.x, uint32_t(a.kv_heads * a.parts), &tile, &kv);
+  const int head_part = int(kv) % a.parts;  // neighbours: the parts of a kv head
+  kv /= uint32_t(a.parts);
+  Tile t;
+  if (!pick_tile<kRows, false>(a, tile, &t)) return;
+  const int width = a.width;
+  const int wave = __builtin_amdgcn_readfirstlane(int(threadIdx.x >> 6)), lane = threadIdx.x & 63, half = lane >> 5;
+  const int strip = wave & 1, part = wave >> 1;
+  if (t.sample == a.n) {
+    if (a.parts > 1) return;  // the sum of the parts has these rows
+    const int rows = min(kRows, t.len - t.m0);
+    zero_rows<M>(a.dk, a.dk_s, kv, t.begin + t.m0, rows, width);
+    zero_rows<M>(a.dv, a.dv_s, kv, t.begin + t.m0, rows, width);
+    return;
   }
+  const int k0 = t.m0 + 32 * strip;
+  const int ki = k0 + (lane & 31);  // the lane's key
+  const int64_t kr = t.begin + min(ki, t.len - 1);
+  const T* krow = static_cast<const T*>(a.k) + kr * a.k_s[0] + kv * a.k_s[1];
+  const T* vrow = static_cast<const T*>(a.v) + kr * a.v_s[0] + kv * a.v_s[1];
+  V8 k[DC], v[DC];
+#pragma unroll
+  for (int c = 0; c < DC; ++c) {
+    k[c] = own_chunk<M>(krow, c, width);
+    v[c] = own_chunk<M>(vrow, c, width);
+  }
+  f32x16 dk[2], dv[2];  // elements 64 part .. 64 part + 63
+#pragma unroll
+  for (int i = 0; i < 2; ++i)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) dk[i][e] = dv[i][e] = 0.0f;
+  const float c2 = a.scale * kLog2e;
+
+  const int group = a.heads / a.kv_heads / a.parts;
+  const int j0 = t.m0 / kQs;
+  const int j1 = (t.len + kQs - 1) / kQs;
+  const int n_tiles = (j1 - j0) * group;
+  const TileCopy<DP, kQs> cq(a.q_s[0], width), cd(a.do_s[0], width);
+  int64_t h_next = (int64_t(kv) * a.parts + head_part) * group;
+  int j_next = j0;
+  auto copy = [&](char* lq, char* ld, f32x2& stat) {
+    const int row0 = j_next * kQs;
+    const int64_t at = h_next * a.T + t.begin + min(row0 + lane, t.len - 1);
+    stat = f32x2{a.lse[at], a.delta[at]};  // of row `lane` of the tile
+    cq.copy(reinterpret_cast<const char*>(static_cast<const T*>(a.q) + (t.begin + row0) * a.q_s[0] + h_next * a.q_s[1]),
+            t.len - row0, lq);
+    cd.copy(reinterpret_cast<const char*>(static_cast<const T*>(a.d_o) + (t.begin + row0) * a.do_s[0] + h_next * a.do_s[1]),
+            t.len - row0, ld);
+    if (++j_next == j1) {
+      j_next = j0;
+      ++h_next;
+    }
+  };
+  if (width < DP) {
+    cq.zero_pad(lq0);
+    cq.zero_pad(lq1);
+    cd.zero_pad(ld0);
+    cd.zero_pad(ld1);
+  }
+  f32x2 stat0, stat1;
+  copy(lq0, ld0, stat0);
+  int q0 = j0 * kQs;
+  V8* const own = reinterpret_cast<V8*>(lx + (2 * strip + part) * 4096) + lane;
+  const V8* const others = reinterpret_cast<const V8*>(lx + (2 * strip + 1 - part) * 4096) + lane;
+  auto step = [&](int i, const char* lq, const char* ld, const f32x2& stat, char* next_q, char* next_d,
+                  f32x2& next_stat) {
+    meet<0>();  // tile i is in LDS, and tile i - 1 is done with
+    if (i + 1 < n_tiles) copy(next_q, next_d, next_stat);
+    const int row0 = q0;
+    q0 = q0 + kQs < t.len ? q0 + kQs : j0 * kQs;
+    // a block of 32 queries counts unless all are earlier than the strip's keys or past the end
+    const bool on[2] = {row0 >= k0 && row0 < t.len, row0 + 32 >= k0 && row0 + 32 < t.len};
+    V8 p[2], g[2];
+    if (part ? on[1] : on[0]) {
+      f32x16 s, dp;
+#pragma unroll
+      for (int e = 0; e < 16; ++e) s[e] = dp[e] = 0.0f;
+#pragma unroll
+      for (int c = 0; c < DC; ++c) {
+        s = M::mma(frag_row<M, DP>(lq, 32 * part, 2 * c), k[c], s);
+        dp = M::mma(frag_row<M, DP>(ld, 32 * part, 2 * c), v[c], dp);
+      }
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const int from = (32 * part + acc_row(r) + 4 * half) * 4;
+        const float lse = __int_as_float(__builtin_amdgcn_ds_bpermute(from, __float_as_int(stat[0])));
+        const float delta = __int_as_float(__builtin_amdgcn_ds_bpermute(from, __float_as_int(stat[1])));
+        s[r] = exp2_fast(fmaf(s[r], c2, -lse * kLog2e));
+        dp[r] = s[r] * (dp[r] - delta);
+      }
+      const int b0 = row0 + 32 * part;
+      if (b0 == k0 || b0 + 32 > t.len) {  // the diagonal, or rows past the end
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          const int row = b0 + acc_row(r) + 4 * half;
+          if (row < ki || row >= t.len) s[r] = dp[r] = 0.0f;
+        }
+      }
+#pragma unroll
+      for (int c = 0; c < 2; ++c) {
+        p[c] = pack8<M>(s, c);
+        g[c] = pack8<M>(dp, c);
+        own[64 * c] = p[c];
+        own[64 * (2 + c)] = g[c];
+      }
+    }
+    meet<63>();  // P and dS are in LDS; the next tile is still on its way
+#pragma unroll
+    for (int w = 0; w < 2; ++w) {  // the wave's own block, then the other's
+      const int u = w == 0 ? part : 1 - part;
+      if (!(u ? on[1] : on[0])) continue;
+      if (w == 1) {
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+          p[c] = others[64 * c];
+          g[c] = others[64 * (2 + c)];
+        }
+      }
+#pragma unroll
+      for (int c = 0; c < 2; ++c)
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+          const int d0 = 64 * part + 32 * x;
+          dv[x] = M::mma(frag_col<M, DP>(ld, 32 * u + 16 * c, d0), p[c], dv[x]);
+          dk[x] = M::mma(frag_col<M, DP>(lq, 32 * u + 16 * c, d0), g[c], dk[x]);
+        }
+    }
+  };
+  for (int i = 0; i < n_tiles; i += 2) {
+    step(i, lq0, ld0, stat0, lq1, ld1, stat1);
+    if (i + 1 < n_tiles) step(i + 1, lq1, ld1, stat1, lq0, ld0, stat0);
+  }
+  if (ki < t.len) store_dkv<M, 2>(a, kr, kv, head_part, 64 * part, dk, dv);
+}
+
+// dk and dv from the parts' sums, four elements a thread.
+template <class M>
+__global__ void __launch_bounds__(256) at_sum(const Attention a) {
+  const int64_t size = a.T * a.kv_heads * a.width;
+  const int64_t i = (int64_t(blockIdx.x) * 256 + threadIdx.x) * 4;
+  if (i >= size) return;
+  const int64_t rk = i / a.width;
+  const int d = int(i - rk * a.width);
+  const int64_t row = rk / a.kv_heads, kv = rk - row * a.kv_heads;
+  f32x4 dk = {0, 0, 0, 0}, dv = {0, 0, 0, 0};
+  if (row < sample_begin(a, a.n))
+    for (int p = 0; p < a.parts; ++p) {
+      dk += *reinterpret_cast<const f32x4*>(a.partial + 2 * p * size + i);
+      dv += *reinterpret_cast<const f32x4*>(a.partial + (2 * p + 1) * size + i);
+    }
+  typedef typename M::T T;
+  typename M::V4 k, v;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    k[e] = T(dk[e] * a.scale);
+    v[e] = T(dv[e]);
+  }
+  *reinterpret_cast<typename M::V4*>(static_cast<T*>(a.dk) + row * a.dk_s[0] + kv * a.dk_s[1] + d) = k;
+  *reinterpret_cast<typename M::V4*>(static_cast<T*>(a.dv) + row * a.dv_s[0] + kv * a.dv_s[1] + d) = v;
 }
 
 // --------------------------------------------------------------------- host --
@@ -924,16 +1140,32 @@ int attention_impl(const nopfs_attention* p, const void* q, const void* k, const
   return p->dtype == NOPFS_BF16 ? launch_forward<MBf16, 128>(a, st) : launch_forward<MFp16, 128>(a, st);
 }
 
+// Parts of a group's query heads for dk and dv. A key tile's workgroup goes
+// through its sample's later queries of all of them, one after the other: with
+// few key tiles the longest holds up the call. As many parts as make T x
+// kv_heads x parts what brings the longest workgroup near the average load of
+// the chip (samples of like length), if the group divides so: 8,192 tokens, 16
+// query heads on 4, dk and dv 1168 -> 734 us with 2 parts, 2,048 tokens, 8 on
+// 2, 267 -> 83 with 4, 16,384 tokens of 32 documents, 16 on 4, 377 -> 272 with
+// 2 and 330 with 4 (their sums: 8 bytes per element and part, written and read).
+int32_t dkv_parts(const Attention& a) {
+  const int32_t group = a.heads / a.kv_heads;
+  const int64_t want = 65536 / (a.T * a.kv_heads) + 1;
+  int32_t parts = 1;
+  for (int32_t p = 1; p <= group && p <= want; ++p)
+    if (group % p == 0) parts = p;
+  return parts;
+}
+
 template <class M, int DP>
 int launch_grad(Attention a, hipStream_t st) {
-  // dk, dv: 128 elements a head leave one wave per SIMD its registers, and two
-  // splits then halve the longest workgroup
-  const bool two_q = two_splits(a, a.heads), two_k = DP == 128 || two_splits(a, a.kv_heads);
+  const bool two_q = two_splits(a, a.heads);
+  const bool two_k = DP == 128 || two_splits(a, a.kv_heads * a.parts);
   Attention ak = a;
   dim3 gq, gk;
   int rc = tile_grid(&a, two_q ? 64 : 128, a.heads, &gq);
   if (rc) return rc;
-  if ((rc = tile_grid(&ak, two_k ? 64 : 128, a.kv_heads, &gk))) return rc;
+  if ((rc = tile_grid(&ak, two_k ? 64 : 128, a.kv_heads * a.parts, &gk))) return rc;
   Scratch sc(st);
   if (needs_order(a)) {
     OrderJob jq{nullptr, a.tiles, two_q ? 64 : 128, true}, jk{nullptr, ak.tiles, two_k ? 64 : 128, false};
@@ -947,11 +1179,14 @@ int launch_grad(Attention a, hipStream_t st) {
              : launch("at_dq", at_dq<M, DP, 1>, gq, dim3(256), 0, st, a);
   if (rc) return rc;
   if constexpr (DP == 128) {
-    return launch("at_dkv", at_dkv<M, DP, 2, 64, 3, 1>, gk, dim3(256), 0, st, ak);
+    rc = launch("at_dkv", at_dkv_wide<M>, gk, dim3(256), 0, st, ak);
   } else {
-    return two_k ? launch("at_dkv", at_dkv<M, DP, 2, 64, 2, 2>, gk, dim3(256), 0, st, ak)
-                 : launch("at_dkv", at_dkv<M, DP, 1, 64, 3, 2>, gk, dim3(256), 0, st, ak);
+    rc = two_k ? launch("at_dkv", at_dkv<M, DP, 2, 64, 2, 2>, gk, dim3(256), 0, st, ak)
+               : launch("at_dkv", at_dkv<M, DP, 1, 64, 3, 2>, gk, dim3(256), 0, st, ak);
   }
+  if (rc || a.parts == 1) return rc;
+  const int64_t blocks = ceil_div(a.T * a.kv_heads * a.width / 4, 256);
+  return launch("at_sum", at_sum<M>, dim3(uint32_t(blocks)), dim3(256), 0, st, ak);
 }
 
 int attention_grad_impl(const nopfs_attention* p, const void* d_o, const void* q, const void* k,
@@ -982,6 +1217,10 @@ int attention_grad_impl(const nopfs_attention* p, const void* d_o, const void* q
   a.start = start;
   Scratch sc(st);
   if ((rc = sc.alloc_n(&a.delta, size_t(a.heads) * size_t(a.T)))) return rc;
+  a.parts = dkv_parts(a);
+  if (a.parts > 1 &&
+      (rc = sc.alloc_n(&a.partial, size_t(2 * a.parts) * size_t(a.T) * size_t(a.kv_heads) * size_t(a.width))))
+    return rc;
   if (a.width <= 64)
     return p->dtype == NOPFS_BF16 ? launch_grad<MBf16, 64>(a, st) : launch_grad<MFp16, 64>(a, st);
   return p->dtype == NOPFS_BF16 ? launch_grad<MBf16, 128>(a, st) : launch_grad<MFp16, 128>(a, st);

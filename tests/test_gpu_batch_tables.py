@@ -51,6 +51,8 @@ CASES = [  # G, n, F, blocks, block, width, cap, longest, zeros, pads
     (1, 3, 60, 9, 4_096, 5, 9_001, 9_000, 0, 0),          # blocks larger than a read
     (1_030, 2, 60, 9, 8, 5, 33, 30, 0.1, 0),
     (2, 5_000, 2_000, 30_000, 8, 5, 70_001, 30, 0.1, 0.02),
+    (1, 20_000, 500, 9_000, 8, 2, 30_000, 12, 0.8, 0),   # thousands of reads in a tile
+    (3, 200, 900, 9_000, 16, 40, 120_000, 600, 0.1, 0),   # few reads, many tokens
 ]
 
 
