@@ -318,6 +318,25 @@ __device__ __forceinline__ typename M::V8 pack8(const f32x16& x, int c) {
   return u.v;
 }
 
+// A row's value minus what a first product will add to it: the accumulator of
+// a 32x32 tile, every column -x of its row, from one bf16 matrix product. The
+// lanes of half `part` hold x of rows 0..31; x as a sum of three bf16 values is
+// exact to 2^-24 of it, and the ones of the other operand pick them.
+__device__ __forceinline__ f32x16 minus_rows(float x, int part) {
+  const bool mine = ((threadIdx.x & 63) >> 5) == part;
+  const float y = mine ? -x : 0.0f;
+  const __bf16 one = __bf16(1.0f), zero = __bf16(0.0f);
+  const __bf16 hi = __bf16(y);
+  const float r = y - float(hi);
+  const __bf16 mid = __bf16(r);
+  const MBf16::V8 a = {hi, mid, __bf16(r - float(mid)), zero, zero, zero, zero, zero};
+  const MBf16::V8 b = {one, one, one, zero, zero, zero, zero, zero};
+  f32x16 c;
+#pragma unroll
+  for (int e = 0; e < 16; ++e) c[e] = 0.0f;
+  return MBf16::mma(a, b, c);
+}
+
 // A column's operand chunk straight from global memory: 8 elements at
 // 16 c + 8 half of the lane's own row, 0 past the width.
 template <class M>
@@ -423,10 +442,10 @@ __device__ inline void zero_rows(void* base, const int64_t* s, int64_t head, int
 constexpr int kKeys = 64;  // keys of a tile (forward, dq)
 
 // ------------------------------------------------------------------ forward --
-template <class M, int DP, int kSplits>
+template <class M, int DP, int DW, int kSplits>
 __global__ void __launch_bounds__(256, 2) at_forward(const Attention a) {
   typedef typename M::T T;
-  constexpr int DT = DP / 32, DC = DP / 16;
+  constexpr int DT = DW / 32, DC = DW / 16;
   constexpr int kStrips = 4 / kSplits, kRows = 32 * kStrips, NU = 2 / kSplits;
   constexpr int kTileBytes = kKeys * DP * 2;
   // two buffers, apart by name so that a read waits for its own buffer's copies only
@@ -489,6 +508,8 @@ __global__ void __launch_bounds__(256, 2) at_forward(const Attention a) {
     }
     const int kb = k0 + 32 * NU * split;  // the wave's keys of the tile
     if (kb > q0 + 31) return;  // all later than this wave's queries
+    // the other wave of the SIMD fills in with its exponentials (64 elements a head: no gain)
+    if constexpr (DP == 128) __builtin_amdgcn_s_setprio(1);
     f32x16 s[NU];
 #pragma unroll
     for (int u = 0; u < NU; ++u) {
@@ -498,6 +519,7 @@ __global__ void __launch_bounds__(256, 2) at_forward(const Attention a) {
       for (int c = 0; c < DC; ++c)
         s[u] = M::mma(frag_row<M, DP>(lk, 32 * (NU * split + u), 2 * c), q[c], s[u]);
     }
+    if constexpr (DP == 128) __builtin_amdgcn_s_setprio(0);
     if (kb + 32 * NU - 1 > q0) {
 #pragma unroll
       for (int u = 0; u < NU; ++u)
@@ -529,6 +551,7 @@ __global__ void __launch_bounds__(256, 2) at_forward(const Attention a) {
         s[u][e] = exp2_fast(fmaf(s[u][e], c2, -mc));
         l += s[u][e];
       }
+    if constexpr (DP == 128) __builtin_amdgcn_s_setprio(1);
 #pragma unroll
     for (int u = 0; u < NU; ++u)
 #pragma unroll
@@ -538,6 +561,7 @@ __global__ void __launch_bounds__(256, 2) at_forward(const Attention a) {
         for (int i = 0; i < DT; ++i)
           acc[i] = M::mma(frag_col<M, DP>(lv, 32 * (NU * split + u) + 16 * c, 32 * i), p, acc[i]);
       }
+    if constexpr (DP == 128) __builtin_amdgcn_s_setprio(0);
   };
   for (int j = 0; j < n_tiles; j += 2) {
     step(j, lk0, lv0, lk1, lv1);
@@ -570,10 +594,10 @@ __global__ void __launch_bounds__(256, 2) at_forward(const Attention a) {
 
 // ----------------------------------------------------------------------- dq --
 // Also writes delta_i = do_i.o_i for the dk/dv kernel.
-template <class M, int DP, int kSplits>
+template <class M, int DP, int DW, int kSplits>
 __global__ void __launch_bounds__(256, 2) at_dq(const Attention a) {
   typedef typename M::T T;
-  constexpr int DT = DP / 32, DC = DP / 16;
+  constexpr int DT = DW / 32, DC = DW / 16;
   constexpr int kStrips = 4 / kSplits, kRows = 32 * kStrips, NU = 2 / kSplits;
   constexpr int kTileBytes = kKeys * DP * 2;
   __shared__ __align__(16) char lk0[kTileBytes], lv0[kTileBytes], lk1[kTileBytes], lv1[kTileBytes];
@@ -609,7 +633,7 @@ __global__ void __launch_bounds__(256, 2) at_dq(const Attention a) {
   }
   delta = half_sum(delta);
   const int64_t stat = int64_t(head) * a.T + qr;
-  const float c2 = a.scale * kLog2e, lc = a.lse[stat] * kLog2e;
+  const float c2 = a.scale * kLog2e, minus_lse = -a.lse[stat] / a.scale;
   if (half == 0 && split == 0 && qi < t.len) a.delta[stat] = delta;
 
   f32x16 acc[DT];
@@ -645,14 +669,17 @@ __global__ void __launch_bounds__(256, 2) at_dq(const Attention a) {
       if (kb > q0) break;  // all later than this wave's queries
       f32x16 s, dp;
 #pragma unroll
-      for (int e = 0; e < 16; ++e) s[e] = dp[e] = 0.0f;
+      for (int e = 0; e < 16; ++e) {
+        s[e] = minus_lse;
+        dp[e] = -delta;
+      }
 #pragma unroll
       for (int c = 0; c < DC; ++c) {
         s = M::mma(frag_row<M, DP>(lk, 32 * u, 2 * c), q[c], s);
         dp = M::mma(frag_row<M, DP>(lv, 32 * u, 2 * c), d[c], dp);
       }
 #pragma unroll
-      for (int e = 0; e < 16; ++e) s[e] = exp2_fast(fmaf(s[e], c2, -lc)) * (dp[e] - delta);
+      for (int e = 0; e < 16; ++e) s[e] = exp2_fast(s[e] * c2) * dp[e];
       if (kb == q0) {  // the diagonal: both are multiples of 32
   #pragma unroll
         for (int e = 0; e < 16; ++e)
@@ -686,17 +713,15 @@ __global__ void __launch_bounds__(256, 2) at_dq(const Attention a) {
 // One workgroup: 128 keys of one kv head, over the query heads of its group in
 // order and over the query tiles from the diagonal on. Nothing is added to
 // memory from two places, so the sums' order never changes.
-template <class M, int DP, int kSplits, int kQs, int kStages, int kWaves>
-__global__ void __launch_bounds__(256, kWaves) at_dkv(const Attention a) {
+template <class M, int DP, int DW, int kSplits, int kStages>
+__global__ void __launch_bounds__(256, 2) at_dkv(const Attention a) {
   typedef typename M::T T;
-  constexpr int DT = DP / 32, DC = DP / 16;
-  constexpr int kStrips = 4 / kSplits, kRows = 32 * kStrips;
+  constexpr int DT = DW / 32, DC = DW / 16;
+  constexpr int kStrips = 4 / kSplits, kRows = 32 * kStrips, kQs = 64;
   constexpr int kTileBytes = kQs * DP * 2;
   // buffers, apart by name so that a read waits for its own buffer's copies only
   __shared__ __align__(16) char lq0[kTileBytes], ld0[kTileBytes], lq1[kTileBytes], ld1[kTileBytes];
   __shared__ __align__(16) char lq2[kStages > 2 ? kTileBytes : 1], ld2[kStages > 2 ? kTileBytes : 1];
-  __shared__ __align__(16) char lq3[kStages > 3 ? kTileBytes : 1], ld3[kStages > 3 ? kTileBytes : 1];
-  __shared__ __align__(16) float ls0[2 * kQs], ls1[2 * kQs], ls2[2 * kQs], ls3[2 * kQs];  // lse, delta
   uint32_t tile, kv;
   tile_and_head(blockIdx.x, uint32_t(a.kv_heads * a.parts), &tile, &kv);
   const int head_part = int(kv) % a.parts;  // neighbours: the parts of a kv head
@@ -729,7 +754,7 @@ __global__ void __launch_bounds__(256, kWaves) at_dkv(const Attention a) {
   for (int i = 0; i < DT; ++i)
 #pragma unroll
     for (int e = 0; e < 16; ++e) dk[i][e] = dv[i][e] = 0.0f;
-  const float c2 = a.scale * kLog2e;
+  const float c2 = a.scale * kLog2e, inv_scale = 1.0f / a.scale;
 
   const int group = a.heads / a.kv_heads / a.parts;  // query heads of this part
   const int j0 = t.m0 / kQs;  // the first query tile that sees the tile's keys
@@ -739,68 +764,52 @@ __global__ void __launch_bounds__(256, kWaves) at_dkv(const Attention a) {
   // the tile copied next: query head and tile of the sample
   int64_t h_next = (int64_t(kv) * a.parts + head_part) * group;
   int j_next = j0;
-  // lse and delta go with the tile: a wave copies 64 of the 2 kQs values
-  constexpr int kStatWaves = 2 * kQs / 64;
-  auto copy = [&](char* lq, char* ld, float* ls) {
+  auto copy = [&](char* lq, char* ld, f32x2& stat) {
     const int row0 = j_next * kQs;
+    const int64_t at = h_next * a.T + t.begin + min(row0 + lane, t.len - 1);
+    stat = f32x2{a.lse[at], a.delta[at]};  // of row `lane` of the tile
     cq.copy(reinterpret_cast<const char*>(static_cast<const T*>(a.q) + (t.begin + row0) * a.q_s[0] + h_next * a.q_s[1]),
             t.len - row0, lq);
     cd.copy(reinterpret_cast<const char*>(static_cast<const T*>(a.d_o) + (t.begin + row0) * a.do_s[0] + h_next * a.do_s[1]),
             t.len - row0, ld);
-    const int part = wave % kStatWaves;  // waves beyond them copy the same again: all issue alike
-    const int at = part * 64 % kQs;
-    const float* from = (part * 64 < kQs ? a.lse : a.delta) + h_next * a.T + t.begin;
-    __builtin_amdgcn_global_load_lds(
-        (const __attribute__((address_space(1))) void*)(from + min(row0 + at + lane, t.len - 1)),
-        (__attribute__((address_space(3))) void*)(ls + part * 64), 4, 0, 0);
     if (++j_next == j1) {
       j_next = j0;
       ++h_next;
     }
   };
-  constexpr int kCopies = cq.kPer + cd.kPer + 1;  // of a tile, by each wave
+  constexpr int kCopies = cq.kPer + cd.kPer + 2;  // of a tile, by each wave
   if (width < DP) {
     cq.zero_pad(lq0);
     cq.zero_pad(lq1);
     cd.zero_pad(ld0);
     cd.zero_pad(ld1);
     if (kStages > 2) cq.zero_pad(lq2), cd.zero_pad(ld2);
-    if (kStages > 3) cq.zero_pad(lq3), cd.zero_pad(ld3);
   }
-  copy(lq0, ld0, ls0);
-  if (kStages > 2 && n_tiles > 1) copy(lq1, ld1, ls1);
-  if (kStages > 3 && n_tiles > 2) copy(lq2, ld2, ls2);
+  f32x2 stat0, stat1, stat2;
+  copy(lq0, ld0, stat0);
+  if (kStages > 2 && n_tiles > 1) copy(lq1, ld1, stat1);
   int q0 = j0 * kQs;
-  auto step = [&](int i, const char* lq, const char* ld, const float* ls, char* next_q, char* next_d, float* next_s) {
+  auto step = [&](int i, const char* lq, const char* ld, const f32x2& stat, char* next_q, char* next_d,
+                  f32x2& next_stat) {
     // tile i is in LDS, and tile i - 1 is done with
-    const int behind = min(n_tiles - 1 - i, kStages - 2);
-    if (behind == 2) meet<2 * kCopies>();
-    else if (behind == 1) meet<kCopies>();
+    if (kStages > 2 && i + 1 < n_tiles) meet<kCopies>();
     else meet<0>();
-    if (i + kStages - 1 < n_tiles) copy(next_q, next_d, next_s);
+    if (i + kStages - 1 < n_tiles) copy(next_q, next_d, next_stat);
     const int row0 = q0;
     q0 = q0 + kQs < t.len ? q0 + kQs : j0 * kQs;
 #pragma unroll 1
     for (int u = split; u < kQs / 32; u += kSplits) {
       if (row0 + 32 * u < k0) continue;  // all earlier than this wave's keys
-      f32x16 s, dp;
-#pragma unroll
-      for (int e = 0; e < 16; ++e) s[e] = dp[e] = 0.0f;
+      f32x16 s = minus_rows(stat[0] * inv_scale, u), dp = minus_rows(stat[1], u);
 #pragma unroll
       for (int c = 0; c < DC; ++c) {
         s = M::mma(frag_row<M, DP>(lq, 32 * u, 2 * c), k[c], s);
         dp = M::mma(frag_row<M, DP>(ld, 32 * u, 2 * c), v[c], dp);
       }
 #pragma unroll
-      for (int b = 0; b < 4; ++b) {
-        const f32x4 lc = *reinterpret_cast<const f32x4*>(ls + 32 * u + 8 * b + 4 * half);
-        const f32x4 de = *reinterpret_cast<const f32x4*>(ls + kQs + 32 * u + 8 * b + 4 * half);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const int r = 4 * b + e;
-          s[r] = exp2_fast(fmaf(s[r], c2, -lc[e] * kLog2e));
-          dp[r] = s[r] * (dp[r] - de[e]);
-        }
+      for (int r = 0; r < 16; ++r) {
+        s[r] = exp2_fast(s[r] * c2);
+        dp[r] *= s[r];
       }
       if (row0 + 32 * u == k0) {  // the diagonal: both are multiples of 32
   #pragma unroll
@@ -826,17 +835,12 @@ __global__ void __launch_bounds__(256, kWaves) at_dkv(const Attention a) {
   };
   for (int i = 0; i < n_tiles; i += kStages) {
     if constexpr (kStages == 2) {
-      step(i, lq0, ld0, ls0, lq1, ld1, ls1);
-      if (i + 1 < n_tiles) step(i + 1, lq1, ld1, ls1, lq0, ld0, ls0);
-    } else if constexpr (kStages == 3) {
-      step(i, lq0, ld0, ls0, lq2, ld2, ls2);
-      if (i + 1 < n_tiles) step(i + 1, lq1, ld1, ls1, lq0, ld0, ls0);
-      if (i + 2 < n_tiles) step(i + 2, lq2, ld2, ls2, lq1, ld1, ls1);
+      step(i, lq0, ld0, stat0, lq1, ld1, stat1);
+      if (i + 1 < n_tiles) step(i + 1, lq1, ld1, stat1, lq0, ld0, stat0);
     } else {
-      step(i, lq0, ld0, ls0, lq3, ld3, ls3);
-      if (i + 1 < n_tiles) step(i + 1, lq1, ld1, ls1, lq0, ld0, ls0);
-      if (i + 2 < n_tiles) step(i + 2, lq2, ld2, ls2, lq1, ld1, ls1);
-      if (i + 3 < n_tiles) step(i + 3, lq3, ld3, ls3, lq2, ld2, ls2);
+      step(i, lq0, ld0, stat0, lq2, ld2, stat2);
+      if (i + 1 < n_tiles) step(i + 1, lq1, ld1, stat1, lq0, ld0, stat0);
+      if (i + 2 < n_tiles) step(i + 2, lq2, ld2, stat2, lq1, ld1, stat1);
     }
   }
   if constexpr (kSplits == 2) {
@@ -863,11 +867,11 @@ __global__ void __launch_bounds__(256, kWaves) at_dkv(const Attention a) {
 // lane), and then sums one half of the head's elements over all 64: half the
 // sums per wave, and two workgroups share a compute unit. Their LDS is exactly
 // half of it, so lse and delta stay in registers, one row per lane.
-template <class M>
+template <class M, int DW>
 __global__ void __launch_bounds__(256, 2) at_dkv_wide(const Attention a) {
   typedef typename M::T T;
   typedef typename M::V8 V8;
-  constexpr int DP = 128, DC = DP / 16, kRows = 64, kQs = 64;
+  constexpr int DP = 128, DC = DW / 16, kRows = 64, kQs = 64;
   constexpr int kTileBytes = kQs * DP * 2;
   __shared__ __align__(16) char lq0[kTileBytes], ld0[kTileBytes], lq1[kTileBytes], ld1[kTileBytes];
   __shared__ __align__(16) char lx[4 * 4096];  // P and dS: 4 operands of every wave
@@ -903,7 +907,7 @@ __global__ void __launch_bounds__(256, 2) at_dkv_wide(const Attention a) {
   for (int i = 0; i < 2; ++i)
 #pragma unroll
     for (int e = 0; e < 16; ++e) dk[i][e] = dv[i][e] = 0.0f;
-  const float c2 = a.scale * kLog2e;
+  const float c2 = a.scale * kLog2e, inv_scale = 1.0f / a.scale;
 
   const int group = a.heads / a.kv_heads / a.parts;
   const int j0 = t.m0 / kQs;
@@ -946,21 +950,18 @@ __global__ void __launch_bounds__(256, 2) at_dkv_wide(const Attention a) {
     const bool on[2] = {row0 >= k0 && row0 < t.len, row0 + 32 >= k0 && row0 + 32 < t.len};
     V8 p[2], g[2];
     if (part ? on[1] : on[0]) {
-      f32x16 s, dp;
-#pragma unroll
-      for (int e = 0; e < 16; ++e) s[e] = dp[e] = 0.0f;
+      __builtin_amdgcn_s_setprio(1);  // the other wave of the SIMD fills in with its exponentials
+      f32x16 s = minus_rows(stat[0] * inv_scale, part), dp = minus_rows(stat[1], part);
 #pragma unroll
       for (int c = 0; c < DC; ++c) {
         s = M::mma(frag_row<M, DP>(lq, 32 * part, 2 * c), k[c], s);
         dp = M::mma(frag_row<M, DP>(ld, 32 * part, 2 * c), v[c], dp);
       }
+      __builtin_amdgcn_s_setprio(0);
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
-        const int from = (32 * part + acc_row(r) + 4 * half) * 4;
-        const float lse = __int_as_float(__builtin_amdgcn_ds_bpermute(from, __float_as_int(stat[0])));
-        const float delta = __int_as_float(__builtin_amdgcn_ds_bpermute(from, __float_as_int(stat[1])));
-        s[r] = exp2_fast(fmaf(s[r], c2, -lse * kLog2e));
-        dp[r] = s[r] * (dp[r] - delta);
+        s[r] = exp2_fast(s[r] * c2);
+        dp[r] *= s[r];
       }
       const int b0 = row0 + 32 * part;
       if (b0 == k0 || b0 + 32 > t.len) {  // the diagonal, or rows past the end
@@ -979,6 +980,7 @@ __global__ void __launch_bounds__(256, 2) at_dkv_wide(const Attention a) {
       }
     }
     meet<63>();  // P and dS are in LDS; the next tile is still on its way
+    __builtin_amdgcn_s_setprio(1);
 #pragma unroll
     for (int w = 0; w < 2; ++w) {  // the wave's own block, then the other's
       const int u = w == 0 ? part : 1 - part;
@@ -995,10 +997,12 @@ __global__ void __launch_bounds__(256, 2) at_dkv_wide(const Attention a) {
 #pragma unroll
         for (int x = 0; x < 2; ++x) {
           const int d0 = 64 * part + 32 * x;
+          if (d0 >= DW) continue;
           dv[x] = M::mma(frag_col<M, DP>(ld, 32 * u + 16 * c, d0), p[c], dv[x]);
           dk[x] = M::mma(frag_col<M, DP>(lq, 32 * u + 16 * c, d0), g[c], dk[x]);
         }
     }
+    __builtin_amdgcn_s_setprio(0);
   };
   for (int i = 0; i < n_tiles; i += 2) {
     step(i, lq0, ld0, stat0, lq1, ld1, stat1);
@@ -1100,7 +1104,7 @@ bool two_splits(const Attention& a, int32_t heads) { return (a.T / 128 + 1) * he
 // is in order by itself, and samples below a tile all cost the same.
 bool needs_order(const Attention& a) { return a.n > 1 && a.T >= 4096 && a.T / a.n >= 64; }
 
-template <class M, int DP>
+template <class M, int DP, int DW>
 int launch_forward(Attention a, hipStream_t st) {
   const bool two = two_splits(a, a.heads);
   const int32_t rows = two ? 64 : 128;
@@ -1114,8 +1118,18 @@ int launch_forward(Attention a, hipStream_t st) {
     if ((rc = launch("at_order", at_order, dim3(1), dim3(1024), 0, st, a, j, j))) return rc;
     a.order = j.order;
   }
-  return two ? launch("at_forward", at_forward<M, DP, 2>, grid, dim3(256), 0, st, a)
-             : launch("at_forward", at_forward<M, DP, 1>, grid, dim3(256), 0, st, a);
+  return two ? launch("at_forward", at_forward<M, DP, DW, 2>, grid, dim3(256), 0, st, a)
+             : launch("at_forward", at_forward<M, DP, DW, 1>, grid, dim3(256), 0, st, a);
+}
+
+// Products run over the head's elements rounded up to 32; LDS rows hold 64 or
+// 128 of them, the rest of a row is 0.
+template <class M>
+int launch_forward(const Attention& a, hipStream_t st) {
+  if (a.width <= 32) return launch_forward<M, 64, 32>(a, st);
+  if (a.width <= 64) return launch_forward<M, 64, 64>(a, st);
+  if (a.width <= 96) return launch_forward<M, 128, 96>(a, st);
+  return launch_forward<M, 128, 128>(a, st);
 }
 
 int attention_impl(const nopfs_attention* p, const void* q, const void* k, const void* v,
@@ -1135,9 +1149,7 @@ int attention_impl(const nopfs_attention* p, const void* q, const void* k, const
   a.o = o;
   a.lse = lse;
   a.start = start;
-  if (a.width <= 64)
-    return p->dtype == NOPFS_BF16 ? launch_forward<MBf16, 64>(a, st) : launch_forward<MFp16, 64>(a, st);
-  return p->dtype == NOPFS_BF16 ? launch_forward<MBf16, 128>(a, st) : launch_forward<MFp16, 128>(a, st);
+  return p->dtype == NOPFS_BF16 ? launch_forward<MBf16>(a, st) : launch_forward<MFp16>(a, st);
 }
 
 // Parts of a group's query heads for dk and dv. A key tile's workgroup goes
@@ -1157,7 +1169,7 @@ int32_t dkv_parts(const Attention& a) {
   return parts;
 }
 
-template <class M, int DP>
+template <class M, int DP, int DW>
 int launch_grad(Attention a, hipStream_t st) {
   const bool two_q = two_splits(a, a.heads);
   const bool two_k = DP == 128 || two_splits(a, a.kv_heads * a.parts);
@@ -1175,18 +1187,26 @@ int launch_grad(Attention a, hipStream_t st) {
     a.order = jq.order;
     ak.order = jk.order;
   }
-  rc = two_q ? launch("at_dq", at_dq<M, DP, 2>, gq, dim3(256), 0, st, a)
-             : launch("at_dq", at_dq<M, DP, 1>, gq, dim3(256), 0, st, a);
+  rc = two_q ? launch("at_dq", at_dq<M, DP, DW, 2>, gq, dim3(256), 0, st, a)
+             : launch("at_dq", at_dq<M, DP, DW, 1>, gq, dim3(256), 0, st, a);
   if (rc) return rc;
   if constexpr (DP == 128) {
-    rc = launch("at_dkv", at_dkv_wide<M>, gk, dim3(256), 0, st, ak);
+    rc = launch("at_dkv", at_dkv_wide<M, DW>, gk, dim3(256), 0, st, ak);
   } else {
-    rc = two_k ? launch("at_dkv", at_dkv<M, DP, 2, 64, 2, 2>, gk, dim3(256), 0, st, ak)
-               : launch("at_dkv", at_dkv<M, DP, 1, 64, 3, 2>, gk, dim3(256), 0, st, ak);
+    rc = two_k ? launch("at_dkv", at_dkv<M, DP, DW, 2, 2>, gk, dim3(256), 0, st, ak)
+               : launch("at_dkv", at_dkv<M, DP, DW, 1, 3>, gk, dim3(256), 0, st, ak);
   }
   if (rc || a.parts == 1) return rc;
   const int64_t blocks = ceil_div(a.T * a.kv_heads * a.width / 4, 256);
   return launch("at_sum", at_sum<M>, dim3(uint32_t(blocks)), dim3(256), 0, st, ak);
+}
+
+template <class M>
+int launch_grad(const Attention& a, hipStream_t st) {
+  if (a.width <= 32) return launch_grad<M, 64, 32>(a, st);
+  if (a.width <= 64) return launch_grad<M, 64, 64>(a, st);
+  if (a.width <= 96) return launch_grad<M, 128, 96>(a, st);
+  return launch_grad<M, 128, 128>(a, st);
 }
 
 int attention_grad_impl(const nopfs_attention* p, const void* d_o, const void* q, const void* k,
@@ -1221,9 +1241,7 @@ int attention_grad_impl(const nopfs_attention* p, const void* d_o, const void* q
   if (a.parts > 1 &&
       (rc = sc.alloc_n(&a.partial, size_t(2 * a.parts) * size_t(a.T) * size_t(a.kv_heads) * size_t(a.width))))
     return rc;
-  if (a.width <= 64)
-    return p->dtype == NOPFS_BF16 ? launch_grad<MBf16, 64>(a, st) : launch_grad<MFp16, 64>(a, st);
-  return p->dtype == NOPFS_BF16 ? launch_grad<MBf16, 128>(a, st) : launch_grad<MFp16, 128>(a, st);
+  return p->dtype == NOPFS_BF16 ? launch_grad<MBf16>(a, st) : launch_grad<MFp16>(a, st);
 }
 
 }  // namespace
