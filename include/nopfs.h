@@ -407,7 +407,7 @@ int nopfs_batch_tables(const nopfs_batch* batch, const int32_t* ids, const int32
 /* Causal attention over n packed samples of different lengths. Strides are in
  * elements: [0] from token to token, [1] from head to head; the `width`
  * elements of a head are adjacent. Pointers and strides of the 16-bit arrays
- * are multiples of 16 bytes. */
+ * are multiples of 16 bytes, token strides at most 2^23 elements. */
 typedef struct nopfs_attention {
   int64_t T;           /* rows (tokens, padding included)                    */
   int32_t n;           /* samples, >= 0                                      */
@@ -429,7 +429,9 @@ typedef struct nopfs_attention {
  *          but in-bounds results).
  *   lse:   float [heads][T].
  * Rows from start[n] on belong to no sample: o = 0 and lse = -inf, and what q,
- * k and v hold there is not read. Errors: EINVAL, ERANGE, ENOMEM, EDEVICE. */
+ * k and v hold there is not read. A NaN or infinity in a sample's own later
+ * tokens may reach up to 63 rows before it (as 0 times it), other samples'
+ * never do. Errors: EINVAL, ERANGE, ENOMEM, EDEVICE. */
 int nopfs_packed_attention(const nopfs_attention* a, const void* q, const void* k, const void* v,
                            const int32_t* start, void* o, float* lse, void* hip_stream);
 

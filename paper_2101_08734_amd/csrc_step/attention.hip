@@ -1052,13 +1052,9 @@ int check_array(const char* name, const void* p, const int64_t* s, int64_t heads
 }
 
 // Row tiles of `rows` rows at most, and the grid over them and the heads.
-int tile_grid(Attention* a, int rows, int32_t heads, dim3* grid) {
-  const int64_t tiles = a->T / rows + a->n + 1;
-  if (tiles * heads > (int64_t(1) << 31) - 16)
-    return fail(NOPFS_ERANGE, "too many rows, samples and heads for one call");
-  a->tiles = uint32_t(tiles);
-  *grid = dim3(uint32_t(tiles * heads));
-  return NOPFS_OK;
+dim3 tile_grid(Attention* a, int rows, int32_t heads) {
+  a->tiles = uint32_t(a->T / rows + a->n + 1);
+  return dim3(a->tiles * uint32_t(heads));
 }
 
 int make_attention(const nopfs_attention* p, Attention* a) {
@@ -1074,6 +1070,8 @@ int make_attention(const nopfs_attention* p, Attention* a) {
     return fail(NOPFS_EINVAL, "scale must be positive and finite");
   if (p->T >= (int64_t(1) << 31) - 128 || p->n > (1 << 30))
     return fail(NOPFS_ERANGE, "T must be < 2^31 - 128, n <= 2^30");
+  if ((p->T / 64 + p->n + 1) * p->heads >= (int64_t(1) << 31))  // the largest grid
+    return fail(NOPFS_ERANGE, "too many rows, samples and heads for one call");
   a->T = p->T;
   a->n = p->n;
   a->heads = p->heads;
@@ -1108,9 +1106,8 @@ template <class M, int DP, int DW>
 int launch_forward(Attention a, hipStream_t st) {
   const bool two = two_splits(a, a.heads);
   const int32_t rows = two ? 64 : 128;
-  dim3 grid;
-  int rc = tile_grid(&a, rows, a.heads, &grid);
-  if (rc) return rc;
+  const dim3 grid = tile_grid(&a, rows, a.heads);
+  int rc;
   Scratch sc(st);
   if (needs_order(a)) {
     OrderJob j{nullptr, a.tiles, rows, true};
@@ -1174,10 +1171,9 @@ int launch_grad(Attention a, hipStream_t st) {
   const bool two_q = two_splits(a, a.heads);
   const bool two_k = DP == 128 || two_splits(a, a.kv_heads * a.parts);
   Attention ak = a;
-  dim3 gq, gk;
-  int rc = tile_grid(&a, two_q ? 64 : 128, a.heads, &gq);
-  if (rc) return rc;
-  if ((rc = tile_grid(&ak, two_k ? 64 : 128, a.kv_heads * a.parts, &gk))) return rc;
+  const dim3 gq = tile_grid(&a, two_q ? 64 : 128, a.heads);
+  const dim3 gk = tile_grid(&ak, two_k ? 64 : 128, a.kv_heads * a.parts);
+  int rc;
   Scratch sc(st);
   if (needs_order(a)) {
     OrderJob jq{nullptr, a.tiles, two_q ? 64 : 128, true}, jk{nullptr, ak.tiles, two_k ? 64 : 128, false};
