@@ -146,10 +146,10 @@ __global__ void __launch_bounds__(kThreads) bt_scan(const Batch b, const Divider
   }
 }
 
-// Packed tokens or table entries of a workgroup. Of bt_expand, 256 groups x
-// 294,912 tokens: 241 us with 8,192, 258 with 4,096, 330 with 1,024, 261 with
-// 16,384. Of bt_small, one group of 12,288 tokens: 6.8 us with 1,024, 10 with
-// 4,096.
+// Packed tokens or table entries of a workgroup: 256 groups x 294,912 tokens
+// took bt_expand 241 us with 8,192, 258 with 4,096, 330 with 1,024, 261 with
+// 16,384; where that leaves compute units idle, 1,024 (one group of 12,288
+// tokens took bt_small 6.8 us with 1,024, 10 with 4,096).
 constexpr int kTile = 8192, kSmallTile = 1024;
 constexpr int kTileRows = 1024;  // starts of a tile kept in LDS
 
@@ -264,6 +264,7 @@ __device__ inline int32_t find_read(const int32_t* start, int32_t lo, int32_t hi
   return lo;
 }
 
+template <int kTile>
 __global__ void __launch_bounds__(256) bt_expand(const Batch b, uint32_t tok_tiles, uint32_t tab_tiles,
                                                  const Divider by_block) {
   __shared__ int32_t s_start[kTileRows + 2], s_first[kTileRows + 2];
@@ -326,8 +327,9 @@ __global__ void __launch_bounds__(256) bt_small(const Batch b, uint32_t tok_tile
     table_tile<kSmallTile>(b, g, int64_t(t - tok_tiles) * kSmallTile, s_first);
 }
 
-// Tiles up to which the sums are repeated rather than made in a launch of
-// their own: as many as the chip runs at once.
+// Tiles that the chip runs at once: up to so many small ones the sums are
+// repeated rather than made in a launch of their own, and below so many large
+// ones small ones are taken.
 constexpr int64_t kSmallTiles = 2048;
 
 int batch_tables_impl(const nopfs_batch* p, const int32_t* ids, const int32_t* tokens,
@@ -344,14 +346,16 @@ int batch_tables_impl(const nopfs_batch* p, const int32_t* ids, const int32_t* t
     return fail(NOPFS_EINVAL, "tokens, the free lists and every output must be non-NULL");
   if (p->cap > (1 << 30) || p->n > (1 << 30)) return fail(NOPFS_ERANGE, "cap and n must be <= 2^30");
   const int64_t entries = int64_t(p->n) * p->width;
-  const int64_t tok_tiles = ceil_div(p->cap, kTile), tab_tiles = ceil_div(entries, kTile);
+  const int64_t small_tok = ceil_div(p->cap, kSmallTile), small_tab = ceil_div(entries, kSmallTile);
+  int64_t tok_tiles = ceil_div(p->cap, kTile), tab_tiles = ceil_div(entries, kTile);
+  const bool small = p->G * (tok_tiles + tab_tiles) < kSmallTiles;
+  if (small) tok_tiles = small_tok, tab_tiles = small_tab;
   const int64_t tiles = int64_t(p->G) * (tok_tiles + tab_tiles);
   if (tiles >= int64_t(INT32_MAX))
     return fail(NOPFS_ERANGE, "too many table entries and packed tokens for one call");
   Batch b{p->F, p->ids_stride, p->free_stride, p->G, p->n, p->blocks, p->block, p->width, p->cap,
           ids, tokens, free_list, start, table, slot, row, pos, used, nullptr};
   const Divider by_block(p->block);
-  const int64_t small_tok = ceil_div(p->cap, kSmallTile), small_tab = ceil_div(entries, kSmallTile);
   if (p->n <= 256 && p->G * (small_tok + small_tab) <= kSmallTiles)
     return launch("bt_small", bt_small, dim3(uint32_t(p->G * (small_tok + small_tab))), dim3(256), 0, st, b,
                   uint32_t(small_tok), uint32_t(small_tab), by_block);
@@ -361,8 +365,8 @@ int batch_tables_impl(const nopfs_batch* p, const int32_t* ids, const int32_t* t
   rc = p->n <= 256 ? launch("bt_scan", bt_scan<256>, dim3(uint32_t(p->G)), dim3(256), 0, st, b, by_block)
                    : launch("bt_scan", bt_scan<1024>, dim3(uint32_t(p->G)), dim3(1024), 0, st, b, by_block);
   if (rc) return rc;
-  return launch("bt_expand", bt_expand, dim3(uint32_t(tiles)), dim3(256), 0, st, b, uint32_t(tok_tiles),
-                uint32_t(tab_tiles), by_block);
+  return launch("bt_expand", small ? bt_expand<kSmallTile> : bt_expand<kTile>, dim3(uint32_t(tiles)), dim3(256), 0, st,
+                b, uint32_t(tok_tiles), uint32_t(tab_tiles), by_block);
 }
 
 }  // namespace

@@ -451,22 +451,38 @@ def _step_shape(t, name, shape):
         raise ValueError(f"{name} must have shape {tuple(shape)}, not {tuple(t.shape)}")
 
 
-def _step_stream(stream, device, tensors):
-    """The stream's handle. Where it is not the current one, the allocator is
-    told that the call's tensors are in use there."""
-    current = torch.cuda.current_stream(device).cuda_stream
-    if stream is None or stream.cuda_stream == current:
-        return current
-    for t in tensors:
-        if t is not None:
-            t.record_stream(stream)
-    return stream.cuda_stream
-
-
 def _dense(t, name):
     if not t.is_contiguous():
         raise ValueError(f"{name} must be contiguous")
     return t
+
+
+def _step_dense(t, name, dtype, shape, device):
+    """A contiguous device tensor of this type and shape on the current device:
+    one test where it is one, the reason where it is not."""
+    if (isinstance(t, torch.Tensor) and t.dtype is dtype and t.shape == shape
+            and t.is_contiguous() and t.get_device() == device):
+        return t
+    _step_shape(_step_tensor(t, name, (dtype,), len(shape), device), name, shape)
+    return _dense(t, name)
+
+
+# The current stream's handle without the object around it, which takes 1 us to
+# make, a tenth of a small call.
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
+    lambda device: torch.cuda.current_stream(device).cuda_stream)
+
+
+def _step_stream(stream, device, tensors):
+    """The stream's handle. Where it is not the current one, the allocator is
+    told that the call's tensors are in use there."""
+    if stream is None:
+        return _raw_stream(device)
+    if stream.cuda_stream != _raw_stream(device):
+        for t in tensors:
+            if t is not None:
+                t.record_stream(stream)
+    return stream.cuda_stream
 
 
 def _row_stride(t):
@@ -500,7 +516,7 @@ def batch_tables(ids, tokens, free, block: int, width: int, cap: int, out=None, 
         raise ValueError(f"free must have {G} rows")
     if not (0 < block < 2**31 and 0 < width < 2**31 and 0 <= cap < 2**31):
         raise ValueError("block and width must be positive, cap not negative, all below 2^31")
-    o = dict(out or {})
+    o = dict(out) if out else {}
     for name, shape, dt in (("start", (G, n + 1), torch.int32), ("table", (G, n, width), torch.int32),
                             ("slot", (G, cap), torch.int64), ("row", (G, cap), torch.int32),
                             ("pos", (G, cap), torch.int32), ("used", (G, 3), torch.int32)):
@@ -508,8 +524,7 @@ def batch_tables(ids, tokens, free, block: int, width: int, cap: int, out=None, 
         if t is None:
             o[name] = lead.new_empty(shape, dtype=dt)
         else:
-            _dense(_step_tensor(t, name, (dt,), len(shape), dev), name)
-            _step_shape(t, name, shape)
+            _step_dense(t, name, dt, shape, dev)
     b = _Batch(F, _row_stride(lead), _row_stride(free), G, n, free.shape[1], block, width, cap)
     st = _step_stream(stream, dev, (ids, tokens, free, *o.values()))
     _check(lib().nopfs_batch_tables(
@@ -562,8 +577,7 @@ def packed_attention(q, k, v, start, scale=None, o=None, lse=None, stream=None):
     if lse is None:
         lse = q.new_empty((a[2], a[0]), dtype=torch.float32)
     else:
-        _step_shape(_dense(_step_tensor(lse, "lse", (torch.float32,), 2, dev), "lse"), "lse",
-                    (a[2], a[0]))
+        _step_dense(lse, "lse", torch.float32, (a[2], a[0]), dev)
     a = _Attention(*a, *_strides(q, k, v, o))
     st = _step_stream(stream, dev, (q, k, v, start, o, lse))
     _check(lib().nopfs_packed_attention(ctypes.byref(a), q.data_ptr(), k.data_ptr(), v.data_ptr(),
@@ -582,8 +596,7 @@ def packed_attention_grad(do, q, k, v, o, lse, start, scale=None, dq=None, dk=No
     same = (q.dtype,)
     for name, t in (("do", do), ("o", o)):
         _step_shape(_step_tensor(t, name, same, 3, dev), name, q.shape)
-    _step_shape(_dense(_step_tensor(lse, "lse", (torch.float32,), 2, dev), "lse"), "lse",
-                (a[2], a[0]))
+    _step_dense(lse, "lse", torch.float32, (a[2], a[0]), dev)
     grads = []
     for name, t, like in (("dq", dq, q), ("dk", dk, k), ("dv", dv, v)):
         if t is None:
@@ -609,18 +622,16 @@ def topk_distill(logits, index, teacher, tau=1.0, weight=None, grad=True, loss=N
     masked). Returns loss [T] float32 and, unless grad is False, its gradient
     by the logits (in their type; dlogits may be logits itself)."""
     dev = torch.cuda.current_device()
-    T, V = _step_tensor(logits, "logits", tuple(_DTYPES), 2, dev).shape
+    T, V = _step_tensor(logits, "logits", _DTYPES, 2, dev).shape
     K = _step_tensor(index, "index", _I32, 2, dev).shape[1]
     _step_shape(index, "index", (T, K))
-    _step_shape(_step_tensor(teacher, "teacher", tuple(_DTYPES), 2, dev), "teacher", (T, K))
+    _step_shape(_step_tensor(teacher, "teacher", _DTYPES, 2, dev), "teacher", (T, K))
     if weight is not None:
-        _step_shape(_dense(_step_tensor(weight, "weight", (torch.float32,), 1, dev), "weight"),
-                    "weight", (T,))
+        _step_dense(weight, "weight", torch.float32, (T,), dev)
     if loss is None:
         loss = logits.new_empty(T, dtype=torch.float32)
     else:
-        _step_shape(_dense(_step_tensor(loss, "loss", (torch.float32,), 1, dev), "loss"), "loss",
-                    (T,))
+        _step_dense(loss, "loss", torch.float32, (T,), dev)
     if not grad:
         dlogits = None
     elif dlogits is None:
