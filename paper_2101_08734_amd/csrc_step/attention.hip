@@ -437,16 +437,18 @@ __device__ inline void zero_rows(void* base, const int64_t* s, int64_t head, int
 }
 
 // A workgroup's 4 waves are strips of 32 columns, times splits of the other
-// side: with two splits, two waves share a strip's columns, each takes every
-// other block of the tiles, and their sums are joined through LDS at the end.
-constexpr int kKeys = 64;  // keys of a tile (forward, dq)
+// side: with several splits, as many waves share a strip's columns, each takes
+// its share of every tile's blocks, and their sums are joined through LDS at
+// the end. Keys of a tile (forward, dq): a block of 32 for every split, or two.
+template <int kSplits>
+constexpr int kTileKeys = kSplits == 4 ? 128 : 64;
 
 // ------------------------------------------------------------------ forward --
 template <class M, int DP, int DW, int kSplits>
-__global__ void __launch_bounds__(256, 2) at_forward(const Attention a) {
+__global__ void __launch_bounds__(256, kSplits == 4 && DP == 128 ? 1 : 2) at_forward(const Attention a) {
   typedef typename M::T T;
   constexpr int DT = DW / 32, DC = DW / 16;
-  constexpr int kStrips = 4 / kSplits, kRows = 32 * kStrips, NU = 2 / kSplits;
+  constexpr int kKeys = kTileKeys<kSplits>, kStrips = 4 / kSplits, kRows = 32 * kStrips, NU = kKeys / 32 / kSplits;
   constexpr int kTileBytes = kKeys * DP * 2;
   // two buffers, apart by name so that a read waits for its own buffer's copies only
   __shared__ __align__(16) char lk0[kTileBytes], lv0[kTileBytes], lk1[kTileBytes], lv1[kTileBytes];
@@ -567,23 +569,28 @@ __global__ void __launch_bounds__(256, 2) at_forward(const Attention a) {
     step(j, lk0, lv0, lk1, lv1);
     if (j + 1 < n_tiles) step(j + 1, lk1, lv1, lk0, lv0);
   }
-  if constexpr (kSplits == 2) {
-    // the second split's sums join the first's, rescaled to the larger maximum
+  if constexpr (kSplits > 1) {
+    // the other splits' sums join the first's, rescaled to the larger maximum
+    auto place = [&](int i) -> char* { return i == 0 ? lk0 : i == 1 ? lv0 : lk1; };
+    float* stats = reinterpret_cast<float*>(lv1) + lane;
     __syncthreads();
-    float* st = reinterpret_cast<float*>(lk1) + strip * 128 + lane;
-    char* part = strip ? lv0 : lk0;
+    const int slot = (split - 1) * kStrips + strip;
     if (split) {
-      give_columns<DT>(part, acc);
-      st[0] = m;
-      st[64] = l;
+      give_columns<DT>(place(slot), acc);
+      stats[128 * slot] = m;
+      stats[128 * slot + 64] = l;
     }
     __syncthreads();
     if (split) return;
-    const float m1 = st[0], top = fmaxf(m, m1);
-    const float f0 = exp2_fast((m - top) * c2), f1 = exp2_fast((m1 - top) * c2);
-    take_columns<DT>(part, acc, f0, f1);
-    l = l * f0 + st[64] * f1;
-    m = top;
+#pragma unroll
+    for (int x = 0; x < kSplits - 1; ++x) {
+      const float* st = stats + 128 * (x * kStrips + strip);
+      const float m1 = st[0], top = fmaxf(m, m1);
+      const float f0 = exp2_fast((m - top) * c2), f1 = exp2_fast((m1 - top) * c2);
+      take_columns<DT>(place(x * kStrips + strip), acc, f0, f1);
+      l = l * f0 + st[64] * f1;
+      m = top;
+    }
   }
   l = half_sum(l);
   if (qi < t.len) {
@@ -595,10 +602,10 @@ __global__ void __launch_bounds__(256, 2) at_forward(const Attention a) {
 // ----------------------------------------------------------------------- dq --
 // Also writes delta_i = do_i.o_i for the dk/dv kernel.
 template <class M, int DP, int DW, int kSplits>
-__global__ void __launch_bounds__(256, 2) at_dq(const Attention a) {
+__global__ void __launch_bounds__(256, kSplits == 4 && DP == 128 ? 1 : 2) at_dq(const Attention a) {
   typedef typename M::T T;
   constexpr int DT = DW / 32, DC = DW / 16;
-  constexpr int kStrips = 4 / kSplits, kRows = 32 * kStrips, NU = 2 / kSplits;
+  constexpr int kKeys = kTileKeys<kSplits>, kStrips = 4 / kSplits, kRows = 32 * kStrips, NU = kKeys / 32 / kSplits;
   constexpr int kTileBytes = kKeys * DP * 2;
   __shared__ __align__(16) char lk0[kTileBytes], lv0[kTileBytes], lk1[kTileBytes], lv1[kTileBytes];
   uint32_t tile, head;
@@ -697,13 +704,14 @@ __global__ void __launch_bounds__(256, 2) at_dq(const Attention a) {
     step(j, lk0, lv0, lk1, lv1);
     if (j + 1 < n_tiles) step(j + 1, lk1, lv1, lk0, lv0);
   }
-  if constexpr (kSplits == 2) {
+  if constexpr (kSplits > 1) {
+    auto place = [&](int i) -> char* { return i == 0 ? lk0 : i == 1 ? lv0 : lk1; };
     __syncthreads();
-    char* part = strip ? lv0 : lk0;
-    if (split) give_columns<DT>(part, acc);
+    if (split) give_columns<DT>(place((split - 1) * kStrips + strip), acc);
     __syncthreads();
     if (split) return;
-    take_columns<DT>(part, acc, 1.0f, 1.0f);
+#pragma unroll
+    for (int x = 0; x < kSplits - 1; ++x) take_columns<DT>(place(x * kStrips + strip), acc, 1.0f, 1.0f);
   }
   if (qi < t.len)
     store_columns<M, DT>(static_cast<T*>(a.dq) + qr * a.dq_s[0] + head * a.dq_s[1], acc, a.scale, width);
@@ -1070,7 +1078,7 @@ int make_attention(const nopfs_attention* p, Attention* a) {
     return fail(NOPFS_EINVAL, "scale must be positive and finite");
   if (p->T >= (int64_t(1) << 31) - 128 || p->n > (1 << 30))
     return fail(NOPFS_ERANGE, "T must be < 2^31 - 128, n <= 2^30");
-  if ((p->T / 64 + p->n + 1) * p->heads >= (int64_t(1) << 31))  // the largest grid
+  if ((p->T / 32 + p->n + 1) * p->heads >= (int64_t(1) << 31))  // the largest grid
     return fail(NOPFS_ERANGE, "too many rows, samples and heads for one call");
   a->T = p->T;
   a->n = p->n;
@@ -1091,11 +1099,18 @@ int make_attention(const nopfs_attention* p, Attention* a) {
   return NOPFS_OK;
 }
 
-// Two splits where one leaves compute units without a second workgroup to
-// overlap with: 5,003 tokens x 6 heads forward 26.2 -> 20.6 us with two, 16,384
-// x 16 heads 99 -> 131.
-constexpr int64_t kSlots = 512;
-bool two_splits(const Attention& a, int32_t heads) { return (a.T / 128 + 1) * heads < kSlots; }
+// Splits of the other side: one where that fills the chip with two workgroups
+// a compute unit, else two (5,003 tokens x 6 heads of 80 forward 26.2 -> 20.6
+// us, 16,384 x 16 of 128 99 -> 131), and four for few, long samples (2,048 x 8
+// of 64 24.3 -> 19.1, 3,000 x 2 of 128 27.0 -> 24.4; 1,000 tokens of four
+// samples x 8 of 128 14.2 -> 17.5), as long as their workgroups run at once:
+// two a compute unit, or one where LDS rows hold 128 elements.
+template <int DP>
+int splits_of(const Attention& a, int32_t heads) {
+  if ((a.T / 128 + 1) * heads >= 512) return 1;
+  const bool few = (a.T / 32 + 1) * heads <= (DP == 64 ? 640 : 320);
+  return few && a.n > 0 && a.T / a.n >= 512 ? 4 : 2;
+}
 
 // An order by cost is worth its launch (4 us) where samples of several tiles
 // differ: 32 documents of 16,384 tokens, forward 127 -> 99 us. A single sample
@@ -1104,19 +1119,18 @@ bool needs_order(const Attention& a) { return a.n > 1 && a.T >= 4096 && a.T / a.
 
 template <class M, int DP, int DW>
 int launch_forward(Attention a, hipStream_t st) {
-  const bool two = two_splits(a, a.heads);
-  const int32_t rows = two ? 64 : 128;
-  const dim3 grid = tile_grid(&a, rows, a.heads);
+  const int splits = splits_of<DP>(a, a.heads);
+  const dim3 grid = tile_grid(&a, 128 / splits, a.heads);
   int rc;
   Scratch sc(st);
   if (needs_order(a)) {
-    OrderJob j{nullptr, a.tiles, rows, true};
+    OrderJob j{nullptr, a.tiles, 128 / splits, true};
     if ((rc = sc.alloc_n(&j.order, a.tiles))) return rc;
     if ((rc = launch("at_order", at_order, dim3(1), dim3(1024), 0, st, a, j, j))) return rc;
     a.order = j.order;
   }
-  return two ? launch("at_forward", at_forward<M, DP, DW, 2>, grid, dim3(256), 0, st, a)
-             : launch("at_forward", at_forward<M, DP, DW, 1>, grid, dim3(256), 0, st, a);
+  const auto kernel = splits == 1 ? at_forward<M, DP, DW, 1> : splits == 2 ? at_forward<M, DP, DW, 2> : at_forward<M, DP, DW, 4>;
+  return launch("at_forward", kernel, grid, dim3(256), 0, st, a);
 }
 
 // Products run over the head's elements rounded up to 32; LDS rows hold 64 or
@@ -1159,6 +1173,7 @@ int attention_impl(const nopfs_attention* p, const void* q, const void* k, const
 // 2 and 330 with 4 (their sums: 8 bytes per element and part, written and read).
 int32_t dkv_parts(const Attention& a) {
   const int32_t group = a.heads / a.kv_heads;
+  if ((a.T / 64 + 1) * group < 16) return 1;  // short anyhow: not worth the launch that adds the parts
   const int64_t want = 65536 / (a.T * a.kv_heads) + 1;
   int32_t parts = 1;
   for (int32_t p = 1; p <= group && p <= want; ++p)
@@ -1168,24 +1183,23 @@ int32_t dkv_parts(const Attention& a) {
 
 template <class M, int DP, int DW>
 int launch_grad(Attention a, hipStream_t st) {
-  const bool two_q = two_splits(a, a.heads);
-  const bool two_k = DP == 128 || two_splits(a, a.kv_heads * a.parts);
+  const int splits = splits_of<DP>(a, a.heads);
+  const bool two_k = DP == 128 || splits_of<DP>(a, a.kv_heads * a.parts) > 1;
   Attention ak = a;
-  const dim3 gq = tile_grid(&a, two_q ? 64 : 128, a.heads);
+  const dim3 gq = tile_grid(&a, 128 / splits, a.heads);
   const dim3 gk = tile_grid(&ak, two_k ? 64 : 128, a.kv_heads * a.parts);
   int rc;
   Scratch sc(st);
   if (needs_order(a)) {
-    OrderJob jq{nullptr, a.tiles, two_q ? 64 : 128, true}, jk{nullptr, ak.tiles, two_k ? 64 : 128, false};
+    OrderJob jq{nullptr, a.tiles, 128 / splits, true}, jk{nullptr, ak.tiles, two_k ? 64 : 128, false};
     if ((rc = sc.alloc_n(&jq.order, a.tiles))) return rc;
     if ((rc = sc.alloc_n(&jk.order, ak.tiles))) return rc;
     if ((rc = launch("at_order", at_order, dim3(2), dim3(1024), 0, st, a, jq, jk))) return rc;
     a.order = jq.order;
     ak.order = jk.order;
   }
-  rc = two_q ? launch("at_dq", at_dq<M, DP, DW, 2>, gq, dim3(256), 0, st, a)
-             : launch("at_dq", at_dq<M, DP, DW, 1>, gq, dim3(256), 0, st, a);
-  if (rc) return rc;
+  const auto dq = splits == 1 ? at_dq<M, DP, DW, 1> : splits == 2 ? at_dq<M, DP, DW, 2> : at_dq<M, DP, DW, 4>;
+  if ((rc = launch("at_dq", dq, gq, dim3(256), 0, st, a))) return rc;
   if constexpr (DP == 128) {
     rc = launch("at_dkv", at_dkv_wide<M, DW>, gk, dim3(256), 0, st, ak);
   } else {

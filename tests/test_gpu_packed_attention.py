@@ -78,6 +78,14 @@ def test_one_sample(length):
     _run_and_check(q, k, v, do, [0, length])
 
 
+@pytest.mark.parametrize("lengths", [[640], [1_111], [2_050, 33], [1_025, 0]])
+@pytest.mark.parametrize("width", [32, 80, 128])
+def test_few_long_samples(lengths, width):
+    """Few workgroups: all four waves share 32 queries."""
+    q, k, v, do = _inputs(lengths, 2, 2, 1, width, FP, sum(lengths))
+    _run_and_check(q, k, v, do, _starts(lengths))
+
+
 @pytest.mark.parametrize("heads,kv_heads", [(1, 1), (3, 1), (6, 2), (8, 1), (5, 5), (16, 4)])
 def test_head_groups(heads, kv_heads):
     lengths = [70, 1, 200]
