@@ -65,9 +65,10 @@ struct Attention {
   void *o, *dq, *dk, *dv;  // o: output of the forward call, input of the gradient
   float* lse;
   float* delta;  // [heads][T] (scratch)
-  // dk, dv: parts of a group's query heads that workgroups of their own sum;
-  // with more than one, their sums [part][dk, dv][T][kv_heads][width] in 32
-  // bits (scratch), added in order afterwards
+  // dk, dv: parts of a key tile's query tiles (of all heads of the group) that
+  // workgroups of their own sum; with more than one, their sums
+  // [part][dk, dv][T][kv_heads][width] in 32 bits (scratch), added in order
+  // afterwards
   int32_t parts;
   float* partial;
   const int32_t* start;
@@ -732,7 +733,7 @@ __global__ void __launch_bounds__(256, 2) at_dkv(const Attention a) {
   __shared__ __align__(16) char lq2[kStages > 2 ? kTileBytes : 1], ld2[kStages > 2 ? kTileBytes : 1];
   uint32_t tile, kv;
   tile_and_head(blockIdx.x, uint32_t(a.kv_heads * a.parts), &tile, &kv);
-  const int head_part = int(kv) % a.parts;  // neighbours: the parts of a kv head
+  const int which = int(kv) % a.parts;  // neighbours: the parts of a kv head
   kv /= uint32_t(a.parts);
   Tile t;
   if (!pick_tile<kRows, false>(a, tile, &t)) return;  // a sample's first keys are seen by most queries
@@ -764,14 +765,17 @@ __global__ void __launch_bounds__(256, 2) at_dkv(const Attention a) {
     for (int e = 0; e < 16; ++e) dk[i][e] = dv[i][e] = 0.0f;
   const float c2 = a.scale * kLog2e, inv_scale = 1.0f / a.scale;
 
-  const int group = a.heads / a.kv_heads / a.parts;  // query heads of this part
-  const int j0 = t.m0 / kQs;  // the first query tile that sees the tile's keys
-  const int j1 = (t.len + kQs - 1) / kQs;
-  const int n_tiles = (j1 - j0) * group;
+  // The key tile's query tiles: from the diagonal to the sample's end, for all
+  // query heads of the group; this part has a run of them.
+  const int group = a.heads / a.kv_heads;
+  const int j0 = t.m0 / kQs, j1 = (t.len + kQs - 1) / kQs;
+  const int64_t all = int64_t(j1 - j0) * group;
+  const int i0 = int(all * which / a.parts), n_tiles = int(all * (which + 1) / a.parts) - i0;
   const TileCopy<DP, kQs> cq(a.q_s[0], width), cd(a.do_s[0], width);
   // the tile copied next: query head and tile of the sample
-  int64_t h_next = (int64_t(kv) * a.parts + head_part) * group;
-  int j_next = j0;
+  int64_t h_next = int64_t(kv) * group + i0 / (j1 - j0);
+  int j_next = j0 + i0 % (j1 - j0);
+  int q0 = j_next * kQs;
   auto copy = [&](char* lq, char* ld, f32x2& stat) {
     const int row0 = j_next * kQs;
     const int64_t at = h_next * a.T + t.begin + min(row0 + lane, t.len - 1);
@@ -794,9 +798,8 @@ __global__ void __launch_bounds__(256, 2) at_dkv(const Attention a) {
     if (kStages > 2) cq.zero_pad(lq2), cd.zero_pad(ld2);
   }
   f32x2 stat0, stat1, stat2;
-  copy(lq0, ld0, stat0);
+  if (n_tiles > 0) copy(lq0, ld0, stat0);
   if (kStages > 2 && n_tiles > 1) copy(lq1, ld1, stat1);
-  int q0 = j0 * kQs;
   auto step = [&](int i, const char* lq, const char* ld, const f32x2& stat, char* next_q, char* next_d,
                   f32x2& next_stat) {
     // tile i is in LDS, and tile i - 1 is done with
@@ -864,7 +867,7 @@ __global__ void __launch_bounds__(256, 2) at_dkv(const Attention a) {
     take_columns<DT>(pk, dk, 1.0f, 1.0f);
     take_columns<DT>(pv, dv, 1.0f, 1.0f);
   }
-  if (ki < t.len) store_dkv<M, DT>(a, kr, kv, head_part, 0, dk, dv);
+  if (ki < t.len) store_dkv<M, DT>(a, kr, kv, which, 0, dk, dv);
 }
 
 // The same for heads of more than 64 elements, where a wave's own rows and
@@ -885,7 +888,7 @@ __global__ void __launch_bounds__(256, 2) at_dkv_wide(const Attention a) {
   __shared__ __align__(16) char lx[4 * 4096];  // P and dS: 4 operands of every wave
   uint32_t tile, kv;
   tile_and_head(blockIdx.x, uint32_t(a.kv_heads * a.parts), &tile, &kv);
-  const int head_part = int(kv) % a.parts;  // neighbours: the parts of a kv head
+  const int which = int(kv) % a.parts;  // neighbours: the parts of a kv head
   kv /= uint32_t(a.parts);
   Tile t;
   if (!pick_tile<kRows, false>(a, tile, &t)) return;
@@ -917,13 +920,14 @@ __global__ void __launch_bounds__(256, 2) at_dkv_wide(const Attention a) {
     for (int e = 0; e < 16; ++e) dk[i][e] = dv[i][e] = 0.0f;
   const float c2 = a.scale * kLog2e, inv_scale = 1.0f / a.scale;
 
-  const int group = a.heads / a.kv_heads / a.parts;
-  const int j0 = t.m0 / kQs;
-  const int j1 = (t.len + kQs - 1) / kQs;
-  const int n_tiles = (j1 - j0) * group;
+  const int group = a.heads / a.kv_heads;
+  const int j0 = t.m0 / kQs, j1 = (t.len + kQs - 1) / kQs;
+  const int64_t all = int64_t(j1 - j0) * group;
+  const int i0 = int(all * which / a.parts), n_tiles = int(all * (which + 1) / a.parts) - i0;
   const TileCopy<DP, kQs> cq(a.q_s[0], width), cd(a.do_s[0], width);
-  int64_t h_next = (int64_t(kv) * a.parts + head_part) * group;
-  int j_next = j0;
+  int64_t h_next = int64_t(kv) * group + i0 / (j1 - j0);
+  int j_next = j0 + i0 % (j1 - j0);
+  int q0 = j_next * kQs;
   auto copy = [&](char* lq, char* ld, f32x2& stat) {
     const int row0 = j_next * kQs;
     const int64_t at = h_next * a.T + t.begin + min(row0 + lane, t.len - 1);
@@ -944,8 +948,7 @@ __global__ void __launch_bounds__(256, 2) at_dkv_wide(const Attention a) {
     cd.zero_pad(ld1);
   }
   f32x2 stat0, stat1;
-  copy(lq0, ld0, stat0);
-  int q0 = j0 * kQs;
+  if (n_tiles > 0) copy(lq0, ld0, stat0);
   V8* const own = reinterpret_cast<V8*>(lx + (2 * strip + part) * 4096) + lane;
   const V8* const others = reinterpret_cast<const V8*>(lx + (2 * strip + 1 - part) * 4096) + lane;
   auto step = [&](int i, const char* lq, const char* ld, const f32x2& stat, char* next_q, char* next_d,
@@ -1016,7 +1019,7 @@ __global__ void __launch_bounds__(256, 2) at_dkv_wide(const Attention a) {
     step(i, lq0, ld0, stat0, lq1, ld1, stat1);
     if (i + 1 < n_tiles) step(i + 1, lq1, ld1, stat1, lq0, ld0, stat0);
   }
-  if (ki < t.len) store_dkv<M, 2>(a, kr, kv, head_part, 64 * part, dk, dv);
+  if (ki < t.len) store_dkv<M, 2>(a, kr, kv, which, 64 * part, dk, dv);
 }
 
 // dk and dv from the parts' sums, four elements a thread.
@@ -1163,22 +1166,22 @@ int attention_impl(const nopfs_attention* p, const void* q, const void* k, const
   return p->dtype == NOPFS_BF16 ? launch_forward<MBf16>(a, st) : launch_forward<MFp16>(a, st);
 }
 
-// Parts of a group's query heads for dk and dv. A key tile's workgroup goes
-// through its sample's later queries of all of them, one after the other: with
-// few key tiles the longest holds up the call. As many parts as make T x
-// kv_heads x parts what brings the longest workgroup near the average load of
-// the chip (samples of like length), if the group divides so: 8,192 tokens, 16
-// query heads on 4, dk and dv 1168 -> 734 us with 2 parts, 2,048 tokens, 8 on
-// 2, 267 -> 83 with 4, 16,384 tokens of 32 documents, 16 on 4, 377 -> 272 with
-// 2 and 330 with 4 (their sums: 8 bytes per element and part, written and read).
+// Parts of a key tile's queries for dk and dv. Its workgroup goes through its
+// sample's later queries of all heads of the group, one tile after the other:
+// with few key tiles, or long ones among short, the longest holds up the call.
+// The lengths are not known here; the longest sample is taken for four times
+// the mean. Parts of 8 tiles or more (the parts' sums cost 8 bytes an element
+// and part, written and read), as many as make two workgroups a compute unit
+// with four times the mean's work, or fill the chip once where all samples are
+// short. 7,825 tokens of three samples x 3 heads: 144 -> 80 us, 5,000 x 4 heads
+// on 1: 151 -> 99, 16,384 tokens of 32 documents x 16 on 4: 311 -> 239; 4,096
+// tokens of 8 like samples x 8 stay whole (35 us, 55 in two parts).
 int32_t dkv_parts(const Attention& a) {
-  const int32_t group = a.heads / a.kv_heads;
-  if ((a.T / 64 + 1) * group < 16) return 1;  // short anyhow: not worth the launch that adds the parts
-  const int64_t want = 65536 / (a.T * a.kv_heads) + 1;
-  int32_t parts = 1;
-  for (int32_t p = 1; p <= group && p <= want; ++p)
-    if (group % p == 0) parts = p;
-  return parts;
+  const int64_t group = a.heads / a.kv_heads, rows = a.T * a.kv_heads;
+  const int64_t longest = a.n > 4 ? 4 * a.T / a.n : a.T;
+  const int64_t want = longest * group >= 4096 ? 65536 / rows + 1 : 32768 / rows;
+  const int64_t most = (longest / 64 + 1) * group / 8;
+  return int32_t(std::max<int64_t>(1, std::min(want, most)));
 }
 
 template <class M, int DP, int DW>

@@ -2,6 +2,7 @@
 #pragma once
 
 #include <limits.h>
+#include <algorithm>
 #include <type_traits>
 #include <math.h>
 
