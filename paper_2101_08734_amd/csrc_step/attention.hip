@@ -722,7 +722,7 @@ __global__ void __launch_bounds__(256, kSplits == 4 && DP == 128 ? 1 : 2) at_dq(
 // One workgroup: 128 keys of one kv head, over the query heads of its group in
 // order and over the query tiles from the diagonal on. Nothing is added to
 // memory from two places, so the sums' order never changes.
-template <class M, int DP, int DW, int kSplits, int kStages>
+template <class M, int DP, int DW, int kSplits>
 __global__ void __launch_bounds__(256, 2) at_dkv(const Attention a) {
   typedef typename M::T T;
   constexpr int DT = DW / 32, DC = DW / 16;
@@ -730,7 +730,6 @@ __global__ void __launch_bounds__(256, 2) at_dkv(const Attention a) {
   constexpr int kTileBytes = kQs * DP * 2;
   // buffers, apart by name so that a read waits for its own buffer's copies only
   __shared__ __align__(16) char lq0[kTileBytes], ld0[kTileBytes], lq1[kTileBytes], ld1[kTileBytes];
-  __shared__ __align__(16) char lq2[kStages > 2 ? kTileBytes : 1], ld2[kStages > 2 ? kTileBytes : 1];
   uint32_t tile, kv;
   tile_and_head(blockIdx.x, uint32_t(a.kv_heads * a.parts), &tile, &kv);
   const int which = int(kv) % a.parts;  // neighbours: the parts of a kv head
@@ -771,6 +770,10 @@ __global__ void __launch_bounds__(256, 2) at_dkv(const Attention a) {
   const int j0 = t.m0 / kQs, j1 = (t.len + kQs - 1) / kQs;
   const int64_t all = int64_t(j1 - j0) * group;
   const int i0 = int(all * which / a.parts), n_tiles = int(all * (which + 1) / a.parts) - i0;
+  if (n_tiles == 0) {  // fewer tiles than parts: this one's sums are 0
+    if (ki < t.len) store_dkv<M, DT>(a, kr, kv, which, 0, dk, dv);
+    return;
+  }
   const TileCopy<DP, kQs> cq(a.q_s[0], width), cd(a.do_s[0], width);
   // the tile copied next: query head and tile of the sample
   int64_t h_next = int64_t(kv) * group + i0 / (j1 - j0);
@@ -789,34 +792,31 @@ __global__ void __launch_bounds__(256, 2) at_dkv(const Attention a) {
       ++h_next;
     }
   };
-  constexpr int kCopies = cq.kPer + cd.kPer + 2;  // of a tile, by each wave
   if (width < DP) {
     cq.zero_pad(lq0);
     cq.zero_pad(lq1);
     cd.zero_pad(ld0);
     cd.zero_pad(ld1);
-    if (kStages > 2) cq.zero_pad(lq2), cd.zero_pad(ld2);
   }
-  f32x2 stat0, stat1, stat2;
-  if (n_tiles > 0) copy(lq0, ld0, stat0);
-  if (kStages > 2 && n_tiles > 1) copy(lq1, ld1, stat1);
+  f32x2 stat0, stat1;
+  copy(lq0, ld0, stat0);
   auto step = [&](int i, const char* lq, const char* ld, const f32x2& stat, char* next_q, char* next_d,
                   f32x2& next_stat) {
-    // tile i is in LDS, and tile i - 1 is done with
-    if (kStages > 2 && i + 1 < n_tiles) meet<kCopies>();
-    else meet<0>();
-    if (i + kStages - 1 < n_tiles) copy(next_q, next_d, next_stat);
+    meet<0>();  // tile i is in LDS, and tile i - 1 is done with
+    if (i + 1 < n_tiles) copy(next_q, next_d, next_stat);
     const int row0 = q0;
     q0 = q0 + kQs < t.len ? q0 + kQs : j0 * kQs;
 #pragma unroll 1
     for (int u = split; u < kQs / 32; u += kSplits) {
       if (row0 + 32 * u < k0) continue;  // all earlier than this wave's keys
+      __builtin_amdgcn_s_setprio(1);
       f32x16 s = minus_rows(stat[0] * inv_scale, u), dp = minus_rows(stat[1], u);
 #pragma unroll
       for (int c = 0; c < DC; ++c) {
         s = M::mma(frag_row<M, DP>(lq, 32 * u, 2 * c), k[c], s);
         dp = M::mma(frag_row<M, DP>(ld, 32 * u, 2 * c), v[c], dp);
       }
+      __builtin_amdgcn_s_setprio(0);
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
         s[r] = exp2_fast(s[r] * c2);
@@ -832,6 +832,7 @@ __global__ void __launch_bounds__(256, 2) at_dkv(const Attention a) {
         for (int r = 0; r < 16; ++r)
           if (row0 + 32 * u + acc_row(r) + 4 * half >= t.len) s[r] = dp[r] = 0.0f;
       }
+      __builtin_amdgcn_s_setprio(1);
 #pragma unroll
       for (int c = 0; c < 2; ++c) {
         const typename M::V8 p = pack8<M>(s, c);
@@ -842,17 +843,12 @@ __global__ void __launch_bounds__(256, 2) at_dkv(const Attention a) {
           dk[x] = M::mma(frag_col<M, DP>(lq, 32 * u + 16 * c, 32 * x), g, dk[x]);
         }
       }
+      __builtin_amdgcn_s_setprio(0);
     }
   };
-  for (int i = 0; i < n_tiles; i += kStages) {
-    if constexpr (kStages == 2) {
-      step(i, lq0, ld0, stat0, lq1, ld1, stat1);
-      if (i + 1 < n_tiles) step(i + 1, lq1, ld1, stat1, lq0, ld0, stat0);
-    } else {
-      step(i, lq0, ld0, stat0, lq2, ld2, stat2);
-      if (i + 1 < n_tiles) step(i + 1, lq1, ld1, stat1, lq0, ld0, stat0);
-      if (i + 2 < n_tiles) step(i + 2, lq2, ld2, stat2, lq1, ld1, stat1);
-    }
+  for (int i = 0; i < n_tiles; i += 2) {
+    step(i, lq0, ld0, stat0, lq1, ld1, stat1);
+    if (i + 1 < n_tiles) step(i + 1, lq1, ld1, stat1, lq0, ld0, stat0);
   }
   if constexpr (kSplits == 2) {
     __syncthreads();
@@ -924,6 +920,10 @@ __global__ void __launch_bounds__(256, 2) at_dkv_wide(const Attention a) {
   const int j0 = t.m0 / kQs, j1 = (t.len + kQs - 1) / kQs;
   const int64_t all = int64_t(j1 - j0) * group;
   const int i0 = int(all * which / a.parts), n_tiles = int(all * (which + 1) / a.parts) - i0;
+  if (n_tiles == 0) {  // fewer tiles than parts: this one's sums are 0
+    if (ki < t.len) store_dkv<M, 2>(a, kr, kv, which, 64 * part, dk, dv);
+    return;
+  }
   const TileCopy<DP, kQs> cq(a.q_s[0], width), cd(a.do_s[0], width);
   int64_t h_next = int64_t(kv) * group + i0 / (j1 - j0);
   int j_next = j0 + i0 % (j1 - j0);
@@ -948,7 +948,7 @@ __global__ void __launch_bounds__(256, 2) at_dkv_wide(const Attention a) {
     cd.zero_pad(ld1);
   }
   f32x2 stat0, stat1;
-  if (n_tiles > 0) copy(lq0, ld0, stat0);
+  copy(lq0, ld0, stat0);
   V8* const own = reinterpret_cast<V8*>(lx + (2 * strip + part) * 4096) + lane;
   const V8* const others = reinterpret_cast<const V8*>(lx + (2 * strip + 1 - part) * 4096) + lane;
   auto step = [&](int i, const char* lq, const char* ld, const f32x2& stat, char* next_q, char* next_d,
@@ -1171,15 +1171,16 @@ int attention_impl(const nopfs_attention* p, const void* q, const void* k, const
 // with few key tiles, or long ones among short, the longest holds up the call.
 // The lengths are not known here; the longest sample is taken for four times
 // the mean. Parts of 8 tiles or more (the parts' sums cost 8 bytes an element
-// and part, written and read), as many as make two workgroups a compute unit
-// with four times the mean's work, or fill the chip once where all samples are
-// short. 7,825 tokens of three samples x 3 heads: 144 -> 80 us, 5,000 x 4 heads
+// and part, written and read), as many as keep the longest workgroup below the
+// chip's average load, with more where lengths differ and fewer where all
+// samples are short. 7,825 tokens of three samples x 3 heads: 144 -> 80 us, 5,000 x 4 heads
 // on 1: 151 -> 99, 16,384 tokens of 32 documents x 16 on 4: 311 -> 239; 4,096
 // tokens of 8 like samples x 8 stay whole (35 us, 55 in two parts).
 int32_t dkv_parts(const Attention& a) {
   const int64_t group = a.heads / a.kv_heads, rows = a.T * a.kv_heads;
   const int64_t longest = a.n > 4 ? 4 * a.T / a.n : a.T;
-  const int64_t want = longest * group >= 4096 ? 65536 / rows + 1 : 32768 / rows;
+  const int64_t load = longest * group < 4096 ? 32768 : a.n > 1 ? 81920 : 65536;
+  const int64_t want = ceil_div(load, rows);
   const int64_t most = (longest / 64 + 1) * group / 8;
   return int32_t(std::max<int64_t>(1, std::min(want, most)));
 }
@@ -1206,8 +1207,8 @@ int launch_grad(Attention a, hipStream_t st) {
   if constexpr (DP == 128) {
     rc = launch("at_dkv", at_dkv_wide<M, DW>, gk, dim3(256), 0, st, ak);
   } else {
-    rc = two_k ? launch("at_dkv", at_dkv<M, DP, DW, 2, 2>, gk, dim3(256), 0, st, ak)
-               : launch("at_dkv", at_dkv<M, DP, DW, 1, 3>, gk, dim3(256), 0, st, ak);
+    rc = two_k ? launch("at_dkv", at_dkv<M, DP, DW, 2>, gk, dim3(256), 0, st, ak)
+               : launch("at_dkv", at_dkv<M, DP, DW, 1>, gk, dim3(256), 0, st, ak);
   }
   if (rc || a.parts == 1) return rc;
   const int64_t blocks = ceil_div(a.T * a.kv_heads * a.width / 4, 256);
