@@ -73,7 +73,7 @@ struct Attention {
   float* partial;
   const int32_t* start;
   uint32_t tiles;  // an upper bound of the row tiles
-  const int2* order;  // the tiles' (sample, first row), costliest first, or NULL
+  const int4* order;  // the tiles' (sample, first row, begin, length), costliest first, or NULL
 };
 
 constexpr float kLog2e = 1.4426950408889634f;
@@ -144,10 +144,9 @@ __device__ inline bool find_tile(const Attention& a, uint32_t tile, Tile* t) {
 template <int BM, bool kLast>
 __device__ __forceinline__ bool pick_tile(const Attention& a, uint32_t rank, Tile* t) {
   if (a.order) {
-    const int2 e = a.order[rank];
-    t->sample = e.x;
-    t->m0 = e.y;
-    return e.x >= 0 && finish_tile(a, t);
+    const int4 e = a.order[rank];
+    *t = Tile{e.x, e.z, e.w, e.y};
+    return e.x >= 0;
   }
   return find_tile<BM>(a, kLast ? a.tiles - 1 - rank : rank, t);
 }
@@ -159,7 +158,7 @@ __device__ __forceinline__ bool pick_tile(const Attention& a, uint32_t rank, Til
 // result depends on it).
 constexpr int kClasses = 1024;
 struct OrderJob {
-  int2* order;
+  int4* order;
   uint32_t tiles;
   int32_t rows;  // of a tile
   bool by_row;
@@ -198,9 +197,9 @@ __global__ void __launch_bounds__(1024) at_order(const Attention a, const OrderJ
   for (uint32_t i = threadIdx.x; i < j.tiles; i += 1024) {
     Tile t;
     const int c = tile(i, &t);
-    if (c >= 0) j.order[atomicAdd(&count[c], 1u)] = int2{t.sample, t.m0};
+    if (c >= 0) j.order[atomicAdd(&count[c], 1u)] = int4{t.sample, t.m0, int32_t(t.begin), t.len};
   }
-  for (uint32_t i = total + threadIdx.x; i < j.tiles; i += 1024) j.order[i] = int2{-1, 0};
+  for (uint32_t i = total + threadIdx.x; i < j.tiles; i += 1024) j.order[i] = int4{-1, 0, 0, 0};
 }
 
 // Workgroup -> (tile, head): all heads of a tile are neighbours, so every die
@@ -1172,10 +1171,10 @@ int attention_impl(const nopfs_attention* p, const void* q, const void* k, const
 // The lengths are not known here; the longest sample is taken for four times
 // the mean. Parts of 8 tiles or more (the parts' sums cost 8 bytes an element
 // and part, written and read), as many as keep the longest workgroup below the
-// chip's average load, with more where lengths differ and fewer where all
-// samples are short. 7,825 tokens of three samples x 3 heads: 144 -> 80 us, 5,000 x 4 heads
-// on 1: 151 -> 99, 16,384 tokens of 32 documents x 16 on 4: 311 -> 239; 4,096
-// tokens of 8 like samples x 8 stay whole (35 us, 55 in two parts).
+// chip's average load, more of them where lengths differ and fewer where all
+// samples are short. 7,825 tokens of three samples x 3 heads: 144 -> 80 us,
+// 5,000 x 4 heads on 1: 151 -> 99, 16,384 tokens of 32 documents x 16 on 4:
+// 311 -> 239; 4,096 tokens of 8 like samples x 8 stay whole (35 us, 55 in two).
 int32_t dkv_parts(const Attention& a) {
   const int64_t group = a.heads / a.kv_heads, rows = a.T * a.kv_heads;
   const int64_t longest = a.n > 4 ? 4 * a.T / a.n : a.T;
