@@ -8,9 +8,14 @@
 //
 // All products are 32x32x16 matrix instructions with 32-bit sums. A wave owns
 // 32 columns (queries in the forward and dq kernels, keys in the dk/dv
-// kernel) and holds its own rows of the operands in registers for the whole
-// pass; tiles of the other side (64 keys, or 32 queries) pass through LDS,
-// double buffered, the next tile's global loads in flight meanwhile.
+// kernels) and holds its own rows of the operands in registers for the whole
+// pass; tiles of the other side (64 rows, or 128 keys) pass through LDS in two
+// buffers, the next tile copied from global memory meanwhile.
+//
+// Where a call has few rows, the other side is split as well: over the waves
+// of a workgroup (splits, joined through LDS) and over workgroups (parts,
+// whose 32-bit sums a small kernel joins in order). Nothing is added to memory
+// from two places, so results never depend on the order of the workgroups.
 //
 // S is computed transposed to its owner: tile[m][n] with n the owned column,
 // so a lane holds 16 of a column's 32 values (its half of the wave the other
@@ -71,6 +76,12 @@ struct Attention {
   // afterwards
   int32_t parts;
   float* partial;
+  // the same of a query tile's keys, for o and dq: sums
+  // [part][T][heads][width], and for o a row's maximum and sum of exponentials
+  // [part][heads][T]
+  int32_t q_parts;
+  float* q_sums;
+  f32x2* q_stats;
   const int32_t* start;
   uint32_t tiles;  // an upper bound of the row tiles
   const int4* order;  // the tiles' (sample, first row, begin, length), costliest first, or NULL
@@ -444,6 +455,14 @@ template <int kSplits>
 constexpr int kTileKeys = kSplits == 4 ? 128 : 64;
 
 // ------------------------------------------------------------------ forward --
+// One pass over the keys up to the diagonal with the running maximum and sum.
+// 16,384 tokens of three samples, 16 heads of 128 on 2: 583 us, 1.02 PFLOP/s of
+// the 1.38 of a large product; matrix units 47% busy, vector units
+// (exponentials, maxima, roundings) 42%, LDS 47%: the phases of a SIMD's two
+// waves overlap in part only. 8,192 x 16 heads of 64: 172
+// us, 0.80 PFLOP/s, vector units 61%: half the products per exponential. 16,384
+// tokens of 32 documents: 105 us, matrix units 28%: the longest documents' last
+// tiles run on when the others are done.
 template <class M, int DP, int DW, int kSplits>
 __global__ void __launch_bounds__(256, kSplits == 4 && DP == 128 ? 1 : 2) at_forward(const Attention a) {
   typedef typename M::T T;
@@ -453,7 +472,9 @@ __global__ void __launch_bounds__(256, kSplits == 4 && DP == 128 ? 1 : 2) at_for
   // two buffers, apart by name so that a read waits for its own buffer's copies only
   __shared__ __align__(16) char lk0[kTileBytes], lv0[kTileBytes], lk1[kTileBytes], lv1[kTileBytes];
   uint32_t tile, head;
-  tile_and_head(blockIdx.x, uint32_t(a.heads), &tile, &head);
+  tile_and_head(blockIdx.x, uint32_t(a.heads * a.q_parts), &tile, &head);
+  const int which = int(head) % a.q_parts;  // neighbours: the parts of a head
+  head /= uint32_t(a.q_parts);
   Tile t;
   // the last tiles of the packed rows first: long samples' last rows see most keys
   if (!pick_tile<kRows, true>(a, tile, &t)) return;
@@ -463,6 +484,7 @@ __global__ void __launch_bounds__(256, kSplits == 4 && DP == 128 ? 1 : 2) at_for
   T* o = static_cast<T*>(a.o) + t.begin * a.o_s[0] + head * a.o_s[1];
   float* lse = a.lse + int64_t(head) * a.T + t.begin;
   if (t.sample == a.n) {
+    if (a.q_parts > 1) return;  // the sum of the parts has these rows
     const int rows = min(kRows, t.len - t.m0);
     zero_rows<M>(a.o, a.o_s, head, t.begin + t.m0, rows, width);
     for (int i = threadIdx.x; i < rows; i += 256) lse[t.m0 + i] = -INFINITY;
@@ -487,18 +509,22 @@ __global__ void __launch_bounds__(256, kSplits == 4 && DP == 128 ? 1 : 2) at_for
   float m = -INFINITY, l = 0.0f;  // l: over the lane's own keys
   const float c2 = a.scale * kLog2e, slack = kSlack / c2;
 
-  const int n_tiles = (min(t.len, t.m0 + kRows) + kKeys - 1) / kKeys;
+  // this part's tiles of those up to the diagonal: j_first .. n_tiles - 1
+  const int64_t all = (min(t.len, t.m0 + kRows) + kKeys - 1) / kKeys;
+  const int j_first = int(all * which / a.q_parts), n_tiles = int(all * (which + 1) / a.q_parts);
   const TileCopy<DP, kKeys> ck(a.k_s[0], width), cv(a.v_s[0], width);
-  const char* kt = reinterpret_cast<const char*>(kb);
-  const char* vt = reinterpret_cast<const char*>(vb);
+  const char* kt = reinterpret_cast<const char*>(kb) + int64_t(ck.stride) * (j_first * kKeys);
+  const char* vt = reinterpret_cast<const char*>(vb) + int64_t(cv.stride) * (j_first * kKeys);
   if (width < DP) {
     ck.zero_pad(lk0);
     ck.zero_pad(lk1);
     cv.zero_pad(lv0);
     cv.zero_pad(lv1);
   }
-  ck.copy(kt, t.len, lk0);
-  cv.copy(vt, t.len, lv0);
+  if (j_first < n_tiles) {
+    ck.copy(kt, t.len - j_first * kKeys, lk0);
+    cv.copy(vt, t.len - j_first * kKeys, lv0);
+  }
   auto step = [&](int j, const char* lk, const char* lv, char* next_k, char* next_v) {
     meet<0>();  // tile j is in LDS, and tile j - 1 is done with
     const int k0 = j * kKeys;
@@ -565,7 +591,7 @@ __global__ void __launch_bounds__(256, kSplits == 4 && DP == 128 ? 1 : 2) at_for
       }
     if constexpr (DP == 128) __builtin_amdgcn_s_setprio(0);
   };
-  for (int j = 0; j < n_tiles; j += 2) {
+  for (int j = j_first; j < n_tiles; j += 2) {
     step(j, lk0, lv0, lk1, lv1);
     if (j + 1 < n_tiles) step(j + 1, lk1, lv1, lk0, lv0);
   }
@@ -586,21 +612,63 @@ __global__ void __launch_bounds__(256, kSplits == 4 && DP == 128 ? 1 : 2) at_for
     for (int x = 0; x < kSplits - 1; ++x) {
       const float* st = stats + 128 * (x * kStrips + strip);
       const float m1 = st[0], top = fmaxf(m, m1);
-      const float f0 = exp2_fast((m - top) * c2), f1 = exp2_fast((m1 - top) * c2);
+      const float base = top == -INFINITY ? 0.0f : top;  // neither has a key yet: factors of 0
+      const float f0 = exp2_fast((m - base) * c2), f1 = exp2_fast((m1 - base) * c2);
       take_columns<DT>(place(x * kStrips + strip), acc, f0, f1);
       l = l * f0 + st[64] * f1;
       m = top;
     }
   }
   l = half_sum(l);
-  if (qi < t.len) {
+  if (qi >= t.len) return;
+  if (a.q_parts == 1) {
     store_columns<M, DT>(o + int64_t(qi) * a.o_s[0], acc, 1.0f / l, width);
     if (half == 0) lse[qi] = m * a.scale + logf(l);
+  } else {
+    const int64_t row = which * a.T + t.begin + qi;
+    store_sums<DT>(a.q_sums + (row * a.heads + head) * width, acc, width);
+    if (half == 0) a.q_stats[(int64_t(which) * a.heads + head) * a.T + t.begin + qi] = f32x2{m, l};
   }
 }
 
+// o and lse from the parts' sums, four elements a thread.
+template <class M>
+__global__ void __launch_bounds__(256) at_join(const Attention a) {
+  const int64_t size = a.T * a.heads * a.width;
+  const int64_t i = (int64_t(blockIdx.x) * 256 + threadIdx.x) * 4;
+  if (i >= size) return;
+  const int64_t rh = i / a.width;
+  const int d = int(i - rh * a.width);
+  const int64_t row = rh / a.heads, head = rh - row * a.heads;
+  f32x4 o = {0, 0, 0, 0};
+  float lse = -INFINITY;
+  if (row < sample_begin(a, a.n)) {
+    const f32x2* st = a.q_stats + head * a.T + row;
+    const int64_t step = a.heads * a.T;
+    float m = -INFINITY, l = 0.0f;
+    for (int p = 0; p < a.q_parts; ++p) m = fmaxf(m, st[p * step][0]);
+    for (int p = 0; p < a.q_parts; ++p) {
+      const f32x2 x = st[p * step];
+      const float f = exp2_fast((x[0] - m) * (a.scale * kLog2e));
+      l += f * x[1];
+      o += f * *reinterpret_cast<const f32x4*>(a.q_sums + p * size + i);
+    }
+    o *= 1.0f / l;
+    lse = m * a.scale + logf(l);
+  }
+  typename M::V4 v;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) v[e] = typename M::T(o[e]);
+  *reinterpret_cast<typename M::V4*>(static_cast<typename M::T*>(a.o) + row * a.o_s[0] + head * a.o_s[1] + d) = v;
+  if (d == 0) a.lse[head * a.T + row] = lse;
+}
+
 // ----------------------------------------------------------------------- dq --
-// Also writes delta_i = do_i.o_i for the dk/dv kernel.
+// P again from S and lse, whose subtraction (and delta's) is the accumulators'
+// start, so no row statistic is needed; also writes delta_i = do_i.o_i for the
+// dk/dv kernels. 8,192 x 16 heads of 64: 210 us, 0.98 PFLOP/s of three
+// products; matrix units 48%, vector units 46%. 16,384 tokens of 32 documents x
+// 16 of 128: 150 us, matrix units 30%, again the longest documents.
 template <class M, int DP, int DW, int kSplits>
 __global__ void __launch_bounds__(256, kSplits == 4 && DP == 128 ? 1 : 2) at_dq(const Attention a) {
   typedef typename M::T T;
@@ -609,14 +677,16 @@ __global__ void __launch_bounds__(256, kSplits == 4 && DP == 128 ? 1 : 2) at_dq(
   constexpr int kTileBytes = kKeys * DP * 2;
   __shared__ __align__(16) char lk0[kTileBytes], lv0[kTileBytes], lk1[kTileBytes], lv1[kTileBytes];
   uint32_t tile, head;
-  tile_and_head(blockIdx.x, uint32_t(a.heads), &tile, &head);
+  tile_and_head(blockIdx.x, uint32_t(a.heads * a.q_parts), &tile, &head);
+  const int which = int(head) % a.q_parts;  // neighbours: the parts of a head
+  head /= uint32_t(a.q_parts);
   Tile t;
   if (!pick_tile<kRows, true>(a, tile, &t)) return;
   const int width = a.width;
   const int wave = __builtin_amdgcn_readfirstlane(int(threadIdx.x >> 6)), lane = threadIdx.x & 63, half = lane >> 5;
   const int strip = wave % kStrips, split = kSplits == 1 ? 0 : wave / kStrips;
   if (t.sample == a.n) {
-    zero_rows<M>(a.dq, a.dq_s, head, t.begin + t.m0, min(kRows, t.len - t.m0), width);
+    if (a.q_parts == 1) zero_rows<M>(a.dq, a.dq_s, head, t.begin + t.m0, min(kRows, t.len - t.m0), width);
     return;
   }
   const int64_t kv = head / (a.heads / a.kv_heads);
@@ -641,7 +711,7 @@ __global__ void __launch_bounds__(256, kSplits == 4 && DP == 128 ? 1 : 2) at_dq(
   delta = half_sum(delta);
   const int64_t stat = int64_t(head) * a.T + qr;
   const float c2 = a.scale * kLog2e, minus_lse = -a.lse[stat] / a.scale;
-  if (half == 0 && split == 0 && qi < t.len) a.delta[stat] = delta;
+  if (half == 0 && split == 0 && which == 0 && qi < t.len) a.delta[stat] = delta;
 
   f32x16 acc[DT];
 #pragma unroll
@@ -649,18 +719,22 @@ __global__ void __launch_bounds__(256, kSplits == 4 && DP == 128 ? 1 : 2) at_dq(
 #pragma unroll
     for (int e = 0; e < 16; ++e) acc[i][e] = 0.0f;
 
-  const int n_tiles = (min(t.len, t.m0 + kRows) + kKeys - 1) / kKeys;
+  // this part's tiles of those up to the diagonal: j_first .. n_tiles - 1
+  const int64_t all = (min(t.len, t.m0 + kRows) + kKeys - 1) / kKeys;
+  const int j_first = int(all * which / a.q_parts), n_tiles = int(all * (which + 1) / a.q_parts);
   const TileCopy<DP, kKeys> ck(a.k_s[0], width), cv(a.v_s[0], width);
-  const char* kt = reinterpret_cast<const char*>(kb);
-  const char* vt = reinterpret_cast<const char*>(vb);
+  const char* kt = reinterpret_cast<const char*>(kb) + int64_t(ck.stride) * (j_first * kKeys);
+  const char* vt = reinterpret_cast<const char*>(vb) + int64_t(cv.stride) * (j_first * kKeys);
   if (width < DP) {
     ck.zero_pad(lk0);
     ck.zero_pad(lk1);
     cv.zero_pad(lv0);
     cv.zero_pad(lv1);
   }
-  ck.copy(kt, t.len, lk0);
-  cv.copy(vt, t.len, lv0);
+  if (j_first < n_tiles) {
+    ck.copy(kt, t.len - j_first * kKeys, lk0);
+    cv.copy(vt, t.len - j_first * kKeys, lv0);
+  }
   auto step = [&](int j, const char* lk, const char* lv, char* next_k, char* next_v) {
     meet<0>();
     const int k0 = j * kKeys;
@@ -700,7 +774,7 @@ __global__ void __launch_bounds__(256, kSplits == 4 && DP == 128 ? 1 : 2) at_dq(
       }
     }
   };
-  for (int j = 0; j < n_tiles; j += 2) {
+  for (int j = j_first; j < n_tiles; j += 2) {
     step(j, lk0, lv0, lk1, lv1);
     if (j + 1 < n_tiles) step(j + 1, lk1, lv1, lk0, lv0);
   }
@@ -713,14 +787,18 @@ __global__ void __launch_bounds__(256, kSplits == 4 && DP == 128 ? 1 : 2) at_dq(
 #pragma unroll
     for (int x = 0; x < kSplits - 1; ++x) take_columns<DT>(place(x * kStrips + strip), acc, 1.0f, 1.0f);
   }
-  if (qi < t.len)
+  if (qi >= t.len) return;
+  if (a.q_parts == 1)
     store_columns<M, DT>(static_cast<T*>(a.dq) + qr * a.dq_s[0] + head * a.dq_s[1], acc, a.scale, width);
+  else
+    store_sums<DT>(a.q_sums + ((which * a.T + qr) * a.heads + head) * width, acc, width);
 }
 
 // -------------------------------------------------------------------- dk, dv --
-// One workgroup: 128 keys of one kv head, over the query heads of its group in
-// order and over the query tiles from the diagonal on. Nothing is added to
-// memory from two places, so the sums' order never changes.
+// One workgroup: 128 keys (64 with two splits) of one kv head, over the query
+// heads of its group in order and the query tiles from the diagonal on, or over
+// one part of that list. Four products a block of 32 x 32: 8,192 x 16 heads of
+// 64 303 us, 0.91 PFLOP/s; matrix units 43%, vector units 46%.
 template <class M, int DP, int DW, int kSplits>
 __global__ void __launch_bounds__(256, 2) at_dkv(const Attention a) {
   typedef typename M::T T;
@@ -872,7 +950,9 @@ __global__ void __launch_bounds__(256, 2) at_dkv(const Attention a) {
 // hands them to the other through LDS (as the operands they are, 16 bytes a
 // lane), and then sums one half of the head's elements over all 64: half the
 // sums per wave, and two workgroups share a compute unit. Their LDS is exactly
-// half of it, so lse and delta stay in registers, one row per lane.
+// half of it, so lse and delta stay in registers, one row per lane. 8,192 x 16
+// heads of 128: 600 us, 0.92 PFLOP/s (876 with a strip per wave); the meeting
+// of the waves between the two phases is what it waits for.
 template <class M, int DW>
 __global__ void __launch_bounds__(256, 2) at_dkv_wide(const Attention a) {
   typedef typename M::T T;
@@ -1021,30 +1101,35 @@ __global__ void __launch_bounds__(256, 2) at_dkv_wide(const Attention a) {
   if (ki < t.len) store_dkv<M, 2>(a, kr, kv, which, 64 * part, dk, dv);
 }
 
-// dk and dv from the parts' sums, four elements a thread.
+// Gradients from their parts' sums, four elements a thread: element i of
+// [T][heads][width], the parts `stride` apart.
+template <class M>
+__device__ __forceinline__ void sum_parts(const Attention& a, const float* sums, int64_t stride, int parts, int64_t i,
+                                          int heads, void* to, const int64_t* s, float f) {
+  const int64_t rh = i / a.width;
+  const int d = int(i - rh * a.width);
+  const int64_t row = rh / heads, head = rh - row * heads;
+  f32x4 x = {0, 0, 0, 0};
+  if (row < sample_begin(a, a.n))
+    for (int p = 0; p < parts; ++p) x += *reinterpret_cast<const f32x4*>(sums + p * stride + i);
+  typename M::V4 v;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) v[e] = typename M::T(x[e] * f);
+  *reinterpret_cast<typename M::V4*>(static_cast<typename M::T*>(to) + row * s[0] + head * s[1] + d) = v;
+}
 template <class M>
 __global__ void __launch_bounds__(256) at_sum(const Attention a) {
   const int64_t size = a.T * a.kv_heads * a.width;
   const int64_t i = (int64_t(blockIdx.x) * 256 + threadIdx.x) * 4;
   if (i >= size) return;
-  const int64_t rk = i / a.width;
-  const int d = int(i - rk * a.width);
-  const int64_t row = rk / a.kv_heads, kv = rk - row * a.kv_heads;
-  f32x4 dk = {0, 0, 0, 0}, dv = {0, 0, 0, 0};
-  if (row < sample_begin(a, a.n))
-    for (int p = 0; p < a.parts; ++p) {
-      dk += *reinterpret_cast<const f32x4*>(a.partial + 2 * p * size + i);
-      dv += *reinterpret_cast<const f32x4*>(a.partial + (2 * p + 1) * size + i);
-    }
-  typedef typename M::T T;
-  typename M::V4 k, v;
-#pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    k[e] = T(dk[e] * a.scale);
-    v[e] = T(dv[e]);
-  }
-  *reinterpret_cast<typename M::V4*>(static_cast<T*>(a.dk) + row * a.dk_s[0] + kv * a.dk_s[1] + d) = k;
-  *reinterpret_cast<typename M::V4*>(static_cast<T*>(a.dv) + row * a.dv_s[0] + kv * a.dv_s[1] + d) = v;
+  sum_parts<M>(a, a.partial, 2 * size, a.parts, i, a.kv_heads, a.dk, a.dk_s, a.scale);
+  sum_parts<M>(a, a.partial + size, 2 * size, a.parts, i, a.kv_heads, a.dv, a.dv_s, 1.0f);
+}
+template <class M>
+__global__ void __launch_bounds__(256) at_sum_dq(const Attention a) {
+  const int64_t size = a.T * a.heads * a.width;
+  const int64_t i = (int64_t(blockIdx.x) * 256 + threadIdx.x) * 4;
+  if (i < size) sum_parts<M>(a, a.q_sums, size, a.q_parts, i, a.heads, a.dq, a.dq_s, a.scale);
 }
 
 // --------------------------------------------------------------------- host --
@@ -1066,6 +1151,9 @@ dim3 tile_grid(Attention* a, int rows, int32_t heads) {
   a->tiles = uint32_t(a->T / rows + a->n + 1);
   return dim3(a->tiles * uint32_t(heads));
 }
+
+// The grid over [T][heads][width], 4 elements a thread.
+dim3 sum_grid(const Attention& a, int32_t heads) { return dim3(uint32_t(ceil_div(a.T * heads * a.width / 4, 256))); }
 
 int make_attention(const nopfs_attention* p, Attention* a) {
   if (!p) return fail(NOPFS_EINVAL, "attention is NULL");
@@ -1119,10 +1207,25 @@ int splits_of(const Attention& a, int32_t heads) {
 // is in order by itself, and samples below a tile all cost the same.
 bool needs_order(const Attention& a) { return a.n > 1 && a.T >= 4096 && a.T / a.n >= 64; }
 
+// Parts of a query tile's keys for o and dq, where few rows and heads leave the
+// longest sample's last tiles alone on the chip (its length guessed as in
+// dkv_parts): 24 key tiles or more a part, since a launch that joins them
+// follows (6 to 20 us). Forward and dq, joined: 7,825 tokens of three samples x
+// 3 heads of 80 147 -> 105 us, 5,000 x 4 of 128 160 -> 130, 16,000 x 2 of 64
+// 306 -> 236; like samples, for which the guess is too long, lose a little: three
+// of 2,048 x 8 of 128 103 -> 134, four 114 -> 135. In parts of 12 tiles 4,096
+// tokens of 8 samples x 8 of 128 took 78 for 46.
+int32_t q_parts(const Attention& a) {
+  const int64_t rows = a.T * a.heads;
+  const int64_t longest = a.n > 4 ? 4 * a.T / a.n : a.T;
+  const int64_t most = (longest / 64 + 1) / 24;
+  return int32_t(std::max<int64_t>(1, std::min(ceil_div(81920, rows), most)));
+}
+
 template <class M, int DP, int DW>
 int launch_forward(Attention a, hipStream_t st) {
-  const int splits = splits_of<DP>(a, a.heads);
-  const dim3 grid = tile_grid(&a, 128 / splits, a.heads);
+  const int splits = splits_of<DP>(a, a.heads * a.q_parts);
+  const dim3 grid = tile_grid(&a, 128 / splits, a.heads * a.q_parts);
   int rc;
   Scratch sc(st);
   if (needs_order(a)) {
@@ -1131,8 +1234,14 @@ int launch_forward(Attention a, hipStream_t st) {
     if ((rc = launch("at_order", at_order, dim3(1), dim3(1024), 0, st, a, j, j))) return rc;
     a.order = j.order;
   }
+  if (a.q_parts > 1) {
+    if ((rc = sc.alloc_n(&a.q_sums, size_t(a.q_parts) * size_t(a.T) * size_t(a.heads) * size_t(a.width)))) return rc;
+    if ((rc = sc.alloc_n(&a.q_stats, size_t(a.q_parts) * size_t(a.T) * size_t(a.heads)))) return rc;
+  }
   const auto kernel = splits == 1 ? at_forward<M, DP, DW, 1> : splits == 2 ? at_forward<M, DP, DW, 2> : at_forward<M, DP, DW, 4>;
-  return launch("at_forward", kernel, grid, dim3(256), 0, st, a);
+  rc = launch("at_forward", kernel, grid, dim3(256), 0, st, a);
+  if (rc || a.q_parts == 1) return rc;
+  return launch("at_join", at_join<M>, sum_grid(a, a.heads), dim3(256), 0, st, a);
 }
 
 // Products run over the head's elements rounded up to 32; LDS rows hold 64 or
@@ -1162,6 +1271,7 @@ int attention_impl(const nopfs_attention* p, const void* q, const void* k, const
   a.o = o;
   a.lse = lse;
   a.start = start;
+  a.q_parts = q_parts(a);
   return p->dtype == NOPFS_BF16 ? launch_forward<MBf16>(a, st) : launch_forward<MFp16>(a, st);
 }
 
@@ -1186,10 +1296,10 @@ int32_t dkv_parts(const Attention& a) {
 
 template <class M, int DP, int DW>
 int launch_grad(Attention a, hipStream_t st) {
-  const int splits = splits_of<DP>(a, a.heads);
+  const int splits = splits_of<DP>(a, a.heads * a.q_parts);
   const bool two_k = DP == 128 || splits_of<DP>(a, a.kv_heads * a.parts) > 1;
   Attention ak = a;
-  const dim3 gq = tile_grid(&a, 128 / splits, a.heads);
+  const dim3 gq = tile_grid(&a, 128 / splits, a.heads * a.q_parts);
   const dim3 gk = tile_grid(&ak, two_k ? 64 : 128, a.kv_heads * a.parts);
   int rc;
   Scratch sc(st);
@@ -1203,6 +1313,9 @@ int launch_grad(Attention a, hipStream_t st) {
   }
   const auto dq = splits == 1 ? at_dq<M, DP, DW, 1> : splits == 2 ? at_dq<M, DP, DW, 2> : at_dq<M, DP, DW, 4>;
   if ((rc = launch("at_dq", dq, gq, dim3(256), 0, st, a))) return rc;
+  if (a.q_parts > 1 &&
+      (rc = launch("at_sum_dq", at_sum_dq<M>, sum_grid(a, a.heads), dim3(256), 0, st, a)))
+    return rc;
   if constexpr (DP == 128) {
     rc = launch("at_dkv", at_dkv_wide<M, DW>, gk, dim3(256), 0, st, ak);
   } else {
@@ -1210,8 +1323,7 @@ int launch_grad(Attention a, hipStream_t st) {
                : launch("at_dkv", at_dkv<M, DP, DW, 1>, gk, dim3(256), 0, st, ak);
   }
   if (rc || a.parts == 1) return rc;
-  const int64_t blocks = ceil_div(a.T * a.kv_heads * a.width / 4, 256);
-  return launch("at_sum", at_sum<M>, dim3(uint32_t(blocks)), dim3(256), 0, st, ak);
+  return launch("at_sum", at_sum<M>, sum_grid(a, a.kv_heads), dim3(256), 0, st, ak);
 }
 
 template <class M>
@@ -1250,6 +1362,10 @@ int attention_grad_impl(const nopfs_attention* p, const void* d_o, const void* q
   a.start = start;
   Scratch sc(st);
   if ((rc = sc.alloc_n(&a.delta, size_t(a.heads) * size_t(a.T)))) return rc;
+  a.q_parts = q_parts(a);
+  if (a.q_parts > 1 &&
+      (rc = sc.alloc_n(&a.q_sums, size_t(a.q_parts) * size_t(a.T) * size_t(a.heads) * size_t(a.width))))
+    return rc;
   a.parts = dkv_parts(a);
   if (a.parts > 1 &&
       (rc = sc.alloc_n(&a.partial, size_t(2 * a.parts) * size_t(a.T) * size_t(a.kv_heads) * size_t(a.width))))

@@ -86,6 +86,26 @@ def test_few_long_samples(lengths, width):
     _run_and_check(q, k, v, do, _starts(lengths))
 
 
+@pytest.mark.parametrize("lengths,tail,heads,kv_heads,width,dtype", [
+    ([3_200], 0, 1, 1, 32, BF),
+    ([3_137, 1], 70, 2, 1, 64, FP),
+    ([1, 4_700, 0, 5], 3, 3, 1, 80, BF),
+    ([2_600, 2_222], 0, 6, 2, 128, FP),
+    ([5_000], 33, 6, 6, 64, BF),
+    ([4_900, 63, 0, 1, 1_500, 128, 65, 2, 900, 300, 31, 1_800], 110, 2, 2, 128, BF),
+])
+def test_parts_of_the_keys(lengths, tail, heads, kv_heads, width, dtype):
+    """Few, long samples: several workgroups share a query tile's keys, and
+    tiles of few keys leave some of them without any."""
+    q, k, v, do = _inputs(lengths, tail, heads, kv_heads, width, dtype, sum(lengths))
+    start = _starts(lengths)
+    o, lse, dq, dk, dv = _run_and_check(q, k, v, do, start)
+    again = torch.tensor(start, dtype=torch.int32, device="cuda")
+    o2, lse2 = nopfs.packed_attention(q, k, v, again)
+    for a, b in zip((o, lse, dq, dk, dv), (o2, lse2, *nopfs.packed_attention_grad(do, q, k, v, o2, lse2, again))):
+        assert torch.equal(a, b)
+
+
 @pytest.mark.parametrize("heads,kv_heads", [(1, 1), (3, 1), (6, 2), (8, 1), (5, 5), (16, 4)])
 def test_head_groups(heads, kv_heads):
     lengths = [70, 1, 200]
