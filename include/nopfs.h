@@ -378,7 +378,7 @@ typedef struct nopfs_batch {
   int64_t F;           /* samples (entries of `tokens` when ids is given)   */
   int64_t ids_stride;  /* elements from a group's reads to the next group's */
   int64_t free_stride; /* elements from a group's free list to the next's   */
-  int32_t G, n;        /* groups, reads of each; >= 1, n <= 2^30            */
+  int32_t G, n;        /* groups, reads of each; >= 1, G < 2^22, n <= 2^30  */
   int32_t blocks;      /* free blocks of each group, >= 0                   */
   int32_t block;       /* tokens per block, >= 1                            */
   int32_t width;       /* blocks a read may take (columns of `table`), >= 1 */

@@ -154,6 +154,7 @@ __device__ inline bool find_tile(const Attention& a, uint32_t tile, Tile* t) {
 // packed, from the last (kLast) or from the first.
 template <int BM, bool kLast>
 __device__ __forceinline__ bool pick_tile(const Attention& a, uint32_t rank, Tile* t) {
+  if (rank >= a.tiles) return false;
   if (a.order) {
     const int4 e = a.order[rank];
     *t = Tile{e.x, e.z, e.w, e.y};
@@ -472,7 +473,7 @@ __global__ void __launch_bounds__(256, kSplits == 4 && DP == 128 ? 1 : 2) at_for
   // two buffers, apart by name so that a read waits for its own buffer's copies only
   __shared__ __align__(16) char lk0[kTileBytes], lv0[kTileBytes], lk1[kTileBytes], lv1[kTileBytes];
   uint32_t tile, head;
-  tile_and_head(blockIdx.x, uint32_t(a.heads * a.q_parts), &tile, &head);
+  tile_and_head(row_block(), uint32_t(a.heads * a.q_parts), &tile, &head);
   const int which = int(head) % a.q_parts;  // neighbours: the parts of a head
   head /= uint32_t(a.q_parts);
   Tile t;
@@ -677,7 +678,7 @@ __global__ void __launch_bounds__(256, kSplits == 4 && DP == 128 ? 1 : 2) at_dq(
   constexpr int kTileBytes = kKeys * DP * 2;
   __shared__ __align__(16) char lk0[kTileBytes], lv0[kTileBytes], lk1[kTileBytes], lv1[kTileBytes];
   uint32_t tile, head;
-  tile_and_head(blockIdx.x, uint32_t(a.heads * a.q_parts), &tile, &head);
+  tile_and_head(row_block(), uint32_t(a.heads * a.q_parts), &tile, &head);
   const int which = int(head) % a.q_parts;  // neighbours: the parts of a head
   head /= uint32_t(a.q_parts);
   Tile t;
@@ -808,7 +809,7 @@ __global__ void __launch_bounds__(256, 2) at_dkv(const Attention a) {
   // buffers, apart by name so that a read waits for its own buffer's copies only
   __shared__ __align__(16) char lq0[kTileBytes], ld0[kTileBytes], lq1[kTileBytes], ld1[kTileBytes];
   uint32_t tile, kv;
-  tile_and_head(blockIdx.x, uint32_t(a.kv_heads * a.parts), &tile, &kv);
+  tile_and_head(row_block(), uint32_t(a.kv_heads * a.parts), &tile, &kv);
   const int which = int(kv) % a.parts;  // neighbours: the parts of a kv head
   kv /= uint32_t(a.parts);
   Tile t;
@@ -962,7 +963,7 @@ __global__ void __launch_bounds__(256, 2) at_dkv_wide(const Attention a) {
   __shared__ __align__(16) char lq0[kTileBytes], ld0[kTileBytes], lq1[kTileBytes], ld1[kTileBytes];
   __shared__ __align__(16) char lx[4 * 4096];  // P and dS: 4 operands of every wave
   uint32_t tile, kv;
-  tile_and_head(blockIdx.x, uint32_t(a.kv_heads * a.parts), &tile, &kv);
+  tile_and_head(row_block(), uint32_t(a.kv_heads * a.parts), &tile, &kv);
   const int which = int(kv) % a.parts;  // neighbours: the parts of a kv head
   kv /= uint32_t(a.parts);
   Tile t;
@@ -1149,7 +1150,7 @@ int check_array(const char* name, const void* p, const int64_t* s, int64_t heads
 // Row tiles of `rows` rows at most, and the grid over them and the heads.
 dim3 tile_grid(Attention* a, int rows, int32_t heads) {
   a->tiles = uint32_t(a->T / rows + a->n + 1);
-  return dim3(a->tiles * uint32_t(heads));
+  return row_grid(int64_t(a->tiles) * heads);
 }
 
 // The grid over [T][heads][width], 4 elements a thread.

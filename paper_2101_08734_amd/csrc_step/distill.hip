@@ -161,7 +161,8 @@ __global__ void __launch_bounds__(kThreads) td_row(const Distill d) {
   __shared__ int s_any;
   extern __shared__ float lds[];  // 4 K
   const Entries en{lds, lds + d.K, lds + 2 * d.K, reinterpret_cast<int32_t*>(lds + 3 * d.K)};
-  const int64_t t = blockIdx.x;
+  const int64_t t = row_block();
+  if (t >= d.T) return;
   const int tid = threadIdx.x;
   const T* s = static_cast<const T*>(d.logits) + t * d.logits_stride;
   T* ds = d.grad ? static_cast<T*>(d.grad) + t * d.grad_stride : nullptr;
@@ -289,7 +290,7 @@ __global__ void __launch_bounds__(kThreads) td_row(const Distill d) {
 
 template <class E, class Y, int kThreads, int kHold>
 int launch_row(const Distill& d, hipStream_t st) {
-  return launch("td_row", td_row<E, Y, kThreads, kHold>, dim3(uint32_t(d.T)), dim3(kThreads), size_t(d.K) * 16, st,
+  return launch("td_row", td_row<E, Y, kThreads, kHold>, row_grid(d.T), dim3(kThreads), size_t(d.K) * 16, st,
                 d);
 }
 

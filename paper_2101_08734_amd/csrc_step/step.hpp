@@ -27,4 +27,12 @@ struct Fp32 {
   static constexpr int kBits = 24;
 };
 
+// A launch counts its threads in 32 bits per dimension (2^22 workgroups of 1024):
+// `blocks` workgroups in rows of 2^20, and a workgroup's number among them (the
+// last row's may pass `blocks`).
+inline dim3 row_grid(int64_t blocks) {
+  return dim3(uint32_t(std::min<int64_t>(blocks, 1 << 20)), uint32_t(ceil_div(blocks, 1 << 20)));
+}
+__device__ __forceinline__ uint32_t row_block() { return blockIdx.y << 20 | blockIdx.x; }
+
 }  // namespace nopfs

@@ -351,8 +351,8 @@ int batch_tables_impl(const nopfs_batch* p, const int32_t* ids, const int32_t* t
   const bool small = p->G * (tok_tiles + tab_tiles) < kSmallTiles;
   if (small) tok_tiles = small_tok, tab_tiles = small_tab;
   const int64_t tiles = int64_t(p->G) * (tok_tiles + tab_tiles);
-  if (tiles >= int64_t(INT32_MAX))
-    return fail(NOPFS_ERANGE, "too many table entries and packed tokens for one call");
+  if (tiles >= int64_t(1) << 24 || p->G >= 1 << 22)  // a launch has fewer than 2^32 threads
+    return fail(NOPFS_ERANGE, "too many workers, table entries and packed tokens for one call");
   Batch b{p->F, p->ids_stride, p->free_stride, p->G, p->n, p->blocks, p->block, p->width, p->cap,
           ids, tokens, free_list, start, table, slot, row, pos, used, nullptr};
   const Divider by_block(p->block);

@@ -129,6 +129,23 @@ def test_many_short_samples(n):
     _run_and_check(q, k, v, do, _starts(lengths))
 
 
+@pytest.mark.parametrize("n", [2**20 + 70, 2**23 + 9])
+def test_more_workgroups_than_one_launch_dimension_holds(n):
+    """Samples of no token, and a few of some: two heads make 2^24 workgroups of
+    256 threads."""
+    at = {5: 40, 2**20 - 3: 1, 2**20 + 60: 130, n - 1: 33}
+    lengths = torch.zeros(n, dtype=torch.int64)
+    for i, x in at.items():
+        lengths[i] = x
+    start = torch.cat([torch.zeros(1, dtype=torch.int64), lengths.cumsum(0)]).to(torch.int32).cuda()
+    q, k, v, do = _inputs(list(at.values()), 3, 2, 1, 64, BF, 13)
+    o, lse = nopfs.packed_attention(q, k, v, start)
+    grads = nopfs.packed_attention_grad(do, q, k, v, o, lse, start)
+    val, err = step_ref.attention(q, k, v, _starts(list(at.values())), 64**-0.5, do)
+    for name, t in zip(("o", "lse", "dq", "dk", "dv"), (o, lse, *grads)):
+        _close(name, t, val[name], err[name])
+
+
 @pytest.mark.parametrize("width", [64, 128])
 @pytest.mark.parametrize("kv_heads", [200, 520])
 def test_many_heads(width, kv_heads):

@@ -189,3 +189,16 @@ def test_gradient_against_differences():
         f0 = nopfs.topk_distill(down, index, y, tau, weight=w, grad=False)[0].double()
         diff = (f1 - f0) / step
         assert float((diff - ds[:, v].double()).abs().max()) <= h * h / tau + 2.0**-17 / h
+
+
+def test_more_rows_than_one_launch_dimension_holds():
+    """2^26 workgroups of 64 threads are 2^32 threads."""
+    T = 2**26 + 5
+    s, index, y, w = _inputs(64, 8, 1, BF, BF, 7)
+
+    def rows(x):
+        return x[:61].repeat(T // 61 + 1, *[1] * (x.dim() - 1))[:T]
+
+    loss, ds = nopfs.topk_distill(rows(s), rows(index), rows(y), 1.0, weight=rows(w))
+    one, grad = nopfs.topk_distill(s[:61], index[:61], y[:61], 1.0, weight=w[:61])
+    assert torch.equal(loss, rows(one)) and torch.equal(ds, rows(grad))

@@ -43,6 +43,12 @@ def test_batch_refusals(L, kw, code):
     assert L.nopfs_last_error()
 
 
+@pytest.mark.parametrize("kw", [dict(G=2**22), dict(G=2**20, cap=2**20)])
+def test_batch_launch_limits(L, kw):
+    """A launch has fewer than 2^32 threads."""
+    assert _tables(L, _batch(**kw)) == ERANGE
+
+
 def test_batch_null_pointers(L):
     assert _tables(L, None) == EINVAL
     for name in BATCH_ARGS[1:]:
