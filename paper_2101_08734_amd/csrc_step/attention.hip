@@ -164,38 +164,48 @@ __device__ __forceinline__ bool pick_tile(const Attention& a, uint32_t rank, Til
 }
 
 // Orders the tiles by what they cost, so that the longest work starts first:
-// by their first row (a query tile sees the keys up to itself, kByRow), or by
+// by their first row (a query tile sees the keys up to itself, by_row), or by
 // the rows from there to the sample's end (a key tile). A counting sort by one
 // workgroup; which of two tiles of one class comes first is left open (no
-// result depends on it).
-constexpr int kClasses = 1024;
+// result depends on it). Bound by the latency of its searches: the starts are
+// in LDS where they fit (16,384 tokens of 32 samples: 9.2 -> 6.5 us,
+// launch included).
+constexpr int kClasses = 1024, kHeldStarts = 4096;
 struct OrderJob {
   int4* order;
   uint32_t tiles;
-  int32_t rows;  // of a tile
+  int32_t log_rows;  // of a tile
   bool by_row;
 };
 __global__ void __launch_bounds__(1024) at_order(const Attention a, const OrderJob j0, const OrderJob j1) {
   __shared__ uint32_t count[kClasses];
   __shared__ uint32_t tmp[65];
+  __shared__ int32_t starts[kHeldStarts];
   const OrderJob& j = blockIdx.x == 0 ? j0 : j1;
+  const bool held = a.n < kHeldStarts;
+  if (held)
+    for (int32_t s = threadIdx.x; s <= a.n; s += 1024) starts[s] = int32_t(sample_begin(a, s));
   int shift = 0;
-  while ((a.T / j.rows) >> shift >= kClasses) ++shift;
+  while (a.T >> j.log_rows >> shift >= kClasses) ++shift;
   count[threadIdx.x] = 0;
+  __syncthreads();
+  auto begin = [&](int32_t s) { return held ? starts[s] : int32_t(sample_begin(a, s)); };
+  auto number = [&](int32_t s) { return (begin(s) >> j.log_rows) + s; };  // < 2^31
   auto tile = [&](uint32_t i, Tile* t) {
     int32_t lo = 0, hi = a.n;
     while (hi > lo) {
       const int32_t mid = lo + (hi - lo + 1) / 2;
-      if (sample_begin(a, mid) / j.rows + mid <= int64_t(i)) lo = mid;
+      if (uint32_t(number(mid)) <= i) lo = mid;
       else hi = mid - 1;
     }
     t->sample = lo;
-    t->m0 = int32_t((int64_t(i) - (sample_begin(a, lo) / j.rows + lo)) * j.rows);
-    if (!finish_tile(a, t)) return -1;
-    const int cost = (j.by_row ? t->m0 : t->len - t->m0 - 1) / j.rows;
+    t->begin = begin(lo);
+    t->len = (lo < a.n ? begin(lo + 1) : int32_t(a.T)) - int32_t(t->begin);
+    t->m0 = (int32_t(i) - number(lo)) << j.log_rows;
+    if (t->m0 < 0 || t->m0 >= t->len) return -1;
+    const int cost = (j.by_row ? t->m0 : t->len - t->m0 - 1) >> j.log_rows;
     return kClasses - 1 - min(lo == a.n ? 0 : cost >> shift, kClasses - 1);
   };
-  __syncthreads();
   for (uint32_t i = threadIdx.x; i < j.tiles; i += 1024) {
     Tile t;
     const int c = tile(i, &t);
@@ -1230,7 +1240,7 @@ int launch_forward(Attention a, hipStream_t st) {
   int rc;
   Scratch sc(st);
   if (needs_order(a)) {
-    OrderJob j{nullptr, a.tiles, 128 / splits, true};
+    OrderJob j{nullptr, a.tiles, __builtin_ctz(128 / splits), true};
     if ((rc = sc.alloc_n(&j.order, a.tiles))) return rc;
     if ((rc = launch("at_order", at_order, dim3(1), dim3(1024), 0, st, a, j, j))) return rc;
     a.order = j.order;
@@ -1305,7 +1315,7 @@ int launch_grad(Attention a, hipStream_t st) {
   int rc;
   Scratch sc(st);
   if (needs_order(a)) {
-    OrderJob jq{nullptr, a.tiles, 128 / splits, true}, jk{nullptr, ak.tiles, two_k ? 64 : 128, false};
+    OrderJob jq{nullptr, a.tiles, __builtin_ctz(128 / splits), true}, jk{nullptr, ak.tiles, two_k ? 6 : 7, false};
     if ((rc = sc.alloc_n(&jq.order, a.tiles))) return rc;
     if ((rc = sc.alloc_n(&jk.order, ak.tiles))) return rc;
     if ((rc = launch("at_order", at_order, dim3(2), dim3(1024), 0, st, a, jq, jk))) return rc;
