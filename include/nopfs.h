@@ -415,7 +415,7 @@ typedef struct nopfs_attention {
   int32_t kv_heads;    /* query head h reads kv head h div (heads/kv_heads)  */
   int32_t width;       /* elements of a head: a multiple of 8, 8..128        */
   int32_t dtype;       /* NOPFS_BF16 or NOPFS_FP16                           */
-  float scale;         /* of the products q.k, positive and finite           */
+  float scale;         /* of the products q.k, 2^-60 .. 2^60                 */
   int64_t q_stride[2], k_stride[2], v_stride[2], o_stride[2];
   int64_t do_stride[2], dq_stride[2], dk_stride[2], dv_stride[2]; /* gradient only */
 } nopfs_attention;
@@ -457,7 +457,7 @@ typedef struct nopfs_distill {
   int32_t K;              /* teacher entries per row, 1..1024                 */
   int32_t dtype;          /* of logits and grad                               */
   int32_t teacher_dtype;
-  float tau;              /* temperature, positive and finite                 */
+  float tau;              /* temperature, 2^-60 .. 2^60                       */
 } nopfs_distill;
 
 /* Loss and gradient. With p the softmax of teacher / tau over a row's valid

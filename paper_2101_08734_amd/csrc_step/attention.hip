@@ -1177,6 +1177,8 @@ int make_attention(const nopfs_attention* p, Attention* a) {
   if (p->width > 128) return fail(NOPFS_ERANGE, "width must be <= 128");
   if (!(p->scale > 0.0f) || !isfinite(p->scale))
     return fail(NOPFS_EINVAL, "scale must be positive and finite");
+  // 1 / scale and the rows' lse in units of it stay finite
+  if (p->scale < 0x1p-60f || p->scale > 0x1p60f) return fail(NOPFS_ERANGE, "scale must be in 2^-60 .. 2^60");
   if (p->T >= (int64_t(1) << 31) - 128 || p->n > (1 << 30))
     return fail(NOPFS_ERANGE, "T must be < 2^31 - 128, n <= 2^30");
   if ((p->T / 32 + p->n + 1) * p->heads >= (int64_t(1) << 31))  // the largest grid

@@ -332,6 +332,8 @@ int distill_impl(const nopfs_distill* p, const void* logits, const int32_t* inde
       p->teacher_dtype > NOPFS_FP32)
     return fail(NOPFS_EINVAL, "unknown dtype");
   if (!(p->tau > 0.0f) || !isfinite(p->tau)) return fail(NOPFS_EINVAL, "tau must be positive and finite");
+  if (p->tau < 0x1p-60f || p->tau > 0x1p60f)  // tau^2 and 1 / tau stay finite
+    return fail(NOPFS_ERANGE, "tau must be in 2^-60 .. 2^60");
   if (p->T > 1 && (p->logits_stride < p->V || p->index_stride < p->K || p->teacher_stride < p->K ||
                    (grad && p->grad_stride < p->V)))
     return fail(NOPFS_EINVAL, "rows overlap");

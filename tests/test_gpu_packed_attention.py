@@ -213,6 +213,12 @@ def test_flat_and_steep_rows(spread):
     _run_and_check(q, k, v, do, _starts(lengths), scale=0.37)
 
 
+@pytest.mark.parametrize("scale", [2.0**-60, 2.0**-30, 3.0])
+def test_small_and_large_scales(scale):
+    q, k, v, do = _inputs([200, 1, 70], 0, 2, 1, 64, BF, 14)
+    _run_and_check(q, k, v, do, [0, 200, 201, 271], scale=scale)
+
+
 def test_scores_that_grow_along_the_keys():
     """The running maximum moves in every tile."""
     T = 700

@@ -169,3 +169,9 @@ def test_host_tensors_are_refused():
         nopfs.batch_tables(None, start[None], start[None], 4, 4, 4)
     with pytest.raises(TypeError):
         nopfs.topk_distill(q[0], start[None], q[0], 1.0)
+
+
+@pytest.mark.parametrize("x", [2.0**-61, 2.0**61, 1e-40])
+def test_scales_and_temperatures_out_of_range(L, x):
+    assert _forward(L, _attention(scale=x)) == ERANGE and _grad(L, _attention(scale=x)) == ERANGE
+    assert _loss(L, _distill(tau=x)) == ERANGE
