@@ -441,7 +441,9 @@ int nopfs_packed_attention(const nopfs_attention* a, const void* q, const void* 
  *   dq_i = scale sum_j dS_ij k_j,
  *   dk_j = scale sum over the query heads of the group and i of dS_ij q_i,
  *   dv_j = the same sum of P_ij do_i.
- * Rows from start[n] on get 0. Errors: EINVAL, ERANGE, ENOMEM, EDEVICE. */
+ * Rows from start[n] on get 0. A NaN or infinity of a row may reach, as 0 times
+ * it, dq of up to 31 rows before it and dk and dv of up to 31 after it in its
+ * sample, which do not depend on it. Errors: EINVAL, ERANGE, ENOMEM, EDEVICE. */
 int nopfs_packed_attention_grad(const nopfs_attention* a, const void* d_o, const void* q,
                                 const void* k, const void* v, const void* o, const float* lse,
                                 const int32_t* start, void* dq, void* dk, void* dv,

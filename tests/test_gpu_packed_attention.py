@@ -249,6 +249,31 @@ def test_outputs_into_slices_and_layouts():
     assert bool((wide[:, :, 64:] == 5.0).all())
 
 
+@pytest.mark.parametrize("token,head", [(2**23, 72), (72, 2**31 + 8)])
+def test_offsets_past_32_bits(token, head):
+    """Rows or heads so far apart that byte offsets pass 2^32."""
+    lengths = [250, 7, 40]
+    q, k, v, do = _inputs(lengths, 5, 2, 1, 64, BF, 15)
+    start = torch.tensor(_starts(lengths), dtype=torch.int32, device="cuda")
+    o, lse = nopfs.packed_attention(q, k, v, start)
+    grads = nopfs.packed_attention_grad(do, q, k, v, o, lse, start)
+    T = q.shape[0]
+
+    def far(x):
+        size = (T - 1) * token + (x.shape[1] - 1) * head + 64
+        y = torch.empty(size, dtype=BF, device="cuda").as_strided(x.shape, (token, head, 1))
+        return y.copy_(x)
+
+    fq, fk, fv, fdo, fo = far(q), far(k), far(v), far(do), far(torch.zeros_like(o))
+    out, stat = nopfs.packed_attention(fq, fk, fv, start, o=fo)
+    assert torch.equal(out, o) and torch.equal(stat, lse)
+    far_grads = [far(torch.zeros_like(g)) for g in grads]
+    nopfs.packed_attention_grad(fdo, fq, fk, fv, fo, stat, start,
+                                **dict(zip(("dq", "dk", "dv"), far_grads)))
+    for a, b in zip(far_grads, grads):
+        assert torch.equal(a, b)
+
+
 def test_same_bits_again_and_on_another_stream():
     lengths = [500, 3, 260]
     q, k, v, do = _inputs(lengths, 9, 6, 2, 128, FP, 8)
@@ -275,6 +300,33 @@ def test_in_a_graph():
     grads = nopfs.packed_attention_grad(do, q, k, v, o, lse, start)
     s = torch.cuda.Stream()
     nopfs.packed_attention_grad(do, q, k, v, o, lse, start, stream=s)  # its scratch
+    s.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=s):
+        go, gl = nopfs.packed_attention(q, k, v, start, stream=s)
+        gg = nopfs.packed_attention_grad(do, q, k, v, go, gl, start, stream=s)
+    for i in range(3):
+        for t in (go, gl, *gg):
+            t.fill_(3.0)
+        q.mul_(-1.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        o, lse = nopfs.packed_attention(q, k, v, start)
+        grads = nopfs.packed_attention_grad(do, q, k, v, o, lse, start)
+        torch.cuda.synchronize()
+        for a, b in zip((o, lse, *grads), (go, gl, *gg)):
+            assert torch.equal(a, b), i
+
+
+def test_parts_in_a_graph():
+    """Parts of the keys and of the queries: partial sums in the stream's scratch."""
+    lengths = [3_300, 900]
+    q, k, v, do = _inputs(lengths, 20, 2, 1, 64, BF, 16)
+    start = torch.tensor(_starts(lengths), dtype=torch.int32, device="cuda")
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    o, lse = nopfs.packed_attention(q, k, v, start, stream=s)  # the stream's scratch
+    nopfs.packed_attention_grad(do, q, k, v, o, lse, start, stream=s)
     s.synchronize()
     graph = torch.cuda.CUDAGraph()
     with torch.cuda.graph(graph, stream=s):

@@ -202,3 +202,14 @@ def test_more_rows_than_one_launch_dimension_holds():
     loss, ds = nopfs.topk_distill(rows(s), rows(index), rows(y), 1.0, weight=rows(w))
     one, grad = nopfs.topk_distill(s[:61], index[:61], y[:61], 1.0, weight=w[:61])
     assert torch.equal(loss, rows(one)) and torch.equal(ds, rows(grad))
+
+
+def test_offsets_past_32_bits():
+    """Rows so far apart that byte offsets pass 2^32."""
+    T, V, stride = 36, 700, 2**26 + 8
+    s, index, y, w = _inputs(T, V, 9, BF, FP, 8)
+    one, grad = nopfs.topk_distill(s, index, y, 1.0, weight=w)
+    far = torch.empty((T - 1) * stride + V, dtype=BF, device="cuda").as_strided((T, V), (stride, 1))
+    far.copy_(s)
+    loss, ds = nopfs.topk_distill(far, index, y, 1.0, weight=w, dlogits=far)
+    assert torch.equal(loss, one) and torch.equal(ds, grad)
