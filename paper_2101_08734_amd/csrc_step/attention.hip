@@ -677,9 +677,14 @@ __global__ void __launch_bounds__(256) at_join(const Attention a) {
 // ----------------------------------------------------------------------- dq --
 // P again from S and lse, whose subtraction (and delta's) is the accumulators'
 // start, so no row statistic is needed; also writes delta_i = do_i.o_i for the
-// dk/dv kernels. 8,192 x 16 heads of 64: 210 us, 0.98 PFLOP/s of three
-// products; matrix units 48%, vector units 46%. 16,384 tokens of 32 documents x
-// 16 of 128: 150 us, matrix units 30%, again the longest documents.
+// dk/dv kernels. A sample's first rows see few keys: there o's rounding, times
+// do, is not small beside dP - delta (two tokens of bf16: dq off by 0.0054
+// relative, by 0.0025 now), so a sample's first tile takes sum_j P_ij dP_ij,
+// delta before o was rounded, from a pass of its own over its keys (no more
+// than 1 us at 300 to 16,384 tokens). 8,192 x 16 heads of 64: 210 us, 0.98
+// PFLOP/s of three products; matrix units 48%, vector units 46%. 16,384 tokens
+// of 32 documents x 16 of 128: 150 us, matrix units 30%, again the longest
+// documents.
 template <class M, int DP, int DW, int kSplits>
 __global__ void __launch_bounds__(256, kSplits == 4 && DP == 128 ? 1 : 2) at_dq(const Attention a) {
   typedef typename M::T T;
@@ -722,13 +727,6 @@ __global__ void __launch_bounds__(256, kSplits == 4 && DP == 128 ? 1 : 2) at_dq(
   delta = half_sum(delta);
   const int64_t stat = int64_t(head) * a.T + qr;
   const float c2 = a.scale * kLog2e, minus_lse = -a.lse[stat] / a.scale;
-  if (half == 0 && split == 0 && which == 0 && qi < t.len) a.delta[stat] = delta;
-
-  f32x16 acc[DT];
-#pragma unroll
-  for (int i = 0; i < DT; ++i)
-#pragma unroll
-    for (int e = 0; e < 16; ++e) acc[i][e] = 0.0f;
 
   // this part's tiles of those up to the diagonal: j_first .. n_tiles - 1
   const int64_t all = (min(t.len, t.m0 + kRows) + kKeys - 1) / kKeys;
@@ -742,10 +740,50 @@ __global__ void __launch_bounds__(256, kSplits == 4 && DP == 128 ? 1 : 2) at_dq(
     cv.zero_pad(lv0);
     cv.zero_pad(lv1);
   }
-  if (j_first < n_tiles) {
+  if (t.m0 == 0) {
+    static_assert(kRows <= 2 * kKeys);  // the first tile's keys are in the two buffers
+    ck.copy(reinterpret_cast<const char*>(kb), t.len, lk0);
+    cv.copy(reinterpret_cast<const char*>(vb), t.len, lv0);
+    if (kRows > kKeys && t.len > kKeys) {
+      ck.copy(reinterpret_cast<const char*>(kb) + int64_t(ck.stride) * kKeys, t.len - kKeys, lk1);
+      cv.copy(reinterpret_cast<const char*>(vb) + int64_t(cv.stride) * kKeys, t.len - kKeys, lv1);
+    }
+    meet<0>();
+    delta = 0.0f;
+#pragma unroll 1
+    for (int k0 = 0; k0 <= q0 && k0 < t.len; k0 += 32) {
+      const char* lk = k0 < kKeys ? lk0 : lk1;
+      const char* lv = k0 < kKeys ? lv0 : lv1;
+      f32x16 s, dp;
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        s[e] = minus_lse;
+        dp[e] = 0.0f;
+      }
+#pragma unroll
+      for (int c = 0; c < DC; ++c) {
+        s = M::mma(frag_row<M, DP>(lk, k0 % kKeys, 2 * c), q[c], s);
+        dp = M::mma(frag_row<M, DP>(lv, k0 % kKeys, 2 * c), d[c], dp);
+      }
+#pragma unroll
+      for (int e = 0; e < 16; ++e)
+        if (k0 + acc_row(e) + 4 * half <= qi) delta += exp2_fast(s[e] * c2) * dp[e];
+    }
+    delta = half_sum(delta);
+    if (j_first > 0) __syncthreads();  // the buffers are free again
+  }
+  if (half == 0 && split == 0 && which == 0 && qi < t.len) a.delta[stat] = delta;
+  if ((t.m0 > 0 || j_first > 0) && j_first < n_tiles) {
     ck.copy(kt, t.len - j_first * kKeys, lk0);
     cv.copy(vt, t.len - j_first * kKeys, lv0);
   }
+
+  f32x16 acc[DT];
+#pragma unroll
+  for (int i = 0; i < DT; ++i)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) acc[i][e] = 0.0f;
+
   auto step = [&](int j, const char* lk, const char* lv, char* next_k, char* next_v) {
     meet<0>();
     const int k0 = j * kKeys;

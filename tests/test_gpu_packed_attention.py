@@ -219,6 +219,35 @@ def test_small_and_large_scales(scale):
     _run_and_check(q, k, v, do, [0, 200, 201, 271], scale=scale)
 
 
+@pytest.mark.parametrize("dtype", [BF, FP], ids=["bf16", "fp16"])
+@pytest.mark.parametrize("lengths,heads", [([2] * 40 + [1, 0] + [3] * 20, 3), ([2, 3, 2, 4], 300)])
+@pytest.mark.parametrize("width", [32, 80, 128])
+def test_short_samples_do_not_feel_the_rounding_of_o(lengths, heads, width, dtype):
+    """dS and dq are rounded to the inputs' type, of unit u (half the spacing over
+    the least value that has it): each rounding is off by u / sqrt(3) of its value
+    at most in the mean square, all of them independent. delta from the rounded o
+    would add to all dS of a row together, where dP - delta is small."""
+    q, k, v, do = _inputs(lengths, 0, heads, heads, width, dtype, 17)
+    start = _starts(lengths)
+    st = torch.tensor(start, dtype=torch.int32, device="cuda")
+    o, lse = nopfs.packed_attention(q, k, v, st)
+    dq = nopfs.packed_attention_grad(do, q, k, v, o, lse, st)[0]
+    u, scale = (2.0**-8 if dtype == BF else 2.0**-11), width**-0.5
+    off = allowed = 0.0
+    for a, b in zip(start, start[1:]):
+        if a == b:
+            continue
+        qi, ki, vi, di = (x[a:b].double().transpose(0, 1).contiguous() for x in (q, k, v, do))
+        seen = torch.ones(b - a, b - a, dtype=torch.bool, device="cuda").tril()
+        s = torch.where(seen, qi @ ki.transpose(1, 2).contiguous() * scale, -math.inf)
+        p, dp = torch.softmax(s, 2), di @ vi.transpose(1, 2).contiguous()
+        ds = p * (dp - (p * dp).sum(2, keepdim=True))
+        want = ds @ ki * scale
+        off += float(((dq[a:b].double().transpose(0, 1) - want) ** 2).sum())
+        allowed += float((ds**2 @ ki**2).sum() * scale**2 + (want**2).sum()) * u**2 / 3
+    assert off <= allowed
+
+
 def test_scores_that_grow_along_the_keys():
     """The running maximum moves in every tile."""
     T = 700
