@@ -26,6 +26,14 @@
  *    nopfs_scratch_release (or the end of the process): at most the largest
  *    call's scratch per stream. Calls on one stream from several host
  *    threads are enqueued one at a time.
+ *  - Graph capture: a call on a stream that is being captured allocates
+ *    nothing. It takes its scratch from the stream's block, and is refused
+ *    with ENOMEM where that has no room (make the call once before the
+ *    capture). The graph holds the block's address: a block that a captured
+ *    call used is kept when a larger one replaces it, until
+ *    nopfs_scratch_release, after which the graph must not be replayed. Graphs
+ *    captured on one stream share its block with each other and with that
+ *    stream's calls: the caller orders their replays.
  *  - Host waits: a GPU call returns without waiting for the device, except
  *    a call that outgrows its stream's block (the first call of a larger job
  *    on a stream, or the first after nopfs_scratch_release), which
@@ -507,8 +515,8 @@ int nopfs_calibration_copy(const void* src, void* dst, int64_t bytes,
 
 /* Returns the scratch block of (current device, hip_stream) to the device:
  * waits for the work enqueued on the stream (hipStreamSynchronize), then
- * frees the block (hipFree). The next call on that stream allocates a new
- * one. A call being enqueued on the stream from another host thread
+ * frees the block, and earlier ones that captured calls used (hipFree). The
+ * next call on that stream allocates a new one. A call being enqueued on the stream from another host thread
  * finishes first. Nothing to release is not an error. Errors: EDEVICE. */
 int nopfs_scratch_release(void* hip_stream);
 

@@ -67,7 +67,10 @@ bool take_alloc_failure() { return g_debug[3] > 0 && --g_debug[3] == 0; }
 // stream-ordered allocations of gigabytes stalled the host for hundreds of
 // milliseconds per call after ~100 calls (the allocator returned and mapped
 // memory again); the arena keeps its memory until nopfs_scratch_release or
-// the end of the process.
+// the end of the process. A call on a stream that is being captured allocates
+// nothing: its block has the room or it is refused. The graph holds the
+// block's address from then on, so a block that a capture used is not freed
+// when a larger one takes its place.
 struct Arena {
   std::recursive_mutex mu;
   bool fixed = false;       // a fixed block that never grows (no allocation)
@@ -79,12 +82,23 @@ struct Arena {
   size_t peak = 0;          // largest extent of the current call
   size_t peak_total = 0;    // largest extent of any call (sizing passes)
   bool failed = false;      // an allocation of the current call failed
+  bool captured = false;    // a captured call used `block`
   std::vector<void*> extra; // blocks beyond `block`, freed at the call's end
+  std::vector<void*> kept;  // earlier blocks that captured calls used
   struct Rec {
     size_t off, bytes;
     bool in_block, live;
   };
   std::vector<Rec> stack;
+
+  // Notes a block that a captured call used; false for any other block.
+  bool keep_block() noexcept {
+    try {
+      if (captured) kept.push_back(block);
+    } catch (...) {  // no host memory for the note: the block stays all the same
+    }
+    return captured;
+  }
 };
 
 static std::mutex g_arenas_mu;
@@ -193,9 +207,10 @@ Scratch::~Scratch() {
       for (void* q : a->extra) (void)hipFree(q);
       a->extra.clear();
       if (!a->failed) {
-        if (a->block) (void)hipFree(a->block);
+        if (a->block && !a->keep_block()) (void)hipFree(a->block);
         a->block = nullptr;
         a->cap = 0;
+        a->captured = false;
         void* q = nullptr;
         if (hipMalloc(&q, a->peak) == hipSuccess && q) {
           a->block = static_cast<char*>(q);
@@ -208,6 +223,16 @@ Scratch::~Scratch() {
     a->failed = false;
   }
   a->mu.unlock();
+}
+
+bool Scratch::capturing() {
+  if (!asked_) {
+    hipStreamCaptureStatus status = hipStreamCaptureStatusNone;
+    if (!sizing_only() && hipStreamIsCapturing(stream_, &status) != hipSuccess) (void)hipGetLastError();
+    capturing_ = status != hipStreamCaptureStatusNone;
+    asked_ = true;
+  }
+  return capturing_;
 }
 
 int Scratch::alloc(void** p, size_t bytes) {
@@ -227,9 +252,14 @@ int Scratch::alloc(void** p, size_t bytes) {
     r.in_block = true;
     a->top += bytes;
     *p = a->block + r.off;
+    if (!a->fixed && capturing()) a->captured = true;
   } else if (a->fixed) {
     return fail(NOPFS_ENOMEM, std::string("scratch of ") + std::to_string(a->top + bytes) +
                                   " bytes exceeds the fixed block of " + std::to_string(a->cap));
+  } else if (capturing()) {
+    a->failed = true;
+    return fail(NOPFS_ENOMEM, std::string("the stream is being captured and its scratch block has no room for ") +
+                                  std::to_string(bytes) + " bytes: make the call once before the capture");
   } else {
     void* q = nullptr;
     const hipError_t e = hipMalloc(&q, bytes);
@@ -253,11 +283,7 @@ bool Scratch::try_alloc(void** p, size_t bytes) {
   *p = nullptr;
   Arena* a = arena_;
   if (!a) return false;
-  if (a->top + ((bytes + 255) & ~size_t(255)) > a->cap) {
-    hipStreamCaptureStatus capture = hipStreamCaptureStatusNone;
-    if (hipStreamIsCapturing(stream_, &capture) != hipSuccess) (void)hipGetLastError();
-    if (capture != hipStreamCaptureStatusNone) return false;
-  }
+  if (a->top + ((bytes + 255) & ~size_t(255)) > a->cap && !a->fixed && capturing()) return false;
   const bool failed = a->failed;
   const std::string detail = g_last_error;
   if (alloc(p, bytes) == NOPFS_OK) return true;
@@ -409,12 +435,17 @@ int nopfs_scratch_release(void* hip_stream) {
     if (!a) return NOPFS_OK;  // no block on this stream
     std::lock_guard<std::recursive_mutex> g(a->mu);  // waits for a call being enqueued
     if (a->depth != 0) return fail(NOPFS_EINVAL, "scratch release from inside a call");
-    if (!a->block) return NOPFS_OK;
+    if (!a->block && a->kept.empty()) return NOPFS_OK;
     NOPFS_HIP(hipStreamSynchronize(s));
-    NOPFS_HIP(hipFree(a->block));
+    while (!a->kept.empty()) {
+      NOPFS_HIP(hipFree(a->kept.back()));
+      a->kept.pop_back();
+    }
+    if (a->block) NOPFS_HIP(hipFree(a->block));
     a->block = nullptr;
     a->cap = 0;
     a->top = 0;
+    a->captured = false;
     return NOPFS_OK;
   } catch (...) {
     return fail(NOPFS_EDEVICE, "unexpected host exception");

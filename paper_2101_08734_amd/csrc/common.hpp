@@ -63,7 +63,8 @@ class Scratch {
   ~Scratch();
   Scratch(const Scratch&) = delete;
   Scratch& operator=(const Scratch&) = delete;
-  // Allocates `bytes` (rounded up to 256) and returns NOPFS_OK or ENOMEM.
+  // Allocates `bytes` (rounded up to 256) and returns NOPFS_OK or ENOMEM (also
+  // where the stream is being captured and its block has no room).
   int alloc(void** p, size_t bytes);
   template <typename T>
   int alloc_n(T** p, size_t n) { return alloc(reinterpret_cast<void**>(p), n * sizeof(T)); }
@@ -76,7 +77,9 @@ class Scratch {
 
  private:
   bool try_alloc(void** p, size_t bytes);
+  bool capturing();  // the stream, when first asked
   hipStream_t stream_;
+  bool asked_ = false, capturing_ = false;
   struct Arena* arena_ = nullptr;
   size_t recs_[32] = {};  // this object's entries on the arena's stack
   int n_ = 0;
