@@ -373,7 +373,13 @@ int nopfs_policy_sim(const nopfs_job* job, const int32_t* R, const int64_t* size
  * every token, attention over the packed samples, and the loss against
  * teacher logits stored with the samples. These follow the conventions above;
  * results of 16- and 32-bit arithmetic are rounded, and the same from call to
- * call (no sum depends on the order in which work finishes). */
+ * call (no sum depends on the order in which work finishes).
+ * Scratch is the stream's block, or what the caller gives in `scratch`: at
+ * least the bytes that the call's _scratch function tells for the same sizes
+ * and strides (0: none is needed; ENOMEM where it is too small), not touched by
+ * others until the call's work has completed. In a graph capture a call that needs
+ * scratch has to be given it (else EINVAL): the graph writes there whenever it
+ * is replayed. */
 
 /* Element types. */
 #define NOPFS_BF16 0
@@ -391,6 +397,8 @@ typedef struct nopfs_batch {
   int32_t block;       /* tokens per block, >= 1                            */
   int32_t width;       /* blocks a read may take (columns of `table`), >= 1 */
   int32_t cap;         /* packed tokens a group may hold, 0 <= cap <= 2^30  */
+  void* scratch;         /* the call's scratch, a multiple of 256 bytes, or   */
+  int64_t scratch_bytes; /* NULL; its size                                    */
 } nopfs_batch;
 
 /* Block tables and slot maps from the lengths of the next reads. Read r of
@@ -411,6 +419,8 @@ typedef struct nopfs_batch {
 int nopfs_batch_tables(const nopfs_batch* batch, const int32_t* ids, const int32_t* tokens,
                        const int32_t* free_blocks, int32_t* start, int32_t* table, int64_t* slot,
                        int32_t* row, int32_t* pos, int32_t* used, void* hip_stream);
+/* Its scratch, on the host. Errors: EINVAL, ERANGE. */
+int nopfs_batch_tables_scratch(const nopfs_batch* batch, int64_t* bytes);
 
 /* Causal attention over n packed samples of different lengths. Strides are in
  * elements: [0] from token to token, [1] from head to head; the `width`
@@ -426,6 +436,8 @@ typedef struct nopfs_attention {
   float scale;         /* of the products q.k, 2^-60 .. 2^60                 */
   int64_t q_stride[2], k_stride[2], v_stride[2], o_stride[2];
   int64_t do_stride[2], dq_stride[2], dk_stride[2], dv_stride[2]; /* gradient only */
+  void* scratch;         /* the call's scratch, a multiple of 256 bytes, or    */
+  int64_t scratch_bytes; /* NULL; its size                                     */
 } nopfs_attention;
 
 /* Forward. Sample s holds tokens start[s]..start[s+1]-1; a token sees its own
@@ -456,6 +468,9 @@ int nopfs_packed_attention_grad(const nopfs_attention* a, const void* d_o, const
                                 const void* k, const void* v, const void* o, const float* lse,
                                 const int32_t* start, void* dq, void* dk, void* dv,
                                 void* hip_stream);
+/* The scratch of the forward call, or of the gradient, on the host. Errors:
+ * EINVAL, ERANGE. */
+int nopfs_packed_attention_scratch(const nopfs_attention* a, int32_t gradient, int64_t* bytes);
 
 /* Distillation from a teacher's K top logits per row. */
 typedef struct nopfs_distill {

@@ -182,6 +182,23 @@ int run_in_fixed_block(char* block, size_t cap, const std::function<int()>& call
   return rc;
 }
 
+int run_in_caller_block(void* block, size_t cap, const std::function<int()>& call) {
+  Arena a;
+  a.fixed = true;
+  a.block = static_cast<char*>(block);
+  a.cap = cap;
+  Arena* prev = t_fixed_arena;
+  t_fixed_arena = &a;
+  int rc;
+  try {
+    rc = call();
+  } catch (...) {
+    rc = fail(NOPFS_EDEVICE, "unexpected host exception");
+  }
+  t_fixed_arena = prev;
+  return rc;
+}
+
 Scratch::Scratch(hipStream_t s) : stream_(s), arena_(t_fixed_arena ? t_fixed_arena : arena_of(s)) {
   if (!arena_) return;
   arena_->mu.lock();
@@ -234,6 +251,8 @@ bool Scratch::capturing() {
   }
   return capturing_;
 }
+
+bool Scratch::shared_in_capture() { return arena_ && !arena_->fixed && capturing(); }
 
 int Scratch::alloc(void** p, size_t bytes) {
   *p = nullptr;

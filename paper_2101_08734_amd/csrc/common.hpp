@@ -74,6 +74,9 @@ class Scratch {
   // grows to what the call did get.
   template <typename T>
   bool try_alloc_n(T** p, size_t n) { return try_alloc(reinterpret_cast<void**>(p), n * sizeof(T)); }
+  // Whether a buffer would come from the stream's block into a graph that is
+  // being captured there.
+  bool shared_in_capture();
 
  private:
   bool try_alloc(void** p, size_t bytes);
@@ -94,6 +97,8 @@ int run_sizing(const std::function<int()>& call, size_t* peak);
 // block [block, block + cap), which never grows: a call that needs more
 // fails with ENOMEM. Calls on one block are enqueued one at a time.
 int run_in_fixed_block(char* block, size_t cap, const std::function<int()>& call);
+// The same with a block that the caller gives with the call, and orders.
+int run_in_caller_block(void* block, size_t cap, const std::function<int()>& call);
 // True inside run_sizing on this thread.
 bool sizing_only();
 

@@ -1279,15 +1279,16 @@ int launch_forward(Attention a, hipStream_t st) {
   const dim3 grid = tile_grid(&a, 128 / splits, a.heads * a.q_parts);
   int rc;
   Scratch sc(st);
+  if (a.q_parts > 1) {
+    if ((rc = step_alloc(&sc, &a.q_sums, size_t(a.q_parts) * size_t(a.T) * size_t(a.heads) * size_t(a.width))))
+      return rc;
+    if ((rc = step_alloc(&sc, &a.q_stats, size_t(a.q_parts) * size_t(a.T) * size_t(a.heads)))) return rc;
+  }
   if (needs_order(a)) {
     OrderJob j{nullptr, a.tiles, __builtin_ctz(128 / splits), true};
-    if ((rc = sc.alloc_n(&j.order, a.tiles))) return rc;
+    if ((rc = step_alloc(&sc, &j.order, a.tiles))) return rc;
     if ((rc = launch("at_order", at_order, dim3(1), dim3(1024), 0, st, a, j, j))) return rc;
     a.order = j.order;
-  }
-  if (a.q_parts > 1) {
-    if ((rc = sc.alloc_n(&a.q_sums, size_t(a.q_parts) * size_t(a.T) * size_t(a.heads) * size_t(a.width)))) return rc;
-    if ((rc = sc.alloc_n(&a.q_stats, size_t(a.q_parts) * size_t(a.T) * size_t(a.heads)))) return rc;
   }
   const auto kernel = splits == 1 ? at_forward<M, DP, DW, 1> : splits == 2 ? at_forward<M, DP, DW, 2> : at_forward<M, DP, DW, 4>;
   rc = launch("at_forward", kernel, grid, dim3(256), 0, st, a);
@@ -1356,8 +1357,8 @@ int launch_grad(Attention a, hipStream_t st) {
   Scratch sc(st);
   if (needs_order(a)) {
     OrderJob jq{nullptr, a.tiles, __builtin_ctz(128 / splits), true}, jk{nullptr, ak.tiles, two_k ? 6 : 7, false};
-    if ((rc = sc.alloc_n(&jq.order, a.tiles))) return rc;
-    if ((rc = sc.alloc_n(&jk.order, ak.tiles))) return rc;
+    if ((rc = step_alloc(&sc, &jq.order, a.tiles))) return rc;
+    if ((rc = step_alloc(&sc, &jk.order, ak.tiles))) return rc;
     if ((rc = launch("at_order", at_order, dim3(2), dim3(1024), 0, st, a, jq, jk))) return rc;
     a.order = jq.order;
     ak.order = jk.order;
@@ -1412,14 +1413,14 @@ int attention_grad_impl(const nopfs_attention* p, const void* d_o, const void* q
   a.dv = dv;
   a.start = start;
   Scratch sc(st);
-  if ((rc = sc.alloc_n(&a.delta, size_t(a.heads) * size_t(a.T)))) return rc;
+  if ((rc = step_alloc(&sc, &a.delta, size_t(a.heads) * size_t(a.T)))) return rc;
   a.q_parts = q_parts(a);
   if (a.q_parts > 1 &&
-      (rc = sc.alloc_n(&a.q_sums, size_t(a.q_parts) * size_t(a.T) * size_t(a.heads) * size_t(a.width))))
+      (rc = step_alloc(&sc, &a.q_sums, size_t(a.q_parts) * size_t(a.T) * size_t(a.heads) * size_t(a.width))))
     return rc;
   a.parts = dkv_parts(a);
   if (a.parts > 1 &&
-      (rc = sc.alloc_n(&a.partial, size_t(2 * a.parts) * size_t(a.T) * size_t(a.kv_heads) * size_t(a.width))))
+      (rc = step_alloc(&sc, &a.partial, size_t(2 * a.parts) * size_t(a.T) * size_t(a.kv_heads) * size_t(a.width))))
     return rc;
   return p->dtype == NOPFS_BF16 ? launch_grad<MBf16>(a, st) : launch_grad<MFp16>(a, st);
 }
@@ -1432,7 +1433,8 @@ using namespace nopfs;
 extern "C" int nopfs_packed_attention(const nopfs_attention* a, const void* q, const void* k, const void* v,
                                       const int32_t* start, void* o, float* lse, void* hip_stream) {
   try {
-    return attention_impl(a, q, k, v, start, o, lse, static_cast<hipStream_t>(hip_stream));
+    auto call = [&]() { return attention_impl(a, q, k, v, start, o, lse, static_cast<hipStream_t>(hip_stream)); };
+    return a ? run_with_scratch(a->scratch, a->scratch_bytes, call) : call();
   } catch (...) {
     return fail(NOPFS_EDEVICE, "unexpected host exception");
   }
@@ -1443,8 +1445,23 @@ extern "C" int nopfs_packed_attention_grad(const nopfs_attention* a, const void*
                                            const int32_t* start, void* dq, void* dk, void* dv,
                                            void* hip_stream) {
   try {
-    return attention_grad_impl(a, d_o, q, k, v, o, lse, start, dq, dk, dv,
-                               static_cast<hipStream_t>(hip_stream));
+    auto call = [&]() {
+      return attention_grad_impl(a, d_o, q, k, v, o, lse, start, dq, dk, dv, static_cast<hipStream_t>(hip_stream));
+    };
+    return a ? run_with_scratch(a->scratch, a->scratch_bytes, call) : call();
+  } catch (...) {
+    return fail(NOPFS_EDEVICE, "unexpected host exception");
+  }
+}
+
+extern "C" int nopfs_packed_attention_scratch(const nopfs_attention* a, int32_t gradient, int64_t* bytes) {
+  try {
+    void* x = no_array();
+    return scratch_size(bytes, [&]() {
+      return gradient ? attention_grad_impl(a, x, x, x, x, x, static_cast<float*>(x), static_cast<int32_t*>(x), x, x, x,
+                                            nullptr)
+                      : attention_impl(a, x, x, x, static_cast<int32_t*>(x), x, static_cast<float*>(x), nullptr);
+    });
   } catch (...) {
     return fail(NOPFS_EDEVICE, "unexpected host exception");
   }

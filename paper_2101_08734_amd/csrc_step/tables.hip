@@ -360,7 +360,7 @@ int batch_tables_impl(const nopfs_batch* p, const int32_t* ids, const int32_t* t
     return launch("bt_small", bt_small, dim3(uint32_t(p->G * (small_tok + small_tab))), dim3(256), 0, st, b,
                   uint32_t(small_tok), uint32_t(small_tab), by_block);
   Scratch sc(st);
-  int rc = sc.alloc_n(&b.first, size_t(p->G) * (size_t(p->n) + 1));
+  int rc = step_alloc(&sc, &b.first, size_t(p->G) * (size_t(p->n) + 1));
   if (rc) return rc;
   rc = p->n <= 256 ? launch("bt_scan", bt_scan<256>, dim3(uint32_t(p->G)), dim3(256), 0, st, b, by_block)
                    : launch("bt_scan", bt_scan<1024>, dim3(uint32_t(p->G)), dim3(1024), 0, st, b, by_block);
@@ -379,8 +379,22 @@ extern "C" int nopfs_batch_tables(const nopfs_batch* batch, const int32_t* ids, 
                                   int64_t* slot, int32_t* row, int32_t* pos, int32_t* used,
                                   void* hip_stream) {
   try {
-    return batch_tables_impl(batch, ids, tokens, free_blocks, start, table, slot, row, pos, used,
-                             static_cast<hipStream_t>(hip_stream));
+    auto call = [&]() {
+      return batch_tables_impl(batch, ids, tokens, free_blocks, start, table, slot, row, pos, used,
+                               static_cast<hipStream_t>(hip_stream));
+    };
+    return batch ? run_with_scratch(batch->scratch, batch->scratch_bytes, call) : call();
+  } catch (...) {
+    return fail(NOPFS_EDEVICE, "unexpected host exception");
+  }
+}
+
+extern "C" int nopfs_batch_tables_scratch(const nopfs_batch* batch, int64_t* bytes) {
+  try {
+    int32_t* x = static_cast<int32_t*>(no_array());
+    return scratch_size(bytes, [&]() {
+      return batch_tables_impl(batch, nullptr, x, x, x, x, static_cast<int64_t*>(no_array()), x, x, x, nullptr);
+    });
   } catch (...) {
     return fail(NOPFS_EDEVICE, "unexpected host exception");
   }

@@ -76,7 +76,8 @@ def make_model(c, beta, b_c, pfs_t, pfs_gamma, w0, p0, r, p) -> Model:
 
 class _Batch(ctypes.Structure):
     _fields_ = ([(x, ctypes.c_int64) for x in ("F", "ids_stride", "free_stride")]
-                + [(x, ctypes.c_int32) for x in ("G", "n", "blocks", "block", "width", "cap")])
+                + [(x, ctypes.c_int32) for x in ("G", "n", "blocks", "block", "width", "cap")]
+                + [("scratch", ctypes.c_void_p), ("scratch_bytes", ctypes.c_int64)])
 
 
 class _Attention(ctypes.Structure):
@@ -85,7 +86,8 @@ class _Attention(ctypes.Structure):
                 + [(x, ctypes.c_int32) for x in ("n", "heads", "kv_heads", "width", "dtype")]
                 + [("scale", ctypes.c_float)]
                 + [(f"{x}_{y}", ctypes.c_int64)
-                   for x in ("q", "k", "v", "o", "do", "dq", "dk", "dv") for y in ("token", "head")])
+                   for x in ("q", "k", "v", "o", "do", "dq", "dk", "dv") for y in ("token", "head")]
+                + [("scratch", ctypes.c_void_p), ("scratch_bytes", ctypes.c_int64)])
 
 
 class _Distill(ctypes.Structure):
@@ -124,6 +126,8 @@ def lib() -> ctypes.CDLL:
             "nopfs_access_streams_range": [jp, ctypes.c_int32, ctypes.c_int32, P, P],
             "nopfs_policy_sim": [jp, P, P, P, P, ctypes.POINTER(Model), ctypes.c_int32, P, P, P, P],
             "nopfs_batch_tables": [ctypes.POINTER(_Batch)] + [P] * 10,
+            "nopfs_batch_tables_scratch": [ctypes.POINTER(_Batch), P],
+            "nopfs_packed_attention_scratch": [ctypes.POINTER(_Attention), ctypes.c_int32, P],
             "nopfs_packed_attention": [ctypes.POINTER(_Attention)] + [P] * 7,
             "nopfs_packed_attention_grad": [ctypes.POINTER(_Attention)] + [P] * 11,
             "nopfs_topk_distill": [ctypes.POINTER(_Distill)] + [P] * 7,
@@ -152,6 +156,7 @@ EXPORTED = ("nopfs_stream_shape", "nopfs_access_streams", "nopfs_access_streams_
             "nopfs_prefetch_order",
             "nopfs_staging_schedule", "nopfs_fetch_model", "nopfs_buffer_sim", "nopfs_policy_sim",
             "nopfs_batch_tables", "nopfs_packed_attention", "nopfs_packed_attention_grad",
+            "nopfs_batch_tables_scratch", "nopfs_packed_attention_scratch",
             "nopfs_topk_distill", "nopfs_strerror",
             "nopfs_last_error", "nopfs_profile_enable", "nopfs_profile_query",
             "nopfs_calibration_copy", "nopfs_scratch_release", "nopfs_debug_set")
@@ -485,6 +490,23 @@ def _step_stream(stream, device, tensors):
     return stream.cuda_stream
 
 
+def _step_scratch(desc, device, stream, size, *args):
+    """Scratch for a call that is being captured into a graph, from torch's
+    allocator, which keeps it as long as the graph; else None (the library's own).
+    size(desc, ..., bytes) tells how much. The current stream is asked: a call
+    captured on another one while the current one is not is refused."""
+    if not torch.cuda.is_current_stream_capturing():
+        return None
+    if stream is not None and stream.cuda_stream != _raw_stream(device):
+        with torch.cuda.stream(stream):
+            return _step_scratch(desc, device, None, size, *args)
+    need = ctypes.c_int64()
+    _check(size(ctypes.byref(desc), *args, ctypes.byref(need)), "scratch")
+    t = torch.empty(need.value, dtype=torch.uint8, device=device)
+    desc.scratch, desc.scratch_bytes = t.data_ptr(), need.value
+    return t
+
+
 def _row_stride(t):
     """Elements from row to row; a single row's stride says nothing."""
     return t.stride(0) if t.shape[0] > 1 else max(t.shape[1], 1)
@@ -527,6 +549,7 @@ def batch_tables(ids, tokens, free, block: int, width: int, cap: int, out=None, 
             _step_dense(t, name, dt, shape, dev)
     b = _Batch(F, _row_stride(lead), _row_stride(free), G, n, free.shape[1], block, width, cap)
     st = _step_stream(stream, dev, (ids, tokens, free, *o.values()))
+    scratch = _step_scratch(b, dev, stream, lib().nopfs_batch_tables_scratch)  # noqa: F841 held until enqueued
     _check(lib().nopfs_batch_tables(
         ctypes.byref(b), None if ids is None else ids.data_ptr(), tokens.data_ptr(),
         free.data_ptr(), o["start"].data_ptr(), o["table"].data_ptr(), o["slot"].data_ptr(),
@@ -580,6 +603,7 @@ def packed_attention(q, k, v, start, scale=None, o=None, lse=None, stream=None):
         _step_dense(lse, "lse", torch.float32, (a[2], a[0]), dev)
     a = _Attention(*a, *_strides(q, k, v, o))
     st = _step_stream(stream, dev, (q, k, v, start, o, lse))
+    scratch = _step_scratch(a, dev, stream, lib().nopfs_packed_attention_scratch, 0)  # noqa: F841
     _check(lib().nopfs_packed_attention(ctypes.byref(a), q.data_ptr(), k.data_ptr(), v.data_ptr(),
                                         start.data_ptr(), o.data_ptr(), lse.data_ptr(), st),
            "nopfs_packed_attention")
@@ -607,6 +631,7 @@ def packed_attention_grad(do, q, k, v, o, lse, start, scale=None, dq=None, dk=No
     dq, dk, dv = grads
     a = _Attention(*a, *_strides(q, k, v, o, do, dq, dk, dv))
     st = _step_stream(stream, dev, (do, q, k, v, o, lse, start, dq, dk, dv))
+    scratch = _step_scratch(a, dev, stream, lib().nopfs_packed_attention_scratch, 1)  # noqa: F841
     _check(lib().nopfs_packed_attention_grad(
         ctypes.byref(a), do.data_ptr(), q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(),
         lse.data_ptr(), start.data_ptr(), dq.data_ptr(), dk.data_ptr(), dv.data_ptr(), st),

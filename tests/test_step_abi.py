@@ -175,3 +175,47 @@ def test_host_tensors_are_refused():
 def test_scales_and_temperatures_out_of_range(L, x):
     assert _forward(L, _attention(scale=x)) == ERANGE and _grad(L, _attention(scale=x)) == ERANGE
     assert _loss(L, _distill(tau=x)) == ERANGE
+
+
+def _size(L, call, *args):
+    need = ctypes.c_int64(-1)
+    rc = call(*args, ctypes.byref(need))
+    return rc, need.value
+
+
+def test_scratch_sizes(L):
+    """On the host, from the description alone; what the refused calls refuse."""
+    batch = lambda **kw: _size(L, L.nopfs_batch_tables_scratch, ctypes.byref(_batch(**kw)))  # noqa: E731
+    assert batch() == (0, 0)  # one launch makes its sums itself
+    rc, need = batch(n=5_000, ids_stride=5_000)
+    assert rc == 0 and need >= 2 * 5_001 * 4
+    assert batch(n=0) == (EINVAL, 0) and L.nopfs_batch_tables_scratch(ctypes.byref(_batch()), None) == EINVAL
+
+    def attention(gradient, **kw):
+        return _size(L, L.nopfs_packed_attention_scratch, ctypes.byref(_attention(**kw)), gradient)
+
+    assert attention(0) == (0, 0)
+    rc, need = attention(1)
+    assert rc == 0 and need >= 4 * 100 * 4
+    one = dict(T=6_000, n=1)  # parts of the keys: 32-bit sums and a row's statistics
+    assert attention(0, **one)[1] >= 6_000 * 4 * (64 * 4 + 8) * 2
+    assert attention(1, **one)[1] >= 6_000 * 4 * 64 * 4 * 2
+    assert attention(0, T=0) == (0, 0) and attention(1, T=0) == (0, 0)
+    assert attention(1, width=60) == (EINVAL, 0) and attention(0, T=2**31) == (ERANGE, 0)
+
+
+def test_scratch_refusals(L):
+    """Too little of it, or in the wrong place, before anything is enqueued."""
+    one = dict(T=6_000, n=1)
+    for call, kw, make, size in (
+            (_tables, dict(n=5_000, ids_stride=5_000), _batch,
+             lambda d: _size(L, L.nopfs_batch_tables_scratch, ctypes.byref(d))),
+            (_forward, one, _attention,
+             lambda d: _size(L, L.nopfs_packed_attention_scratch, ctypes.byref(d), 0)),
+            (_grad, one, _attention,
+             lambda d: _size(L, L.nopfs_packed_attention_scratch, ctypes.byref(d), 1))):
+        need = size(make(**kw))[1]
+        assert call(L, make(**kw, scratch=0x1010, scratch_bytes=need)) == EINVAL
+        assert call(L, make(**kw, scratch=0x1000, scratch_bytes=-1)) == EINVAL
+        assert call(L, make(**kw, scratch=0x1000, scratch_bytes=need - 1)) == ENOMEM
+        assert b"scratch" in L.nopfs_last_error()
