@@ -30,6 +30,7 @@ struct Distill {
 constexpr int32_t kMaxTop = 1024;  // teacher entries per row held in LDS
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr float kNegInf = -INFINITY;
+constexpr float kFusedMost = 0x1p20f;
 
 __device__ inline float wave_max(float v) {
   for (int o = 32; o; o >>= 1) v = fmaxf(v, __shfl_xor(v, o));
@@ -150,8 +151,10 @@ __device__ inline bool teacher_entries(const Distill& d, int64_t t, const typena
 //
 // With c = log2(e) / tau the exponentials are exp2(c a - c m) in one fused
 // multiply-add: c m is rounded once, so all of them carry the same factor,
-// which cancels in q = e / sum and in log q. Where c m is no finite number (a
-// maximum of -inf, inf, or beyond 2^128 / c) they are exp2(c (a - m)).
+// which cancels in q = e / sum and in log q: 2^(half a unit of c m), no more than
+// 2^(1/32) up to c m = kFusedMost. Beyond (small temperatures, large logits, a
+// maximum of +-inf) that factor would grow out of the floats' range, and they are
+// exp2(c (a - m)).
 template <class E, class Y, int kThreads, int kHold>
 __global__ void __launch_bounds__(kThreads) td_row(const Distill d) {
   typedef typename E::T T;
@@ -206,7 +209,7 @@ __global__ void __launch_bounds__(kThreads) td_row(const Distill d) {
     m = block_reduce<kThreads, true>(m, tmp);
     cm = c * m;
     forget<kHold>(hold);
-    if (fabsf(cm) < INFINITY) {
+    if (fabsf(cm) < kFusedMost) {
       sum = exp2_fast(fmaf(last, c, -cm));
 #pragma unroll
       for (int j = 0; j < kHold; ++j)
@@ -245,23 +248,28 @@ __global__ void __launch_bounds__(kThreads) td_row(const Distill d) {
   if (!s_any) return zero_row();
   forget<kHold>(hold);
 
-  const bool fused = fabsf(cm) < INFINITY;  // the same in every thread
+  const bool fused = fabsf(cm) < kFusedMost;  // the same in every thread
+  const float wt = w * d.tau;
   if (tid < 64) {
     const float z = logf(sum);
     float loss = 0.0f;
     for (int k = tid; k < d.K; k += 64) {
       if (en.id[k] < 0) continue;
-      const float a = fused ? fmaf(en.x[k], c, -cm) : (en.x[k] - m) * c;
+      const float under = en.x[k] - m, a = fused ? fmaf(en.x[k], c, -cm) : under * c;
       const float p = en.p[k];
       en.x[k] = a;
-      if (p != 0.0f) loss += p * (en.logp[k] - a * kLn2 + z);
+      if (p == 0.0f) continue;
+      // tau times a term; a itself overflows where the logits are 2^128 tau / log2(e) apart
+      const float term =
+          fused && a != kNegInf ? d.tau * (en.logp[k] - a * kLn2 + z) : d.tau * (en.logp[k] + z) - under;
+      loss += p * wt * term;
     }
     loss = wave_sum(loss);
-    if (tid == 0) d.loss[t] = w * d.tau * d.tau * loss;
+    if (tid == 0) d.loss[t] = loss;
   }
   if (!ds) return;
 
-  const float wt = w * d.tau, scale = wt / sum;
+  const float scale = wt / sum;
   if (kHold > 0 && fused) {
     auto grad = [&](float a) { return exp2_fast(fmaf(a, c, -cm)) * scale; };
 #pragma unroll
