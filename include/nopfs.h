@@ -433,7 +433,7 @@ typedef struct nopfs_attention {
   int32_t kv_heads;    /* query head h reads kv head h div (heads/kv_heads)  */
   int32_t width;       /* elements of a head: a multiple of 8, 8..128        */
   int32_t dtype;       /* NOPFS_BF16 or NOPFS_FP16                           */
-  float scale;         /* of the products q.k, 2^-60 .. 2^60                 */
+  float scale;         /* of the products q.k, 2^-60 .. 2^60 (gradient 2^10) */
   int64_t q_stride[2], k_stride[2], v_stride[2], o_stride[2];
   int64_t do_stride[2], dq_stride[2], dk_stride[2], dv_stride[2]; /* gradient only */
   void* scratch;         /* the call's scratch, a multiple of 256 bytes, or    */
@@ -461,6 +461,8 @@ int nopfs_packed_attention(const nopfs_attention* a, const void* q, const void* 
  *   dq_i = scale sum_j dS_ij k_j,
  *   dk_j = scale sum over the query heads of the group and i of dS_ij q_i,
  *   dv_j = the same sum of P_ij do_i.
+ * P comes from lse, whose 32 bits leave it off by a factor of up to
+ * 1 +- 2^-22 |lse_i|: scores in the thousands cost accuracy.
  * Rows from start[n] on get 0. A NaN or infinity of a row may reach, as 0 times
  * it, dq of up to 31 rows before it and dk and dv of up to 31 after it in its
  * sample, which do not depend on it. Errors: EINVAL, ERANGE, ENOMEM, EDEVICE. */

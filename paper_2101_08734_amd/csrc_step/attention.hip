@@ -92,6 +92,11 @@ constexpr float kLog2e = 1.4426950408889634f;
 // than this (base 2): until then exponentials up to 2^8 are summed, exact to
 // the same relative error, and the sums need no rescaling.
 constexpr float kSlack = 8.0f;
+// Exponentials are exp2(c s - c m) in one fused multiply-add as long as c m, which
+// is rounded, is at most this: all of a row's then carry the same factor, within
+// 2^-15 of 1. Beyond (large scores or scales) it would grow out of the floats'
+// range, and they are exp2(c (s - m)).
+constexpr float kFusedMost = 0x1p10f;
 
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 
@@ -583,13 +588,24 @@ __global__ void __launch_bounds__(256, kSplits == 4 && DP == 128 ? 1 : 2) at_for
         for (int e = 0; e < 16; ++e) acc[i][e] *= f;
     }
     const float mc = m * c2;
+    if (__any(fabsf(mc) > kFusedMost)) {
+      const float base = m == -INFINITY ? 0.0f : m;  // no score but -inf yet: exponentials of 0
 #pragma unroll
-    for (int u = 0; u < NU; ++u)
+      for (int u = 0; u < NU; ++u)
 #pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        s[u][e] = exp2_fast(fmaf(s[u][e], c2, -mc));
-        l += s[u][e];
-      }
+        for (int e = 0; e < 16; ++e) {
+          s[u][e] = exp2_fast((s[u][e] - base) * c2);
+          l += s[u][e];
+        }
+    } else {
+#pragma unroll
+      for (int u = 0; u < NU; ++u)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          s[u][e] = exp2_fast(fmaf(s[u][e], c2, -mc));
+          l += s[u][e];
+        }
+    }
     if constexpr (DP == 128) __builtin_amdgcn_s_setprio(1);
 #pragma unroll
     for (int u = 0; u < NU; ++u)
@@ -1392,6 +1408,8 @@ int attention_grad_impl(const nopfs_attention* p, const void* d_o, const void* q
   Attention a = {};
   int rc = make_attention(p, &a);
   if (rc) return rc;
+  if (a.scale > 0x1p10f)  // lse in 32 bits says too little of the softmax
+    return fail(NOPFS_ERANGE, "the gradient's scale must be <= 2^10");
   if (a.T == 0) return NOPFS_OK;
   if ((rc = check_array("q", q, a.q_s, a.heads, a.width))) return rc;
   if ((rc = check_array("k", k, a.k_s, a.kv_heads, a.width))) return rc;
