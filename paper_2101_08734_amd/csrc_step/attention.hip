@@ -82,6 +82,9 @@ struct Attention {
   int32_t q_parts;
   float* q_sums;
   f32x2* q_stats;
+  // for dq also sum_j P_ij k_j, the row's statistics then eps_i and whether
+  // that sum is there (not 0)
+  float* q_bars;
   const int32_t* start;
   uint32_t tiles;  // an upper bound of the row tiles
   const int4* order;  // the tiles' (sample, first row, begin, length), costliest first, or NULL
@@ -692,17 +695,22 @@ __global__ void __launch_bounds__(256) at_join(const Attention a) {
 
 // ----------------------------------------------------------------------- dq --
 // P again from S and lse, whose subtraction (and delta's) is the accumulators'
-// start, so no row statistic is needed; also writes delta_i = do_i.o_i for the
-// dk/dv kernels. A sample's first rows see few keys: there o's rounding, times
-// do, is not small beside dP - delta (two tokens of bf16: dq off by 0.0054
-// relative, by 0.0025 now), so a sample's first tile takes sum_j P_ij dP_ij,
-// delta before o was rounded, from a pass of its own over its keys (no more
-// than 1 us at 300 to 16,384 tokens). 8,192 x 16 heads of 64: 210 us, 0.98
-// PFLOP/s of three products; matrix units 48%, vector units 46%. 16,384 tokens
-// of 32 documents x 16 of 128: 150 us, matrix units 30%, again the longest
-// documents.
+// start, so no row statistic is needed; also writes delta_i for the dk/dv
+// kernels. delta is do_i.o_i at first, off by eps_i for the roundings of o and of
+// the P in it. That is not small beside dP - delta on keys that have most of a
+// row's weight (scores of standard deviation 16: dq off by 3.4 roundings of its
+// own). The pass sums eps_i = sum_j P_ij (dP_ij - delta_i), 0 for the true delta, in
+// 32 bits; dq_i = scale (sum_j dS_ij k_j - eps_i sum_j P_ij k_j), and a second pass
+// makes the latter sum over the key tiles where a query of the workgroup has more
+// than kHeavy of its weight on a key (the rest of it is small beside what the
+// rounding of dS leaves). 8,192 x 16 heads of 64: 216 us, 0.95
+// PFLOP/s of three products. 16,384 tokens of 32 documents x 16 of 128: 162 us,
+// again the longest documents. Standard normal scores; without eps and the second
+// pass 204 and 152; with kHeavy 1/16 217 and 171, and no smaller errors. Three
+// workgroups of narrow heads a compute unit: 216 us, with two 240.
+constexpr float kHeavy = 1.0f / 8;
 template <class M, int DP, int DW, int kSplits>
-__global__ void __launch_bounds__(256, kSplits == 4 && DP == 128 ? 1 : 2) at_dq(const Attention a) {
+__global__ void __launch_bounds__(256, DP == 64 && kSplits < 4 ? 3 : kSplits == 4 && DP == 128 ? 1 : 2) at_dq(const Attention a) {
   typedef typename M::T T;
   constexpr int DT = DW / 32, DC = DW / 16;
   constexpr int kKeys = kTileKeys<kSplits>, kStrips = 4 / kSplits, kRows = 32 * kStrips, NU = kKeys / 32 / kSplits;
@@ -756,40 +764,7 @@ __global__ void __launch_bounds__(256, kSplits == 4 && DP == 128 ? 1 : 2) at_dq(
     cv.zero_pad(lv0);
     cv.zero_pad(lv1);
   }
-  if (t.m0 == 0) {
-    static_assert(kRows <= 2 * kKeys);  // the first tile's keys are in the two buffers
-    ck.copy(reinterpret_cast<const char*>(kb), t.len, lk0);
-    cv.copy(reinterpret_cast<const char*>(vb), t.len, lv0);
-    if (kRows > kKeys && t.len > kKeys) {
-      ck.copy(reinterpret_cast<const char*>(kb) + int64_t(ck.stride) * kKeys, t.len - kKeys, lk1);
-      cv.copy(reinterpret_cast<const char*>(vb) + int64_t(cv.stride) * kKeys, t.len - kKeys, lv1);
-    }
-    meet<0>();
-    delta = 0.0f;
-#pragma unroll 1
-    for (int k0 = 0; k0 <= q0 && k0 < t.len; k0 += 32) {
-      const char* lk = k0 < kKeys ? lk0 : lk1;
-      const char* lv = k0 < kKeys ? lv0 : lv1;
-      f32x16 s, dp;
-#pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        s[e] = minus_lse;
-        dp[e] = 0.0f;
-      }
-#pragma unroll
-      for (int c = 0; c < DC; ++c) {
-        s = M::mma(frag_row<M, DP>(lk, k0 % kKeys, 2 * c), q[c], s);
-        dp = M::mma(frag_row<M, DP>(lv, k0 % kKeys, 2 * c), d[c], dp);
-      }
-#pragma unroll
-      for (int e = 0; e < 16; ++e)
-        if (k0 + acc_row(e) + 4 * half <= qi) delta += exp2_fast(s[e] * c2) * dp[e];
-    }
-    delta = half_sum(delta);
-    if (j_first > 0) __syncthreads();  // the buffers are free again
-  }
-  if (half == 0 && split == 0 && which == 0 && qi < t.len) a.delta[stat] = delta;
-  if ((t.m0 > 0 || j_first > 0) && j_first < n_tiles) {
+  if (j_first < n_tiles) {
     ck.copy(kt, t.len - j_first * kKeys, lk0);
     cv.copy(vt, t.len - j_first * kKeys, lv0);
   }
@@ -799,6 +774,10 @@ __global__ void __launch_bounds__(256, kSplits == 4 && DP == 128 ? 1 : 2) at_dq(
   for (int i = 0; i < DT; ++i)
 #pragma unroll
     for (int e = 0; e < 16; ++e) acc[i][e] = 0.0f;
+  float eps = 0.0f;
+  int group = 0;  // 2^group tiles share a bit of the tiles to go through again
+  while ((n_tiles - 1 - j_first) >> group >= 64) ++group;
+  uint64_t heavy = 0;  // such tiles of this wave
 
   auto step = [&](int j, const char* lk, const char* lv, char* next_k, char* next_v) {
     meet<0>();
@@ -825,12 +804,20 @@ __global__ void __launch_bounds__(256, kSplits == 4 && DP == 128 ? 1 : 2) at_dq(
         dp = M::mma(frag_row<M, DP>(lv, 32 * u, 2 * c), d[c], dp);
       }
 #pragma unroll
-      for (int e = 0; e < 16; ++e) s[e] = exp2_fast(s[e] * c2) * dp[e];
+      for (int e = 0; e < 16; ++e) s[e] = exp2_fast(s[e] * c2);
       if (kb == q0) {  // the diagonal: both are multiples of 32
-  #pragma unroll
+#pragma unroll
         for (int e = 0; e < 16; ++e)
-          if (acc_row(e) + 4 * half > (lane & 31)) s[e] = 0.0f;
+          if (acc_row(e) + 4 * half > (lane & 31)) s[e] = dp[e] = 0.0f;
       }
+      float top = s[0];
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        top = fmaxf(top, s[e]);
+        s[e] *= dp[e];
+        eps += s[e];
+      }
+      if (__any(top > kHeavy)) heavy |= uint64_t(1) << ((j - j_first) >> group);
 #pragma unroll
       for (int c = 0; c < 2; ++c) {
         const typename M::V8 p = pack8<M>(s, c);
@@ -843,20 +830,105 @@ __global__ void __launch_bounds__(256, kSplits == 4 && DP == 128 ? 1 : 2) at_dq(
     step(j, lk0, lv0, lk1, lv1);
     if (j + 1 < n_tiles) step(j + 1, lk1, lv1, lk0, lv0);
   }
-  if constexpr (kSplits > 1) {
+  auto join_splits = [&](f32x16* x) {  // into the first split's
     auto place = [&](int i) -> char* { return i == 0 ? lk0 : i == 1 ? lv0 : lk1; };
     __syncthreads();
-    if (split) give_columns<DT>(place((split - 1) * kStrips + strip), acc);
+    if (split) give_columns<DT>(place((split - 1) * kStrips + strip), x);
     __syncthreads();
     if (split) return;
 #pragma unroll
-    for (int x = 0; x < kSplits - 1; ++x) take_columns<DT>(place(x * kStrips + strip), acc, 1.0f, 1.0f);
+    for (int y = 0; y < kSplits - 1; ++y) take_columns<DT>(place(y * kStrips + strip), x, 1.0f, 1.0f);
+  };
+  // eps of a row from the waves that share it, and the workgroup's heavy tiles
+  __syncthreads();
+  uint64_t* masks = reinterpret_cast<uint64_t*>(lv0);
+  float* others = reinterpret_cast<float*>(lv0 + 64);
+  eps = half_sum(eps);
+  if (lane == 0) masks[wave] = heavy;
+  if constexpr (kSplits > 1) others[wave * 64 + lane] = eps;
+  __syncthreads();
+  if constexpr (kSplits > 1) {
+    eps = 0.0f;
+#pragma unroll
+    for (int x = 0; x < kSplits; ++x) eps += others[(x * kStrips + strip) * 64 + lane];
+  }
+  uint64_t todo = masks[0] | masks[1] | masks[2] | masks[3];
+  todo = uint64_t(uint32_t(__builtin_amdgcn_readfirstlane(int(todo >> 32)))) << 32 |
+         uint32_t(__builtin_amdgcn_readfirstlane(int(todo)));
+  const int64_t part_row = which * a.T + qr;
+  if (a.q_parts == 1) {
+    if (half == 0 && split == 0 && qi < t.len) a.delta[stat] = delta + eps;
+  } else if (half == 0 && split == 0 && qi < t.len) {  // joined by at_sum_dq
+    if (which == 0) a.delta[stat] = delta;
+    a.q_stats[(int64_t(which) * a.heads + head) * a.T + qr] = f32x2{eps, todo ? 1.0f : 0.0f};
+  }
+  if (todo) {
+    f32x16 bar[DT];  // sum_j P_ij k_j
+#pragma unroll
+    for (int i = 0; i < DT; ++i)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) bar[i][e] = 0.0f;
+    auto next = [&](int j) {  // the first tile to do from j on
+      while (j < n_tiles && !(todo >> ((j - j_first) >> group) & 1)) ++j;
+      return j;
+    };
+    auto copy = [&](int j, char* to) {
+      ck.copy(reinterpret_cast<const char*>(kb) + int64_t(ck.stride) * (int64_t(j) * kKeys), t.len - j * kKeys, to);
+    };
+    int j = next(j_first);
+    copy(j, lk0);
+    auto again = [&](const char* lk, char* other) {
+      meet<0>();  // tile j is in LDS, and the one before it is done with
+      const int k0 = j * kKeys;
+      const bool mine = heavy >> ((j - j_first) >> group) & 1;
+      j = next(j + 1);
+      if (j < n_tiles) copy(j, other);
+      if (!mine) return;
+#pragma unroll 1
+      for (int x = 0; x < NU; ++x) {
+        const int u = NU * split + x, kb = k0 + 32 * u;
+        if (kb > q0) break;
+        f32x16 s;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) s[e] = minus_lse;
+#pragma unroll
+        for (int c = 0; c < DC; ++c) s = M::mma(frag_row<M, DP>(lk, 32 * u, 2 * c), q[c], s);
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          s[e] = exp2_fast(s[e] * c2);
+          if (kb == q0 && acc_row(e) + 4 * half > (lane & 31)) s[e] = 0.0f;
+        }
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+          const typename M::V8 p = pack8<M>(s, c);
+#pragma unroll
+          for (int i = 0; i < DT; ++i) bar[i] = M::mma(frag_col<M, DP>(lk, 32 * u + 16 * c, 32 * i), p, bar[i]);
+        }
+      }
+    };
+    while (j < n_tiles) {
+      again(lk0, lk1);
+      if (j < n_tiles) again(lk1, lk0);
+    }
+    if (a.q_parts == 1) {
+#pragma unroll
+      for (int i = 0; i < DT; ++i)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) acc[i][e] -= eps * bar[i][e];
+    } else {
+      if constexpr (kSplits > 1) join_splits(bar);
+      if (split == 0 && qi < t.len) store_sums<DT>(a.q_bars + (part_row * a.heads + head) * width, bar, width);
+    }
+  }
+  if constexpr (kSplits > 1) {
+    join_splits(acc);
+    if (split) return;
   }
   if (qi >= t.len) return;
   if (a.q_parts == 1)
     store_columns<M, DT>(static_cast<T*>(a.dq) + qr * a.dq_s[0] + head * a.dq_s[1], acc, a.scale, width);
   else
-    store_sums<DT>(a.q_sums + ((which * a.T + qr) * a.heads + head) * width, acc, width);
+    store_sums<DT>(a.q_sums + (part_row * a.heads + head) * width, acc, width);
 }
 
 // -------------------------------------------------------------------- dk, dv --
@@ -1190,11 +1262,34 @@ __global__ void __launch_bounds__(256) at_sum(const Attention a) {
   sum_parts<M>(a, a.partial, 2 * size, a.parts, i, a.kv_heads, a.dk, a.dk_s, a.scale);
   sum_parts<M>(a, a.partial + size, 2 * size, a.parts, i, a.kv_heads, a.dv, a.dv_s, 1.0f);
 }
+// dq and delta from their parts.
 template <class M>
 __global__ void __launch_bounds__(256) at_sum_dq(const Attention a) {
   const int64_t size = a.T * a.heads * a.width;
   const int64_t i = (int64_t(blockIdx.x) * 256 + threadIdx.x) * 4;
-  if (i < size) sum_parts<M>(a, a.q_sums, size, a.q_parts, i, a.heads, a.dq, a.dq_s, a.scale);
+  if (i >= size) return;
+  const int64_t rh = i / a.width;
+  const int d = int(i - rh * a.width);
+  const int64_t row = rh / a.heads, head = rh - row * a.heads;
+  f32x4 x = {0, 0, 0, 0};
+  if (row < sample_begin(a, a.n)) {
+    const f32x2* st = a.q_stats + head * a.T + row;
+    const int64_t step = a.heads * a.T;
+    float eps = 0.0f;
+    f32x4 bar = {0, 0, 0, 0};
+    for (int p = 0; p < a.q_parts; ++p) {
+      const f32x2 y = st[p * step];
+      eps += y[0];
+      x += *reinterpret_cast<const f32x4*>(a.q_sums + p * size + i);
+      if (y[1] != 0.0f) bar += *reinterpret_cast<const f32x4*>(a.q_bars + p * size + i);
+    }
+    x -= eps * bar;
+    if (d == 0) a.delta[head * a.T + row] += eps;
+  }
+  typename M::V4 v;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) v[e] = typename M::T(x[e] * a.scale);
+  *reinterpret_cast<typename M::V4*>(static_cast<typename M::T*>(a.dq) + row * a.dq_s[0] + head * a.dq_s[1] + d) = v;
 }
 
 // --------------------------------------------------------------------- host --
@@ -1433,9 +1528,12 @@ int attention_grad_impl(const nopfs_attention* p, const void* d_o, const void* q
   Scratch sc(st);
   if ((rc = step_alloc(&sc, &a.delta, size_t(a.heads) * size_t(a.T)))) return rc;
   a.q_parts = q_parts(a);
-  if (a.q_parts > 1 &&
-      (rc = step_alloc(&sc, &a.q_sums, size_t(a.q_parts) * size_t(a.T) * size_t(a.heads) * size_t(a.width))))
-    return rc;
+  if (a.q_parts > 1) {
+    const size_t rows = size_t(a.q_parts) * size_t(a.T) * size_t(a.heads);
+    if ((rc = step_alloc(&sc, &a.q_sums, rows * size_t(a.width)))) return rc;
+    if ((rc = step_alloc(&sc, &a.q_bars, rows * size_t(a.width)))) return rc;
+    if ((rc = step_alloc(&sc, &a.q_stats, rows))) return rc;
+  }
   a.parts = dkv_parts(a);
   if (a.parts > 1 &&
       (rc = step_alloc(&sc, &a.partial, size_t(2 * a.parts) * size_t(a.T) * size_t(a.kv_heads) * size_t(a.width))))
