@@ -32,7 +32,13 @@
 //
 // Softmax statistics, sums and the delta_i = do_i.o_i are held in 32 bits.
 // P and dS are rounded to the inputs' type for the second products (they are
-// matrix operands); everything else is rounded once, at the store.
+// matrix operands); everything else is rounded once, at the store. In fp16 the
+// gradient's P and dS carry a power of two that its sums give back, since dS may
+// be out of its range (beyond 65504, or subnormal for small do and long samples)
+// where dq and dk are not: P 2^15; dS of a query in the dq kernel one that follows
+// its largest, dS of a key in the dk/dv kernels one from the largest of all its
+// queries, which the dq kernel leaves for every 32 rows (tops). 5,173 tokens of 41
+// samples x 6 heads of 80: dq 24.5 -> 26.4 us, dk and dv 33.4 -> 35.
 #include "step.hpp"
 
 namespace nopfs {
@@ -47,6 +53,7 @@ struct MBf16 {
   typedef __bf16 V8 __attribute__((ext_vector_type(8)));
   typedef __bf16 V4 __attribute__((ext_vector_type(4)));
   typedef __bf16 V2 __attribute__((ext_vector_type(2)));
+  static constexpr bool kNarrow = false;  // has the exponents of 32-bit floats
   static __device__ __forceinline__ f32x16 mma(V8 a, V8 b, f32x16 c) {
     return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
   }
@@ -56,6 +63,7 @@ struct MFp16 {
   typedef _Float16 V8 __attribute__((ext_vector_type(8)));
   typedef _Float16 V4 __attribute__((ext_vector_type(4)));
   typedef _Float16 V2 __attribute__((ext_vector_type(2)));
+  static constexpr bool kNarrow = true;
   static __device__ __forceinline__ f32x16 mma(V8 a, V8 b, f32x16 c) {
     return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
   }
@@ -85,6 +93,10 @@ struct Attention {
   // for dq also sum_j P_ij k_j, the row's statistics then eps_i and whether
   // that sum is there (not 0)
   float* q_bars;
+  // fp16: the largest |dS| of 32 rows of a head, in the place of the first of
+  // them, from every wave that had a share of it: [tops_of][heads][T]
+  float* tops;
+  int32_t tops_of;
   const int32_t* start;
   uint32_t tiles;  // an upper bound of the row tiles
   const int4* order;  // the tiles' (sample, first row, begin, length), costliest first, or NULL
@@ -102,6 +114,13 @@ constexpr float kSlack = 8.0f;
 constexpr float kFusedMost = 0x1p10f;
 
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// In fp16 P of the dk/dv kernels times 2^kLiftP. dS of a query is scaled again once
+// it passes kMostS, to 2^(kTopS - 1) .. 2^kTopS, and dS of a key's queries to
+// 2^(kTopK - 1) .. 2^kTopK by their bound (dS of tops has the delta from o, and
+// its row's eps, the sum over all parts, comes on top: up to the parts + 1 times).
+constexpr int kLiftP = 15, kTopS = 10, kTopK = 11;
+constexpr float kMostS = 0x1p15f;
 
 // The value of a lane combined with that of lane ^ 32.
 __device__ __forceinline__ float half_max(float v) {
@@ -429,6 +448,35 @@ __device__ __forceinline__ void store_dkv(const Attention& a, int64_t kr, int64_
   float* row = a.partial + 2 * part * size + (kr * a.kv_heads + kv) * a.width + d0;
   store_sums<DT>(row, dk, a.width - d0);
   store_sums<DT>(row + size, dv, a.width - d0);
+}
+
+template <int DT>
+__device__ __forceinline__ void scale_sums(f32x16* acc, float f) {
+#pragma unroll
+  for (int i = 0; i < DT; ++i)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) acc[i][e] *= f;
+}
+
+// The exponent that brings a key tile's dS of query tiles i0 .. i0 + n - 1 (of its
+// sample's from j0 to j1 for all heads of the group) into range; the same in every
+// thread. Infinities and NaN among them count for nothing. lds: free, and free again.
+__device__ inline int ds_exponent(const Attention& a, const Tile& t, int64_t head0, int j0, int j1, int i0, int n,
+                                  float* lds) {
+  float top = 0.0f;
+  for (int x = threadIdx.x; x < 2 * n; x += 256) {
+    const int i = i0 + x / 2, row = (j0 + i % (j1 - j0)) * 64 + 32 * (x & 1);
+    if (row >= t.len) continue;
+    const float* p = a.tops + (head0 + i / (j1 - j0)) * a.T + t.begin + row;
+    for (int c = 0; c < a.tops_of; ++c) top = fmaxf(top, p[c * (a.heads * a.T)]);
+  }
+  for (int o = 32; o; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
+  if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = top;
+  __syncthreads();
+  top = fmaxf(fmaxf(lds[0], lds[1]), fmaxf(lds[2], lds[3]));
+  __syncthreads();
+  const int e = top > 0.0f ? kTopK - __builtin_amdgcn_frexp_expf(top) : 0;
+  return __builtin_amdgcn_readfirstlane(max(-100, min(100, e)));
 }
 
 // A wave's accumulators through LDS to the wave that owns the same columns,
@@ -778,6 +826,9 @@ __global__ void __launch_bounds__(256, DP == 64 && kSplits < 4 ? 3 : kSplits == 
   int group = 0;  // 2^group tiles share a bit of the tiles to go through again
   while ((n_tiles - 1 - j_first) >> group >= 64) ++group;
   uint64_t heavy = 0;  // such tiles of this wave
+  // fp16: P, dS, eps and acc of the lane's query are 2^lift times what they are
+  // (dS is below 2^40: products of 128 elements), most the largest |dS|
+  float lift = 60.0f, most = 0.0f;
 
   auto step = [&](int j, const char* lk, const char* lv, char* next_k, char* next_v) {
     meet<0>();
@@ -804,7 +855,7 @@ __global__ void __launch_bounds__(256, DP == 64 && kSplits < 4 ? 3 : kSplits == 
         dp = M::mma(frag_row<M, DP>(lv, 32 * u, 2 * c), d[c], dp);
       }
 #pragma unroll
-      for (int e = 0; e < 16; ++e) s[e] = exp2_fast(s[e] * c2);
+      for (int e = 0; e < 16; ++e) s[e] = exp2_fast(M::kNarrow ? fmaf(s[e], c2, lift) : s[e] * c2);
       if (kb == q0) {  // the diagonal: both are multiples of 32
 #pragma unroll
         for (int e = 0; e < 16; ++e)
@@ -817,7 +868,23 @@ __global__ void __launch_bounds__(256, DP == 64 && kSplits < 4 ? 3 : kSplits == 
         s[e] *= dp[e];
         eps += s[e];
       }
-      if (__any(top > kHeavy)) heavy |= uint64_t(1) << ((j - j_first) >> group);
+      if (__any(top > (M::kNarrow ? kHeavy * exp2_fast(lift) : kHeavy))) heavy |= uint64_t(1) << ((j - j_first) >> group);
+      if constexpr (M::kNarrow) {
+        top = 0.0f;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) top = fmaxf(top, fabsf(s[e]));
+        top = half_max(top);
+        most = fmaxf(most, top);
+        if (__any(top > kMostS)) {
+          const int d = top > kMostS ? kTopS - __builtin_amdgcn_frexp_expf(top) : 0;
+          const float f = __builtin_ldexpf(1.0f, d);
+          lift += float(d);
+          most *= f;
+          eps *= f;
+          scale_sums<DT>(acc, f);
+          scale_sums<1>(&s, f);
+        }
+      }
 #pragma unroll
       for (int c = 0; c < 2; ++c) {
         const typename M::V8 p = pack8<M>(s, c);
@@ -839,6 +906,16 @@ __global__ void __launch_bounds__(256, DP == 64 && kSplits < 4 ? 3 : kSplits == 
 #pragma unroll
     for (int y = 0; y < kSplits - 1; ++y) take_columns<DT>(place(y * kStrips + strip), x, 1.0f, 1.0f);
   };
+  if constexpr (M::kNarrow) {
+    const float f = exp2_fast(-lift);
+    eps *= f;
+    scale_sums<DT>(acc, f);
+    float top = fmaf(most, f, fabsf(half_sum(eps)));
+    top = top < INFINITY ? top : 0.0f;
+    for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
+    if (lane == 0 && q0 < t.len)
+      a.tops[(int64_t(which * kSplits + split) * a.heads + head) * a.T + t.begin + q0] = top;
+  }
   // eps of a row from the waves that share it, and the workgroup's heavy tiles
   __syncthreads();
   uint64_t* masks = reinterpret_cast<uint64_t*>(lv0);
@@ -988,6 +1065,9 @@ __global__ void __launch_bounds__(256, 2) at_dkv(const Attention a) {
     if (ki < t.len) store_dkv<M, DT>(a, kr, kv, which, 0, dk, dv);
     return;
   }
+  const int lift =
+      M::kNarrow ? ds_exponent(a, t, int64_t(kv) * group, j0, j1, i0, n_tiles, reinterpret_cast<float*>(lq0)) : 0;
+  const float lift_ds = __builtin_ldexpf(1.0f, lift - kLiftP);  // of dS with P's
   const TileCopy<DP, kQs> cq(a.q_s[0], width), cd(a.do_s[0], width);
   // the tile copied next: query head and tile of the sample
   int64_t h_next = int64_t(kv) * group + i0 / (j1 - j0);
@@ -1033,8 +1113,8 @@ __global__ void __launch_bounds__(256, 2) at_dkv(const Attention a) {
       __builtin_amdgcn_s_setprio(0);
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
-        s[r] = exp2_fast(s[r] * c2);
-        dp[r] *= s[r];
+        s[r] = exp2_fast(M::kNarrow ? fmaf(s[r], c2, float(kLiftP)) : s[r] * c2);
+        dp[r] *= M::kNarrow ? s[r] * lift_ds : s[r];
       }
       if (row0 + 32 * u == k0) {  // the diagonal: both are multiples of 32
   #pragma unroll
@@ -1063,6 +1143,10 @@ __global__ void __launch_bounds__(256, 2) at_dkv(const Attention a) {
   for (int i = 0; i < n_tiles; i += 2) {
     step(i, lq0, ld0, stat0, lq1, ld1, stat1);
     if (i + 1 < n_tiles) step(i + 1, lq1, ld1, stat1, lq0, ld0, stat0);
+  }
+  if constexpr (M::kNarrow) {
+    scale_sums<DT>(dk, __builtin_ldexpf(1.0f, -lift));
+    scale_sums<DT>(dv, __builtin_ldexpf(1.0f, -kLiftP));
   }
   if constexpr (kSplits == 2) {
     __syncthreads();
@@ -1140,6 +1224,9 @@ __global__ void __launch_bounds__(256, 2) at_dkv_wide(const Attention a) {
     if (ki < t.len) store_dkv<M, 2>(a, kr, kv, which, 64 * part, dk, dv);
     return;
   }
+  const int lift =
+      M::kNarrow ? ds_exponent(a, t, int64_t(kv) * group, j0, j1, i0, n_tiles, reinterpret_cast<float*>(lq0)) : 0;
+  const float lift_ds = __builtin_ldexpf(1.0f, lift - kLiftP);  // of dS with P's
   const TileCopy<DP, kQs> cq(a.q_s[0], width), cd(a.do_s[0], width);
   int64_t h_next = int64_t(kv) * group + i0 / (j1 - j0);
   int j_next = j0 + i0 % (j1 - j0);
@@ -1187,8 +1274,8 @@ __global__ void __launch_bounds__(256, 2) at_dkv_wide(const Attention a) {
       __builtin_amdgcn_s_setprio(0);
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
-        s[r] = exp2_fast(s[r] * c2);
-        dp[r] *= s[r];
+        s[r] = exp2_fast(M::kNarrow ? fmaf(s[r], c2, float(kLiftP)) : s[r] * c2);
+        dp[r] *= M::kNarrow ? s[r] * lift_ds : s[r];
       }
       const int b0 = row0 + 32 * part;
       if (b0 == k0 || b0 + 32 > t.len) {  // the diagonal, or rows past the end
@@ -1234,6 +1321,10 @@ __global__ void __launch_bounds__(256, 2) at_dkv_wide(const Attention a) {
   for (int i = 0; i < n_tiles; i += 2) {
     step(i, lq0, ld0, stat0, lq1, ld1, stat1);
     if (i + 1 < n_tiles) step(i + 1, lq1, ld1, stat1, lq0, ld0, stat0);
+  }
+  if constexpr (M::kNarrow) {
+    scale_sums<2>(dk, __builtin_ldexpf(1.0f, -lift));
+    scale_sums<2>(dv, __builtin_ldexpf(1.0f, -kLiftP));
   }
   if (ki < t.len) store_dkv<M, 2>(a, kr, kv, which, 64 * part, dk, dv);
 }
@@ -1461,11 +1552,15 @@ template <class M, int DP, int DW>
 int launch_grad(Attention a, hipStream_t st) {
   const int splits = splits_of<DP>(a, a.heads * a.q_parts);
   const bool two_k = DP == 128 || splits_of<DP>(a, a.kv_heads * a.parts) > 1;
+  int rc;
+  Scratch sc(st);
+  if (M::kNarrow) {
+    a.tops_of = splits * a.q_parts;
+    if ((rc = step_alloc(&sc, &a.tops, size_t(a.tops_of) * size_t(a.heads) * size_t(a.T)))) return rc;
+  }
   Attention ak = a;
   const dim3 gq = tile_grid(&a, 128 / splits, a.heads * a.q_parts);
   const dim3 gk = tile_grid(&ak, two_k ? 64 : 128, a.kv_heads * a.parts);
-  int rc;
-  Scratch sc(st);
   if (needs_order(a)) {
     OrderJob jq{nullptr, a.tiles, __builtin_ctz(128 / splits), true}, jk{nullptr, ak.tiles, two_k ? 6 : 7, false};
     if ((rc = step_alloc(&sc, &jq.order, a.tiles))) return rc;
