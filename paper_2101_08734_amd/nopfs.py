@@ -557,6 +557,28 @@ def batch_tables(ids, tokens, free, block: int, width: int, cap: int, out=None, 
     return o
 
 
+def _differentiated(*tensors) -> bool:
+    return torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in tensors)
+
+
+def _no_outputs_given(name, *outputs):
+    if any(t is not None for t in outputs):
+        raise ValueError(f"{name}: given outputs are not part of the graph of an input that "
+                         "requires a gradient (detach it, or call under torch.no_grad())")
+
+
+def _call_in_backward(stream, call):
+    """A call that the forward pass made on `stream`, behind what the backward
+    pass has on its own stream and before what follows there."""
+    if stream is None:
+        return call()
+    here = torch.cuda.current_stream()
+    stream.wait_stream(here)
+    out = call()
+    here.wait_stream(stream)
+    return out
+
+
 _HALVES = (torch.bfloat16, torch.float16)
 
 
@@ -585,12 +607,41 @@ def _strides(*tensors):
     return out
 
 
+class _PackedAttention(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, q, k, v, start, scale, stream):
+        o, lse = packed_attention(q, k, v, start, scale, stream=stream)
+        ctx.save_for_backward(q, k, v, o, lse, start)
+        ctx.scale, ctx.stream = scale, stream
+        ctx.set_materialize_grads(False)
+        return o, lse
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, do, dlse):
+        if dlse is not None:
+            raise RuntimeError("packed_attention: lse has no gradient (detach it)")
+        if do is None:
+            return (None,) * 6
+        q, k, v, o, lse, start = ctx.saved_tensors
+        token, head, element = do.stride()
+        if element != 1 or token % 8 or head % 8 or min(token, head) < do.shape[2] or do.data_ptr() % 16:
+            do = do.clone(memory_format=torch.contiguous_format)
+        grads = _call_in_backward(ctx.stream, lambda: packed_attention_grad(
+            do, q, k, v, o, lse, start, ctx.scale, stream=ctx.stream))
+        return (*grads, None, None, None)
+
+
 def packed_attention(q, k, v, start, scale=None, o=None, lse=None, stream=None):
     """Causal attention over packed samples (nopfs_packed_attention): q
     [T][heads][width], k and v [T][kv_heads][width], bfloat16 or float16, any
     token and head strides of whole 16 bytes (slices of one projection, say);
     start [n+1] int32, a row of batch_tables' start. Returns o (as q) and lse
-    [heads][T] float32. scale: 1/sqrt(width) unless given."""
+    [heads][T] float32. scale: 1/sqrt(width) unless given. Autograd takes o back to
+    q, k and v by packed_attention_grad."""
+    if _differentiated(q, k, v):
+        _no_outputs_given("packed_attention", o, lse)
+        return _PackedAttention.apply(q, k, v, start, scale, stream)
     dev = torch.cuda.current_device()
     a = _attention(q, k, v, start, scale, dev)
     if o is None:
@@ -614,7 +665,7 @@ def packed_attention_grad(do, q, k, v, o, lse, start, scale=None, dq=None, dk=No
                           stream=None):
     """Gradient of packed_attention (nopfs_packed_attention_grad) from its
     outputs and the gradient `do` of o. Returns dq, dk, dv (as q, k, v; slices
-    of one preallocated array, say)."""
+    of one preallocated array, say), which autograd does not differentiate again."""
     dev = torch.cuda.current_device()
     a = _attention(q, k, v, start, scale, dev)
     same = (q.dtype,)
@@ -639,13 +690,42 @@ def packed_attention_grad(do, q, k, v, o, lse, start, scale=None, dq=None, dk=No
     return dq, dk, dv
 
 
+class _TopkDistill(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, logits, index, teacher, tau, weight, stream):
+        loss, dlogits = topk_distill(logits, index, teacher, tau, weight, stream=stream)
+        ctx.save_for_backward(dlogits)
+        ctx.mark_non_differentiable(dlogits)
+        ctx.set_materialize_grads(False)
+        ctx.stream = stream
+        return loss, dlogits
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dloss, _):
+        if dloss is None:
+            return (None,) * 6
+        dlogits, = ctx.saved_tensors
+        if ctx.stream is not None:
+            torch.cuda.current_stream().wait_stream(ctx.stream)
+        return ((dlogits * dloss[:, None]).to(dlogits.dtype), None, None, None, None, None)
+
+
 def topk_distill(logits, index, teacher, tau=1.0, weight=None, grad=True, loss=None, dlogits=None,
                  stream=None):
     """Distillation from a teacher's top logits (nopfs_topk_distill): logits
     [T][V], index [T][K] int32 and teacher [T][K], the teacher's K classes per
     row and their logits; weight [T] float32 scales a row's loss (0: the row is
     masked). Returns loss [T] float32 and, unless grad is False, its gradient
-    by the logits (in their type; dlogits may be logits itself)."""
+    by the logits (in their type; dlogits may be logits itself). Autograd takes the
+    loss back to the logits by that gradient; with grad False the loss is outside
+    its graph. Teacher and weight are data and may not require gradients."""
+    if _differentiated(logits, teacher, weight):
+        if _differentiated(teacher, weight):
+            raise ValueError("topk_distill has no gradient by teacher and weight (detach them)")
+        if grad:
+            _no_outputs_given("topk_distill", loss, dlogits)
+            return _TopkDistill.apply(logits, index, teacher, tau, weight, stream)
     dev = torch.cuda.current_device()
     T, V = _step_tensor(logits, "logits", _DTYPES, 2, dev).shape
     K = _step_tensor(index, "index", _I32, 2, dev).shape[1]
