@@ -490,18 +490,20 @@ def _step_stream(stream, device, tensors):
     return stream.cuda_stream
 
 
+# Whether the current stream is being captured into a graph.
+_capturing = getattr(torch._C, "_cuda_isCurrentStreamCapturing", None) or torch.cuda.is_current_stream_capturing
+
+
 def _step_scratch(desc, device, stream, size, *args):
     """Scratch for a call that is being captured into a graph, from torch's
-    allocator, which keeps it as long as the graph; else None (the library's own).
-    size(desc, ..., bytes) tells how much. The current stream is asked: a call
+    allocator, which keeps it as long as the graph (elsewhere the library has its
+    own). The function `size` tells how much. The current stream is asked: a call
     captured on another one while the current one is not is refused."""
-    if not torch.cuda.is_current_stream_capturing():
-        return None
     if stream is not None and stream.cuda_stream != _raw_stream(device):
         with torch.cuda.stream(stream):
             return _step_scratch(desc, device, None, size, *args)
     need = ctypes.c_int64()
-    _check(size(ctypes.byref(desc), *args, ctypes.byref(need)), "scratch")
+    _check(getattr(lib(), size)(ctypes.byref(desc), *args, ctypes.byref(need)), size)
     t = torch.empty(need.value, dtype=torch.uint8, device=device)
     desc.scratch, desc.scratch_bytes = t.data_ptr(), need.value
     return t
@@ -549,16 +551,13 @@ def batch_tables(ids, tokens, free, block: int, width: int, cap: int, out=None, 
             _step_dense(t, name, dt, shape, dev)
     b = _Batch(F, _row_stride(lead), _row_stride(free), G, n, free.shape[1], block, width, cap)
     st = _step_stream(stream, dev, (ids, tokens, free, *o.values()))
-    scratch = _step_scratch(b, dev, stream, lib().nopfs_batch_tables_scratch)  # noqa: F841 held until enqueued
+    scratch = _capturing() and _step_scratch(  # noqa: F841 held until the call is enqueued
+        b, dev, stream, "nopfs_batch_tables_scratch")
     _check(lib().nopfs_batch_tables(
         ctypes.byref(b), None if ids is None else ids.data_ptr(), tokens.data_ptr(),
         free.data_ptr(), o["start"].data_ptr(), o["table"].data_ptr(), o["slot"].data_ptr(),
         o["row"].data_ptr(), o["pos"].data_ptr(), o["used"].data_ptr(), st), "nopfs_batch_tables")
     return o
-
-
-def _differentiated(*tensors) -> bool:
-    return torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in tensors)
 
 
 def _no_outputs_given(name, *outputs):
@@ -639,7 +638,7 @@ def packed_attention(q, k, v, start, scale=None, o=None, lse=None, stream=None):
     start [n+1] int32, a row of batch_tables' start. Returns o (as q) and lse
     [heads][T] float32. scale: 1/sqrt(width) unless given. Autograd takes o back to
     q, k and v by packed_attention_grad."""
-    if _differentiated(q, k, v):
+    if (q.requires_grad or k.requires_grad or v.requires_grad) and torch.is_grad_enabled():
         _no_outputs_given("packed_attention", o, lse)
         return _PackedAttention.apply(q, k, v, start, scale, stream)
     dev = torch.cuda.current_device()
@@ -654,7 +653,8 @@ def packed_attention(q, k, v, start, scale=None, o=None, lse=None, stream=None):
         _step_dense(lse, "lse", torch.float32, (a[2], a[0]), dev)
     a = _Attention(*a, *_strides(q, k, v, o))
     st = _step_stream(stream, dev, (q, k, v, start, o, lse))
-    scratch = _step_scratch(a, dev, stream, lib().nopfs_packed_attention_scratch, 0)  # noqa: F841
+    scratch = _capturing() and _step_scratch(  # noqa: F841
+        a, dev, stream, "nopfs_packed_attention_scratch", 0)
     _check(lib().nopfs_packed_attention(ctypes.byref(a), q.data_ptr(), k.data_ptr(), v.data_ptr(),
                                         start.data_ptr(), o.data_ptr(), lse.data_ptr(), st),
            "nopfs_packed_attention")
@@ -682,7 +682,8 @@ def packed_attention_grad(do, q, k, v, o, lse, start, scale=None, dq=None, dk=No
     dq, dk, dv = grads
     a = _Attention(*a, *_strides(q, k, v, o, do, dq, dk, dv))
     st = _step_stream(stream, dev, (do, q, k, v, o, lse, start, dq, dk, dv))
-    scratch = _step_scratch(a, dev, stream, lib().nopfs_packed_attention_scratch, 1)  # noqa: F841
+    scratch = _capturing() and _step_scratch(  # noqa: F841
+        a, dev, stream, "nopfs_packed_attention_scratch", 1)
     _check(lib().nopfs_packed_attention_grad(
         ctypes.byref(a), do.data_ptr(), q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(),
         lse.data_ptr(), start.data_ptr(), dq.data_ptr(), dk.data_ptr(), dv.data_ptr(), st),
@@ -720,12 +721,12 @@ def topk_distill(logits, index, teacher, tau=1.0, weight=None, grad=True, loss=N
     by the logits (in their type; dlogits may be logits itself). Autograd takes the
     loss back to the logits by that gradient; with grad False the loss is outside
     its graph. Teacher and weight are data and may not require gradients."""
-    if _differentiated(logits, teacher, weight):
-        if _differentiated(teacher, weight):
+    if teacher.requires_grad or weight is not None and weight.requires_grad:
+        if torch.is_grad_enabled():
             raise ValueError("topk_distill has no gradient by teacher and weight (detach them)")
-        if grad:
-            _no_outputs_given("topk_distill", loss, dlogits)
-            return _TopkDistill.apply(logits, index, teacher, tau, weight, stream)
+    if grad and logits.requires_grad and torch.is_grad_enabled():
+        _no_outputs_given("topk_distill", loss, dlogits)
+        return _TopkDistill.apply(logits, index, teacher, tau, weight, stream)
     dev = torch.cuda.current_device()
     T, V = _step_tensor(logits, "logits", _DTYPES, 2, dev).shape
     K = _step_tensor(index, "index", _I32, 2, dev).shape[1]
