@@ -196,7 +196,8 @@ __device__ __forceinline__ bool pick_tile(const Attention& a, uint32_t rank, Til
 // workgroup; which of two tiles of one class comes first is left open (no
 // result depends on it). Bound by the latency of its searches: the starts are
 // in LDS where they fit (16,384 tokens of 32 samples: 9.2 -> 6.5 us,
-// launch included).
+// launch included). Beyond kHeldStarts samples they are read from global memory,
+// and all tiles are one workgroup's work, however many.
 constexpr int kClasses = 1024, kHeldStarts = 4096;
 struct OrderJob {
   int4* order;
@@ -523,13 +524,13 @@ constexpr int kTileKeys = kSplits == 4 ? 128 : 64;
 
 // ------------------------------------------------------------------ forward --
 // One pass over the keys up to the diagonal with the running maximum and sum.
-// 16,384 tokens of three samples, 16 heads of 128 on 2: 583 us, 1.02 PFLOP/s of
-// the 1.38 of a large product; matrix units 47% busy, vector units
-// (exponentials, maxima, roundings) 42%, LDS 47%: the phases of a SIMD's two
-// waves overlap in part only. 8,192 x 16 heads of 64: 172
-// us, 0.80 PFLOP/s, vector units 61%: half the products per exponential. 16,384
-// tokens of 32 documents: 105 us, matrix units 28%: the longest documents' last
-// tiles run on when the others are done.
+// 16,384 tokens of three samples, 16 heads of 128 on 2: 602 to 629 us on
+// different cards, 0.97 PFLOP/s of the 1.38 of a large product; matrix units 46%
+// busy, vector units (exponentials, maxima, roundings) 42%, LDS 46%: the phases of a
+// SIMD's two waves overlap in part only. 8,192 x 16 heads of 64: 167 to 176 us, 0.80
+// PFLOP/s, vector units 57%: half the products per exponential. 16,384 tokens of 32
+// documents: 105 to 116 us, matrix units 28%; 228 MB read behind the L2s where the
+// arrays hold 101: a sample's tiles on different dies read its keys again.
 template <class M, int DP, int DW, int kSplits>
 __global__ void __launch_bounds__(256, kSplits == 4 && DP == 128 ? 1 : 2) at_forward(const Attention a) {
   typedef typename M::T T;
@@ -751,11 +752,12 @@ __global__ void __launch_bounds__(256) at_join(const Attention a) {
 // 32 bits; dq_i = scale (sum_j dS_ij k_j - eps_i sum_j P_ij k_j), and a second pass
 // makes the latter sum over the key tiles where a query of the workgroup has more
 // than kHeavy of its weight on a key (the rest of it is small beside what the
-// rounding of dS leaves). 8,192 x 16 heads of 64: 216 us, 0.95
-// PFLOP/s of three products. 16,384 tokens of 32 documents x 16 of 128: 162 us,
-// again the longest documents. Standard normal scores; without eps and the second
-// pass 204 and 152; with kHeavy 1/16 217 and 171, and no smaller errors. Three
-// workgroups of narrow heads a compute unit: 216 us, with two 240.
+// rounding of dS leaves). 8,192 x 16 heads of 64: 216 to 230 us, 0.92 PFLOP/s of
+// three products; matrix units 43%, vector units 54%. 16,384 tokens of 32 documents
+// x 16 of 128: 162 to 172 us, matrix units 28%; 393 MB read behind the L2s, where
+// the arrays hold 235. With standard normal scores and on one card eps and the
+// second pass took 204 to 216 and 152 to 162 us; kHeavy 1/16 217 and 171, with no
+// smaller errors; heads of 64 with two workgroups a compute unit instead of three 240.
 constexpr float kHeavy = 1.0f / 8;
 template <class M, int DP, int DW, int kSplits>
 __global__ void __launch_bounds__(256, DP == 64 && kSplits < 4 ? 3 : kSplits == 4 && DP == 128 ? 1 : 2) at_dq(const Attention a) {
@@ -1012,7 +1014,7 @@ __global__ void __launch_bounds__(256, DP == 64 && kSplits < 4 ? 3 : kSplits == 
 // One workgroup: 128 keys (64 with two splits) of one kv head, over the query
 // heads of its group in order and the query tiles from the diagonal on, or over
 // one part of that list. Four products a block of 32 x 32: 8,192 x 16 heads of
-// 64 303 us, 0.91 PFLOP/s; matrix units 43%, vector units 46%.
+// 64 295 to 313 us, 0.90 PFLOP/s; matrix units 43%, vector units 45%.
 template <class M, int DP, int DW, int kSplits>
 __global__ void __launch_bounds__(256, 2) at_dkv(const Attention a) {
   typedef typename M::T T;
@@ -1173,7 +1175,9 @@ __global__ void __launch_bounds__(256, 2) at_dkv(const Attention a) {
 // sums per wave, and two workgroups share a compute unit. Their LDS is exactly
 // half of it, so lse and delta stay in registers, one row per lane. 8,192 x 16
 // heads of 128: 600 us, 0.92 PFLOP/s (876 with a strip per wave); the meeting
-// of the waves between the two phases is what it waits for.
+// of the waves between the two phases is what it waits for. 16,384 tokens of 32
+// documents: 183 to 205 us, 534 MB read behind the L2s, where the arrays hold 168:
+// each key tile of a sample goes through its queries from another one on.
 template <class M, int DW>
 __global__ void __launch_bounds__(256, 2) at_dkv_wide(const Attention a) {
   typedef typename M::T T;
@@ -1463,11 +1467,11 @@ bool needs_order(const Attention& a) { return a.n > 1 && a.T >= 4096 && a.T / a.
 // Parts of a query tile's keys for o and dq, where few rows and heads leave the
 // longest sample's last tiles alone on the chip (its length guessed as in
 // dkv_parts): 24 key tiles or more a part, since a launch that joins them
-// follows (6 to 20 us). Forward and dq, joined: 7,825 tokens of three samples x
-// 3 heads of 80 147 -> 105 us, 5,000 x 4 of 128 160 -> 130, 16,000 x 2 of 64
-// 306 -> 236; like samples, for which the guess is too long, lose a little: three
-// of 2,048 x 8 of 128 103 -> 134, four 114 -> 135. In parts of 12 tiles 4,096
-// tokens of 8 samples x 8 of 128 took 78 for 46.
+// follows (9 to 18 us). Forward and dq, joined: 7,825 tokens of three samples x
+// 3 heads of 80 161 -> 110 us, 5,000 x 4 of 128 173 -> 134, 16,000 x 2 of 64
+// 345 -> 255; like samples, for which the guess is too long, lose: three of 2,048 x
+// 8 of 128 107 -> 142, four 122 -> 144. In parts of 12 tiles 4,096 tokens of 8
+// samples x 8 of 128 took 78 for 46.
 int32_t q_parts(const Attention& a) {
   const int64_t rows = a.T * a.heads;
   const int64_t longest = a.n > 4 ? 4 * a.T / a.n : a.T;

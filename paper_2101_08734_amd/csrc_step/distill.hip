@@ -7,9 +7,13 @@
 //     ds_v  = w tau (exp(s_v / tau - z) - sum_{k: x_k = v} p_k)
 // One workgroup per row, bound by memory: a row is read once and its gradient
 // written once (8,192 rows of 32,768 classes in bf16, a tenth of them masked: 1.02
-// GB in 217 us, 4.7 TB/s; a large copy reaches 4.9 here), except that rows too
-// long for one workgroup's registers are read twice. Maxima, sums, probabilities and the
-// loss are held in 32 bits; the gradient is rounded once, at the store.
+// GB in 220 us, 4.6 TB/s; a large copy reaches 4.9 here), except that rows too
+// long for one workgroup's registers are read twice, and that many teacher entries
+// take longer than the row: a class named twice is looked for among all others, K^2
+// comparisons (8,192 rows without a mask: of 32,768 classes 239 us with 64 entries, 261
+// with 128, 506 with 512, 1,246 with 1,024; of 2,048 classes 26, 41, 468, 3,301).
+// Maxima, sums, probabilities and the loss are held in 32 bits; the gradient is
+// rounded once, at the store.
 #include "step.hpp"
 
 namespace nopfs {
@@ -304,12 +308,13 @@ int launch_row(const Distill& d, hipStream_t st) {
 
 // By the row's 16-byte vectors: held in registers as long as one workgroup can
 // (131,072 classes in 16 bits), by the fewest threads that hold it in at most 8
-// vectors each (12 for the step between 256 and 512 threads), then 16. 8,192
-// rows of 32,768 classes in bf16 took 211 us with 512 x 8, 226 with 256 x 16,
+// vectors each (12 for the step between 256 and 512 threads: 8,192 rows of 21,841
+// classes in bf16 160 us and 84 without a gradient, with 512 x 8 167 and 94; of
+// 24,500 168 and 76, with 512 x 8 159 and 81), then 16. 8,192 rows of 32,768 classes in bf16 took 211 us with 512 x 8, 226 with 256 x 16,
 // 245 with 1024 x 4, and 255 to 426 when read twice; 4,096 rows of 131,072 in
 // fp16 491 with 1024 x 16, 549 when read twice. The loss alone is summed in the
 // same order, so that it has the same bits with a gradient and without (8,192
-// rows of 21,841: 82 us; one pass with nothing held took 74).
+// rows of 21,841: 84 us; one pass with nothing held took 74).
 template <class E, class Y>
 int launch_rows(const Distill& d, hipStream_t st) {
   const int64_t nv = d.V / Packed<E>::kN;

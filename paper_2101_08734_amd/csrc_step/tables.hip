@@ -8,7 +8,9 @@
 //     read r is admitted iff ct_s <= cap, cb_s <= blocks, nb_s <= width for
 //     every s <= r.
 //   1. bt_scan   -- one workgroup per group: lengths gathered, both running
-//                   sums and the cut; packed starts and first free entries.
+//                   sums and the cut; packed starts and first free entries
+//                   (1,024 reads a round, one round after the other: a single
+//                   group of very many reads is one workgroup's work).
 //   2. bt_expand -- one workgroup per 8,192 packed tokens or table entries,
 //                   four adjacent ones per thread: the tile's starts go to
 //                   LDS, a token's read is searched there.
