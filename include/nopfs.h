@@ -504,6 +504,139 @@ int nopfs_topk_distill(const nopfs_distill* distill, const void* logits, const i
                        const void* teacher, const float* weight, float* loss, void* grad,
                        void* hip_stream);
 
+/* ---- Layers of a token model over the packed samples -------------------- *
+ * What stands between nopfs_batch_tables and nopfs_packed_attention, each with
+ * its gradient: the embedding of the packed tokens, norms and rotations of their
+ * queries and keys, and a gated linear recurrence in attention's place. The
+ * conventions of the step's calls hold. Strides are in elements; rows and heads
+ * begin at any element. Outputs overlap no input except where stated. */
+
+typedef struct nopfs_embed {
+  int64_t T;             /* rows (tokens, padding included), < 2^31            */
+  int64_t V;             /* rows of the embedding, 1 .. 2^31 - 2               */
+  int64_t n_ids;         /* entries of ids: T, or with slot those of the buffer */
+  int64_t weight_stride; /* of weight or its gradient, row to row, >= width    */
+  int64_t out_stride;    /* of out or its gradient, the same                   */
+  int32_t width;         /* elements of a row, >= 1                            */
+  int32_t weight_dtype;  /* of weight and its gradient                         */
+  int32_t dtype;         /* of out and its gradient                            */
+  int32_t id_bytes;      /* of an entry of ids: 4 (int32) or 8 (int64)         */
+  float scale;           /* finite                                             */
+  int32_t reserved;      /* 0                                                  */
+  void* scratch;         /* the gradient's scratch, a multiple of 256 bytes,   */
+  int64_t scratch_bytes; /* or NULL; its size                                  */
+} nopfs_embed;
+
+/* out_t = scale weight[id_t], rounded once, with id_t = ids[t], or ids[slot[t]]
+ * where slot is given (a token buffer and the slots of nopfs_batch_tables). A
+ * slot outside [0, n_ids) or an id outside [0, V) is padding: out_t = 0.
+ *   ids:  int32 or int64 [n_ids];  slot: int64 [T], or NULL.
+ * No scratch. Errors: EINVAL, ERANGE, EDEVICE. */
+int nopfs_token_embed(const nopfs_embed* e, const void* weight, const void* ids,
+                      const int64_t* slot, void* out, void* hip_stream);
+
+/* The gradient of weight, all of it: d_weight[v] = scale times the sum of d_out[t]
+ * over the t with id_t = v in 32 bits, in an order that the ids alone decide,
+ * rounded once; 0 where there is none. What d_out holds of padding is not read.
+ * Errors: EINVAL, ERANGE, ENOMEM, EDEVICE. */
+int nopfs_token_embed_grad(const nopfs_embed* e, const void* d_out, const void* ids,
+                           const int64_t* slot, void* d_weight, void* hip_stream);
+/* The gradient's scratch, on the host. Errors: EINVAL, ERANGE. */
+int nopfs_token_embed_scratch(const nopfs_embed* e, int64_t* bytes);
+
+/* Queries and keys of T tokens; [0] of a stride from token to token, [1] from
+ * head to head, the `width` elements of a head are adjacent. */
+typedef struct nopfs_rotate {
+  int64_t T;            /* tokens, padding included, < 2^31                   */
+  int32_t heads;        /* of q, >= 1                                         */
+  int32_t kv_heads;     /* of k, >= 1                                         */
+  int32_t width;        /* elements of a head: a multiple of 8, 8..256        */
+  int32_t rotated;      /* of them rotated, the first: a multiple of 8, 0..width */
+  int32_t interleaved;  /* pairs (2i, 2i+1) if 1, (i, i + rotated/2) if 0     */
+  int32_t dtype;        /* of q, k and what is made of them                   */
+  int32_t weight_dtype; /* of the weights and their gradients                 */
+  float eps;            /* 2^-60 .. 2^60                                      */
+  int64_t q_stride[2], k_stride[2];
+  int64_t q_out_stride[2], k_out_stride[2]; /* and of their gradients         */
+  int64_t dq_stride[2], dk_stride[2];       /* gradient only                  */
+  void* scratch;         /* the gradient's scratch, a multiple of 256 bytes,  */
+  int64_t scratch_bytes; /* or NULL; its size                                 */
+} nopfs_rotate;
+
+/* Norm and rotation of every head x of a token at position p >= 0: with
+ * r = 1 / sqrt(mean of x_i^2 + eps) and y_i = x_i r weight_i, pair i < rotated/2
+ * turns by the angle p freq_i,
+ *   out_a = y_a cos - y_b sin,  out_b = y_b cos + y_a sin,
+ * and the elements from `rotated` on are y. Rows with p < 0 (padding, as
+ * nopfs_batch_tables marks it) get 0; what q and k hold there is not read.
+ *   pos:  int32 [T];  freq: double [rotated/2], radians per position (NULL if 0).
+ *   q_weight, k_weight: [width], or NULL for 1.
+ *   q_out, k_out: may be q and k themselves with the same strides (in place).
+ * No scratch. Errors: EINVAL, ERANGE, EDEVICE. */
+int nopfs_norm_rotate(const nopfs_rotate* r, const void* q, const void* k, const int32_t* pos,
+                      const double* freq, const void* q_weight, const void* k_weight,
+                      void* q_out, void* k_out, void* hip_stream);
+
+/* Its gradient, from the inputs and the gradients d_q_out and d_k_out. With g
+ * the gradient turned back by the same angles and z_i = x_i r:
+ *   d_x_i = r (g_i weight_i - z_i mean of g_j weight_j z_j),
+ *   d_weight_i = the sum of g_i z_i over tokens and heads, in 32 bits.
+ *   d_q, d_k: may be d_q_out and d_k_out themselves with the same strides.
+ *   d_q_weight, d_k_weight: [width], or NULL (not asked for).
+ * Rows with pos < 0 get 0 and add nothing. Errors: EINVAL, ERANGE, ENOMEM, EDEVICE. */
+int nopfs_norm_rotate_grad(const nopfs_rotate* r, const void* d_q_out, const void* d_k_out,
+                           const void* q, const void* k, const int32_t* pos, const double* freq,
+                           const void* q_weight, const void* k_weight, void* d_q, void* d_k,
+                           void* d_q_weight, void* d_k_weight, void* hip_stream);
+/* The gradient's scratch (for both weights), on the host. Errors: EINVAL, ERANGE. */
+int nopfs_norm_rotate_scratch(const nopfs_rotate* r, int64_t* bytes);
+
+/* A gated linear recurrence over n packed samples, for each channel by itself. */
+typedef struct nopfs_scan {
+  int64_t T;           /* rows (tokens, padding included), < 2^31               */
+  int32_t n;           /* samples, 0 .. 2^30                                    */
+  int32_t channels;    /* >= 1                                                  */
+  int32_t dtype;       /* of x, gate, h and their gradients                     */
+  int32_t reserved;    /* 0                                                     */
+  int64_t x_stride, gate_stride, h_stride; /* row to row, >= channels           */
+  int64_t dh_stride, dx_stride, dgate_stride; /* gradient only                  */
+  void* scratch;         /* the call's scratch, a multiple of 256 bytes, or     */
+  int64_t scratch_bytes; /* NULL; its size                                      */
+} nopfs_scan;
+
+/* Tokens from one kept state to the next. */
+#define NOPFS_SCAN_CHUNK 16
+
+/* With a = 1 / (1 + exp(-gate)), sample s of tokens start[s]..start[s+1]-1 has
+ *   h_t = a_t h_(t-1) + (1 - a_t) x_t
+ * from h0[s] (or 0) before its first token. The state is held in 32 bits, as are
+ * a and 1 - a (0 below 2^-126); h is rounded from it.
+ *   start: int32 [n+1], as for nopfs_packed_attention.
+ *   h0:    float [n][channels], or NULL for 0.
+ *   last:  float [n][channels], the state behind each sample's last token (h0 of
+ *          a sample without tokens), or NULL.
+ *   carry: float [ceil(T / NOPFS_SCAN_CHUNK)][channels], the states that the
+ *          gradient starts from, or NULL.
+ * Rows from start[n] on get h = 0 and are not read. A NaN or infinity reaches no
+ * other sample. Errors: EINVAL, ERANGE, ENOMEM, EDEVICE. */
+int nopfs_gated_scan(const nopfs_scan* s, const void* x, const void* gate, const int32_t* start,
+                     const float* h0, void* h, float* last, float* carry, void* hip_stream);
+
+/* Its gradient, from d_h, the gradient of h, and d_last, that of last (or NULL
+ * for 0), and from the forward call's inputs and carry. With G_t = d_h_t +
+ * a_(t+1) G_(t+1) within a sample, d_last[s] in place of the product at its end:
+ *   d_x_t = (1 - a_t) G_t,  d_gate_t = a_t (1 - a_t) (h_(t-1) - x_t) G_t,
+ *   d_h0[s] = a G of its first token (d_last[s] without tokens).
+ *   d_h0: float [n][channels], or NULL.
+ * Rows from start[n] on get 0. Errors: EINVAL, ERANGE, ENOMEM, EDEVICE. */
+int nopfs_gated_scan_grad(const nopfs_scan* s, const void* d_h, const float* d_last,
+                          const void* x, const void* gate, const int32_t* start, const float* h0,
+                          const float* carry, void* d_x, void* d_gate, float* d_h0,
+                          void* hip_stream);
+/* The scratch of the forward call, or of the gradient, on the host. Errors:
+ * EINVAL, ERANGE. */
+int nopfs_gated_scan_scratch(const nopfs_scan* s, int32_t gradient, int64_t* bytes);
+
 /* Static description of a status code. Never NULL. */
 const char* nopfs_strerror(int code);
 

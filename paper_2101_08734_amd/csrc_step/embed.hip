@@ -1,0 +1,323 @@
+// nopfs_token_embed and its gradient: the rows of an embedding that the packed
+// tokens name, and the sums of their gradients by name.
+//     out_t = scale W[id_t],   dW_v = scale sum_{t: id_t = v} dout_t
+// Both are bound by memory. The gradient's sums must not depend on the order in
+// which work finishes, so the tokens are sorted by id first (radix sort, stable:
+// a token's rows are added in the order of the batch).
+#include "rows.hpp"
+
+namespace nopfs {
+namespace {
+
+struct Embed {
+  int64_t T, V, n_ids, weight_stride, out_stride;
+  int32_t width;
+  float scale;
+  const void* ids;
+  const int64_t* slot;
+  bool wide;
+};
+
+// The row of the embedding that token t names, -1 for padding.
+__device__ __forceinline__ int64_t name_of(const Embed& d, int64_t t) {
+  int64_t at = t;
+  if (d.slot) {
+    at = d.slot[t];
+    if (at < 0 || at >= d.n_ids) return -1;
+  }
+  const int64_t id = d.wide ? static_cast<const int64_t*>(d.ids)[at] : static_cast<const int32_t*>(d.ids)[at];
+  return id >= 0 && id < d.V ? id : -1;
+}
+
+constexpr int kVec = 8;  // elements per lane and step
+
+// Rows by groups of 2^lg lanes, kPer rows of a group at a time.
+template <class W, class E, int kPer>
+__global__ void __launch_bounds__(256) te_forward(const Embed d, const typename W::T* weight, typename E::T* out,
+                                                  int lg) {
+  const int lanes = 1 << lg;
+  const int64_t t0 = (int64_t(row_block()) * (256 >> lg) + (threadIdx.x >> lg)) * kPer;
+  if (t0 >= d.T) return;
+  int64_t id[kPer];
+#pragma unroll
+  for (int j = 0; j < kPer; ++j) id[j] = t0 + j < d.T ? name_of(d, t0 + j) : -1;
+  for (int32_t c = int32_t(threadIdx.x & (lanes - 1)) * kVec; c < d.width; c += lanes * kVec) {
+    const int some = d.width - c;
+    Pack<W, kVec> w[kPer];
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) {
+      w[j].zero();
+      const typename W::T* p = weight + id[j] * d.weight_stride + c;
+      if (id[j] >= 0) {
+        if (some >= kVec) w[j].load(p);
+        else w[j].load_some(p, some);
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) {
+      if (t0 + j >= d.T) break;
+      float v[kVec];
+#pragma unroll
+      for (int e = 0; e < kVec; ++e) v[e] = id[j] >= 0 ? w[j].get(e) * d.scale : 0.0f;
+      Pack<E, kVec> o;
+      o.set(v);
+      typename E::T* p = out + (t0 + j) * d.out_stride + c;
+      if (some >= kVec) o.store(p);
+      else o.store_some(p, some);
+    }
+  }
+}
+
+// ---- the tokens in the order of their ids ------------------------------------
+// Least significant digit first, at most 10 bits a pass: a tile's counts of each
+// digit, then each tile's own place among them. The keys are the ids, V for
+// padding, which so comes last.
+constexpr int kMostBits = 10;
+constexpr int kSortTile = 1024;
+
+struct Sort {
+  const uint32_t *key_in, *val_in;  // the pass before (not in the first)
+  uint32_t *key, *val;
+  uint32_t* hist;  // [tiles][1 << bits]
+  int32_t tiles, per_tile, shift, bits;
+};
+
+template <bool kFirst>
+__device__ __forceinline__ uint32_t sort_key(const Embed& d, const Sort& s, int64_t i) {
+  if (!kFirst) return s.key_in[i];
+  const int64_t id = name_of(d, i);
+  return uint32_t(id >= 0 ? id : d.V);
+}
+
+template <bool kFirst>
+__global__ void __launch_bounds__(256) te_count(const Embed d, const Sort s) {
+  __shared__ uint32_t count[1 << kMostBits];
+  const int bins = 1 << s.bits;
+  for (int b = threadIdx.x; b < bins; b += 256) count[b] = 0;
+  __syncthreads();
+  const int64_t i0 = int64_t(blockIdx.x) * s.per_tile;
+  const int64_t i1 = i0 + s.per_tile < d.T ? i0 + s.per_tile : d.T;
+  for (int64_t i = i0 + threadIdx.x; i < i1; i += 256)
+    atomicAdd(&count[sort_key<kFirst>(d, s, i) >> s.shift & (bins - 1)], 1u);
+  __syncthreads();
+  for (int b = threadIdx.x; b < bins; b += 256) s.hist[int64_t(blockIdx.x) * bins + b] = count[b];
+}
+
+template <bool kFirst>
+__global__ void __launch_bounds__(256) te_scatter(const Embed d, const Sort s) {
+  __shared__ uint32_t base[1 << kMostBits], cnt[4][1 << kMostBits], tmp[65];
+  const int bins = 1 << s.bits, wave = threadIdx.x >> 6;
+  uint32_t mine[(1 << kMostBits) / 256];  // of the digit, in the tiles before this one
+#pragma unroll
+  for (int j = 0; j < (1 << kMostBits) / 256; ++j) {
+    const int b = j * 256 + threadIdx.x;
+    if (b >= bins) break;
+    uint32_t before = 0, all = 0;
+    for (int32_t t = 0; t < s.tiles; ++t) {
+      const uint32_t c = s.hist[int64_t(t) * bins + b];
+      before += t < int32_t(blockIdx.x) ? c : 0;
+      all += c;
+    }
+    mine[j] = before;
+    base[b] = all;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) cnt[w][b] = 0;
+  }
+  __syncthreads();
+  block_scan_array(base, uint32_t(bins), tmp);
+#pragma unroll
+  for (int j = 0; j < (1 << kMostBits) / 256; ++j) {
+    const int b = j * 256 + threadIdx.x;
+    if (b < bins) base[b] += mine[j];
+  }
+  __syncthreads();
+  const int64_t i0 = int64_t(blockIdx.x) * s.per_tile;
+  const int64_t i1 = i0 + s.per_tile < d.T ? i0 + s.per_tile : d.T;
+  for (int64_t r = i0; r < i1; r += 256) {
+    const int64_t i = r + threadIdx.x;
+    const bool in = i < i1;
+    const uint32_t key = in ? sort_key<kFirst>(d, s, i) : 0;
+    const uint32_t digit = key >> s.shift & (bins - 1);
+    uint64_t same = __ballot(in);  // the wave's lanes of the same digit
+    for (int b = 0; b < s.bits; ++b) {
+      const uint64_t ones = __ballot(digit >> b & 1);
+      same &= digit >> b & 1 ? ones : ~ones;
+    }
+    const uint32_t rank = __popcll(same & lanemask_lt());
+    const bool leads = in && rank == 0;
+    if (leads) cnt[wave][digit] = __popcll(same);
+    __syncthreads();
+    if (in) {
+      uint32_t at = base[digit] + rank;
+      for (int w = 0; w < wave; ++w) at += cnt[w][digit];
+      s.key[at] = key;
+      s.val[at] = kFirst ? uint32_t(i) : s.val_in[i];
+    }
+    __syncthreads();
+    if (leads) {
+      atomicAdd(&base[digit], cnt[wave][digit]);
+      cnt[wave][digit] = 0;
+    }
+    __syncthreads();
+  }
+}
+
+// ---- sums ------------------------------------------------------------------
+// A row of the embedding by a group of 2^lg lanes: its tokens one after the other.
+template <class W, class E>
+__global__ void __launch_bounds__(256) te_sum(const Embed d, const typename E::T* dout, const uint32_t* key,
+                                              const uint32_t* val, typename W::T* dw, int lg) {
+  const int lanes = 1 << lg;
+  const int64_t v = int64_t(row_block()) * (256 >> lg) + (threadIdx.x >> lg);
+  if (v >= d.V) return;
+  int64_t lo = 0, hi = d.T;
+  while (lo < hi) {
+    const int64_t mid = (lo + hi) >> 1;
+    if (key[mid] < v) lo = mid + 1;
+    else hi = mid;
+  }
+  for (int32_t c = int32_t(threadIdx.x & (lanes - 1)) * kVec; c < d.width; c += lanes * kVec) {
+    const int some = d.width - c;
+    float sum[kVec] = {};
+    for (int64_t i = lo; i < d.T && key[i] == v; ++i) {
+      Pack<E, kVec> x;
+      const typename E::T* p = dout + int64_t(val[i]) * d.out_stride + c;
+      if (some >= kVec) x.load(p);
+      else x.load_some(p, some);
+#pragma unroll
+      for (int e = 0; e < kVec; ++e) sum[e] += x.get(e);
+    }
+#pragma unroll
+    for (int e = 0; e < kVec; ++e) sum[e] *= d.scale;
+    Pack<W, kVec> o;
+    o.set(sum);
+    typename W::T* p = dw + v * d.weight_stride + c;
+    if (some >= kVec) o.store(p);
+    else o.store_some(p, some);
+  }
+}
+
+int check(const nopfs_embed* p) {
+  if (!p) return fail(NOPFS_EINVAL, "embed is NULL");
+  if (p->T < 0 || p->V < 1 || p->width < 1 || p->n_ids < 0)
+    return fail(NOPFS_EINVAL, "T and n_ids must be >= 0, V and width >= 1");
+  if (!is_dtype(p->dtype) || !is_dtype(p->weight_dtype)) return fail(NOPFS_EINVAL, "unknown dtype");
+  if (p->id_bytes != 4 && p->id_bytes != 8) return fail(NOPFS_EINVAL, "id_bytes must be 4 or 8");
+  if (!isfinite(p->scale)) return fail(NOPFS_EINVAL, "scale must be finite");
+  if ((p->V > 1 && p->weight_stride < p->width) || (p->T > 1 && p->out_stride < p->width))
+    return fail(NOPFS_EINVAL, "rows overlap");
+  if (p->T > INT32_MAX || p->V > INT32_MAX - 1) return fail(NOPFS_ERANGE, "T must be < 2^31, V <= 2^31 - 2");
+  if (p->width > 1 << 28 || p->weight_stride > 1 << 28 || p->out_stride > 1 << 28)  // byte offsets below 2^63
+    return fail(NOPFS_ERANGE, "width and row strides must be <= 2^28");
+  return NOPFS_OK;
+}
+
+Embed describe(const nopfs_embed* p, const void* ids, const int64_t* slot) {
+  return {p->T, p->V, p->n_ids, p->weight_stride, p->out_stride, p->width, p->scale, ids, slot, p->id_bytes == 8};
+}
+
+// Lanes for a row: one vector each, a workgroup at most.
+int row_lanes(int32_t width) { return std::min(8, log2_ceil(ceil_div(width, kVec))); }
+
+int embed_impl(const nopfs_embed* p, const void* weight, const void* ids, const int64_t* slot, void* out,
+               hipStream_t st) {
+  const int rc = check(p);
+  if (rc) return rc;
+  if (p->T == 0) return NOPFS_OK;
+  if (!slot && p->n_ids != p->T) return fail(NOPFS_EINVAL, "without slot, ids has an entry per token");
+  if (!weight || !out || (!ids && p->n_ids > 0)) return fail(NOPFS_EINVAL, "weight, ids and out must be non-NULL");
+  const Embed d = describe(p, ids, slot);
+  const int lg = row_lanes(p->width);
+  const int64_t blocks = ceil_div(p->T, 256 >> lg);
+  return by_dtype(p->weight_dtype, [&](auto w) {
+    return by_dtype(p->dtype, [&](auto e) {
+      typedef decltype(w) W;
+      typedef decltype(e) E;
+      return launch("te_forward", te_forward<W, E, 1>, row_grid(blocks), dim3(256), 0, st, d,
+                    static_cast<const typename W::T*>(weight), static_cast<typename E::T*>(out), lg);
+    });
+  });
+}
+
+int embed_grad_impl(const nopfs_embed* p, const void* dout, const void* ids, const int64_t* slot, void* dw,
+                    hipStream_t st) {
+  int rc = check(p);
+  if (rc) return rc;
+  if (p->T > 0 && !slot && p->n_ids != p->T)
+    return fail(NOPFS_EINVAL, "without slot, ids has an entry per token");
+  if (!dw || (p->T > 0 && (!dout || (!ids && p->n_ids > 0))))
+    return fail(NOPFS_EINVAL, "d_out, ids and d_weight must be non-NULL");
+  const Embed d = describe(p, ids, slot);
+  const int bits = log2_ceil(p->V + 1);  // keys 0 .. V
+  const int passes = std::max(1, int(ceil_div(bits, kMostBits)));
+  Sort s{};
+  s.bits = std::max(1, int(ceil_div(bits, passes)));
+  s.tiles = int32_t(std::min<int64_t>(128, ceil_div(p->T, kSortTile)));
+  s.per_tile = s.tiles ? int32_t(ceil_div(p->T, s.tiles)) : 0;
+  Scratch sc(st);
+  uint32_t *key[2], *val[2];
+  const size_t n = size_t(std::max<int64_t>(p->T, 1));
+  for (int i = 0; i < 2; ++i) {
+    if ((rc = step_alloc(&sc, &key[i], n)) || (rc = step_alloc(&sc, &val[i], n))) return rc;
+  }
+  if ((rc = step_alloc(&sc, &s.hist, size_t(std::max(1, s.tiles)) << s.bits))) return rc;
+  int at = 0;
+  for (int pass = 0; pass < passes; ++pass, at ^= 1) {
+    s.key_in = key[at ^ 1], s.val_in = val[at ^ 1], s.key = key[at], s.val = val[at];
+    s.shift = pass * s.bits;
+    const dim3 grid(uint32_t(s.tiles));
+    rc = pass == 0 ? launch("te_count", te_count<true>, grid, dim3(256), 0, st, d, s)
+                   : launch("te_count", te_count<false>, grid, dim3(256), 0, st, d, s);
+    if (rc) return rc;
+    rc = pass == 0 ? launch("te_scatter", te_scatter<true>, grid, dim3(256), 0, st, d, s)
+                   : launch("te_scatter", te_scatter<false>, grid, dim3(256), 0, st, d, s);
+    if (rc) return rc;
+  }
+  at ^= 1;
+  const int lg = row_lanes(p->width);
+  const int64_t blocks = ceil_div(p->V, 256 >> lg);
+  return by_dtype(p->weight_dtype, [&](auto w) {
+    return by_dtype(p->dtype, [&](auto e) {
+      typedef decltype(w) W;
+      typedef decltype(e) E;
+      return launch("te_sum", te_sum<W, E>, row_grid(blocks), dim3(256), 0, st, d,
+                    static_cast<const typename E::T*>(dout), key[at], val[at], static_cast<typename W::T*>(dw), lg);
+    });
+  });
+}
+
+}  // namespace
+}  // namespace nopfs
+
+using namespace nopfs;
+
+extern "C" int nopfs_token_embed(const nopfs_embed* e, const void* weight, const void* ids, const int64_t* slot,
+                                 void* out, void* hip_stream) {
+  try {
+    return embed_impl(e, weight, ids, slot, out, static_cast<hipStream_t>(hip_stream));
+  } catch (...) {
+    return fail(NOPFS_EDEVICE, "unexpected host exception");
+  }
+}
+
+extern "C" int nopfs_token_embed_grad(const nopfs_embed* e, const void* d_out, const void* ids, const int64_t* slot,
+                                      void* d_weight, void* hip_stream) {
+  try {
+    auto call = [&]() {
+      return embed_grad_impl(e, d_out, ids, slot, d_weight, static_cast<hipStream_t>(hip_stream));
+    };
+    return e ? run_with_scratch(e->scratch, e->scratch_bytes, call) : call();
+  } catch (...) {
+    return fail(NOPFS_EDEVICE, "unexpected host exception");
+  }
+}
+
+extern "C" int nopfs_token_embed_scratch(const nopfs_embed* e, int64_t* bytes) {
+  try {
+    return scratch_size(bytes, [&]() {
+      return embed_grad_impl(e, no_array(), no_array(), static_cast<const int64_t*>(no_array()), no_array(), nullptr);
+    });
+  } catch (...) {
+    return fail(NOPFS_EDEVICE, "unexpected host exception");
+  }
+}

@@ -97,6 +97,33 @@ class _Distill(ctypes.Structure):
                 + [("tau", ctypes.c_float)])
 
 
+_SCRATCH = [("scratch", ctypes.c_void_p), ("scratch_bytes", ctypes.c_int64)]
+
+
+class _Embed(ctypes.Structure):
+    _fields_ = ([(x, ctypes.c_int64) for x in ("T", "V", "n_ids", "weight_stride", "out_stride")]
+                + [(x, ctypes.c_int32) for x in ("width", "weight_dtype", "dtype", "id_bytes")]
+                + [("scale", ctypes.c_float), ("reserved", ctypes.c_int32)] + _SCRATCH)
+
+
+class _Rotate(ctypes.Structure):
+    # a stride[2] of the C struct is a pair of fields here: token, head
+    _fields_ = ([("T", ctypes.c_int64)]
+                + [(x, ctypes.c_int32) for x in ("heads", "kv_heads", "width", "rotated", "interleaved",
+                                                 "dtype", "weight_dtype")]
+                + [("eps", ctypes.c_float)]
+                + [(f"{x}_{y}", ctypes.c_int64)
+                   for x in ("q", "k", "q_out", "k_out", "dq", "dk") for y in ("token", "head")]
+                + _SCRATCH)
+
+
+class _Scan(ctypes.Structure):
+    _fields_ = ([("T", ctypes.c_int64)]
+                + [(x, ctypes.c_int32) for x in ("n", "channels", "dtype", "reserved")]
+                + [(x + "_stride", ctypes.c_int64) for x in ("x", "gate", "h", "dh", "dx", "dgate")]
+                + _SCRATCH)
+
+
 _lib = None
 
 
@@ -131,6 +158,15 @@ def lib() -> ctypes.CDLL:
             "nopfs_packed_attention": [ctypes.POINTER(_Attention)] + [P] * 7,
             "nopfs_packed_attention_grad": [ctypes.POINTER(_Attention)] + [P] * 11,
             "nopfs_topk_distill": [ctypes.POINTER(_Distill)] + [P] * 7,
+            "nopfs_token_embed": [ctypes.POINTER(_Embed)] + [P] * 5,
+            "nopfs_token_embed_grad": [ctypes.POINTER(_Embed)] + [P] * 5,
+            "nopfs_token_embed_scratch": [ctypes.POINTER(_Embed), P],
+            "nopfs_norm_rotate": [ctypes.POINTER(_Rotate)] + [P] * 9,
+            "nopfs_norm_rotate_grad": [ctypes.POINTER(_Rotate)] + [P] * 13,
+            "nopfs_norm_rotate_scratch": [ctypes.POINTER(_Rotate), P],
+            "nopfs_gated_scan": [ctypes.POINTER(_Scan)] + [P] * 8,
+            "nopfs_gated_scan_grad": [ctypes.POINTER(_Scan)] + [P] * 11,
+            "nopfs_gated_scan_scratch": [ctypes.POINTER(_Scan), I32, P],
             "nopfs_profile_enable": [ctypes.c_int],
             "nopfs_profile_query": [ctypes.c_int, ctypes.POINTER(ctypes.c_char_p),
                                     ctypes.POINTER(I64), ctypes.POINTER(ctypes.c_double)],
@@ -157,7 +193,10 @@ EXPORTED = ("nopfs_stream_shape", "nopfs_access_streams", "nopfs_access_streams_
             "nopfs_staging_schedule", "nopfs_fetch_model", "nopfs_buffer_sim", "nopfs_policy_sim",
             "nopfs_batch_tables", "nopfs_packed_attention", "nopfs_packed_attention_grad",
             "nopfs_batch_tables_scratch", "nopfs_packed_attention_scratch",
-            "nopfs_topk_distill", "nopfs_strerror",
+            "nopfs_topk_distill", "nopfs_token_embed", "nopfs_token_embed_grad",
+            "nopfs_token_embed_scratch", "nopfs_norm_rotate", "nopfs_norm_rotate_grad",
+            "nopfs_norm_rotate_scratch", "nopfs_gated_scan", "nopfs_gated_scan_grad",
+            "nopfs_gated_scan_scratch", "nopfs_strerror",
             "nopfs_last_error", "nopfs_profile_enable", "nopfs_profile_query",
             "nopfs_calibration_copy", "nopfs_scratch_release", "nopfs_debug_set")
 
@@ -514,7 +553,7 @@ def _row_stride(t):
     return t.stride(0) if t.shape[0] > 1 else max(t.shape[1], 1)
 
 
-_I32 = (torch.int32,)
+_I32, _I64, _F64 = (torch.int32,), (torch.int64,), (torch.float64,)
 
 
 def batch_tables(ids, tokens, free, block: int, width: int, cap: int, out=None, stream=None):
@@ -753,6 +792,303 @@ def topk_distill(logits, index, teacher, tau=1.0, weight=None, grad=True, loss=N
         None if weight is None else weight.data_ptr(), loss.data_ptr(),
         None if dlogits is None else dlogits.data_ptr(), st), "nopfs_topk_distill")
     return loss, dlogits
+
+
+# -- layers of a token model over the packed samples ---------------------------------
+_IDS = (torch.int32, torch.int64)
+
+
+def _row_gradient(d):
+    """A gradient as the kernels read it, its rows apart from each other. Autograd
+    hands over broadcast and transposed ones too."""
+    if d.is_contiguous():
+        return d
+    return d.clone(memory_format=torch.contiguous_format)
+
+
+def _tokens(ids, slot, dev):
+    """Entries of ids, and the tokens."""
+    n_ids = _dense(_step_tensor(ids, "ids", _IDS, 1, dev), "ids").shape[0]
+    return n_ids, n_ids if slot is None else _dense(_step_tensor(slot, "slot", _I64, 1, dev), "slot").shape[0]
+
+
+def _float_types(dtype):
+    """The types that a tensor may have where `dtype` was asked for."""
+    if dtype is None:
+        return _DTYPES
+    if dtype not in _DTYPES:
+        raise ValueError("dtype must be " + " or ".join(str(d) for d in _DTYPES))
+    return (dtype,)
+
+
+class _TokenEmbed(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, weight, ids, scale, slot, dtype, stream):
+        ctx.save_for_backward(ids, *(() if slot is None else (slot,)))
+        ctx.rows, ctx.dtype, ctx.scale, ctx.stream = weight.shape[0], weight.dtype, scale, stream
+        return token_embed(weight, ids, scale, slot, dtype, stream=stream)
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dout):
+        ids, *slot = ctx.saved_tensors
+        dout = _row_gradient(dout)
+        dweight = _call_in_backward(ctx.stream, lambda: token_embed_grad(
+            dout, ids, ctx.rows, ctx.scale, slot[0] if slot else None, ctx.dtype, stream=ctx.stream))
+        return dweight, None, None, None, None, None
+
+
+def token_embed(weight, ids, scale=1.0, slot=None, dtype=None, out=None, stream=None):
+    """The rows of an embedding that the packed tokens name, times `scale`
+    (nopfs_token_embed): weight [V][width], ids [T] int32 or int64; with slot [T]
+    int64 (a row of batch_tables' slot) ids is a token buffer, and token t is
+    ids[slot[t]]. Slots and ids out of range, -1 among them, are padding: rows of
+    zeros. Returns [T][width] of `dtype` (weight's unless given). Autograd takes it
+    back to weight by token_embed_grad."""
+    if weight.requires_grad and torch.is_grad_enabled():
+        _no_outputs_given("token_embed", out)
+        return _TokenEmbed.apply(weight, ids, scale, slot, dtype, stream)
+    dev = torch.cuda.current_device()
+    V, width = _step_tensor(weight, "weight", _DTYPES, 2, dev).shape
+    n_ids, T = _tokens(ids, slot, dev)
+    types = _float_types(dtype)
+    if out is None:
+        out = weight.new_empty((T, width), dtype=dtype)
+    else:
+        _step_shape(_step_tensor(out, "out", types, 2, dev), "out", (T, width))
+    e = _Embed(T, V, n_ids, _row_stride(weight), _row_stride(out), width, _DTYPES[weight.dtype],
+               _DTYPES[out.dtype], ids.element_size(), scale)
+    st = _step_stream(stream, dev, (weight, ids, slot, out))
+    _check(lib().nopfs_token_embed(ctypes.byref(e), weight.data_ptr(), ids.data_ptr(),
+                                   None if slot is None else slot.data_ptr(), out.data_ptr(), st),
+           "nopfs_token_embed")
+    return out
+
+
+def token_embed_grad(dout, ids, rows: int, scale=1.0, slot=None, dtype=None, dweight=None,
+                     stream=None):
+    """Gradient of token_embed by its weight of `rows` rows (nopfs_token_embed_grad),
+    from `dout` [T][width], the gradient of its output. Returns all of it,
+    [rows][width] of `dtype` (dout's unless given)."""
+    dev = torch.cuda.current_device()
+    n_ids, T = _tokens(ids, slot, dev)
+    width = _step_tensor(dout, "dout", _DTYPES, 2, dev).shape[1]
+    _step_shape(dout, "dout", (T, width))
+    rows, types = int(rows), _float_types(dtype)
+    if not 0 < rows < 2**31:
+        raise ValueError("rows must be positive and below 2^31")
+    if dweight is None:
+        dweight = dout.new_empty((rows, width), dtype=dtype)
+    else:
+        _step_shape(_step_tensor(dweight, "dweight", types, 2, dev), "dweight", (rows, width))
+    e = _Embed(T, rows, n_ids, _row_stride(dweight), _row_stride(dout), width, _DTYPES[dweight.dtype],
+               _DTYPES[dout.dtype], ids.element_size(), scale)
+    st = _step_stream(stream, dev, (dout, ids, slot, dweight))
+    scratch = _capturing() and _step_scratch(e, dev, stream, "nopfs_token_embed_scratch")  # noqa: F841
+    _check(lib().nopfs_token_embed_grad(ctypes.byref(e), dout.data_ptr(), ids.data_ptr(),
+                                        None if slot is None else slot.data_ptr(),
+                                        dweight.data_ptr(), st), "nopfs_token_embed_grad")
+    return dweight
+
+
+def _rotate(q, k, pos, freq, q_weight, k_weight, eps, interleaved, dev):
+    """What comes before the strides in the call's description."""
+    _step_tensor(q, "q", _DTYPES, 3, dev)
+    T, heads, width = q.shape
+    kv_heads = _step_tensor(k, "k", (q.dtype,), 3, dev).shape[1]
+    _step_shape(k, "k", (T, kv_heads, width))
+    _step_dense(pos, "pos", torch.int32, (T,), dev)
+    rotated = 0
+    if freq is not None:
+        rotated = 2 * _dense(_step_tensor(freq, "freq", _F64, 1, dev), "freq").shape[0]
+    kinds = [w.dtype for w in (q_weight, k_weight) if w is not None]
+    for name, w in (("q_weight", q_weight), ("k_weight", k_weight)):
+        if w is not None:
+            _step_shape(_step_tensor(w, name, _DTYPES, 1, dev), name, (width,))
+    if kinds and kinds[-1] is not kinds[0]:
+        raise ValueError("q_weight and k_weight must be of one type")
+    return (T, heads, kv_heads, width, rotated, 1 if interleaved else 0, _DTYPES[q.dtype],
+            _DTYPES[kinds[0]] if kinds else 0, eps)
+
+
+def _optional(t):
+    return None if t is None else t.data_ptr()
+
+
+class _NormRotate(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, q, k, pos, freq, q_weight, k_weight, eps, interleaved, stream):
+        ctx.save_for_backward(q, k, pos, freq, q_weight, k_weight)
+        ctx.eps, ctx.interleaved, ctx.stream = eps, interleaved, stream
+        return norm_rotate(q, k, pos, freq, q_weight, k_weight, eps, interleaved, stream=stream)
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dq_out, dk_out):
+        need = ctx.needs_input_grad
+        dq_out, dk_out = _row_gradient(dq_out), _row_gradient(dk_out)
+        dq, dk, dqw, dkw = _call_in_backward(ctx.stream, lambda: norm_rotate_grad(
+            dq_out, dk_out, *ctx.saved_tensors, ctx.eps, ctx.interleaved, weights=need[4] or need[5],
+            stream=ctx.stream))
+        return dq, dk, None, None, dqw, dkw, None, None, None
+
+
+def norm_rotate(q, k, pos, freq=None, q_weight=None, k_weight=None, eps=1e-6, interleaved=False,
+                q_out=None, k_out=None, stream=None):
+    """Root-mean-square norms of queries and keys per head and their rotation by
+    position (nopfs_norm_rotate): q [T][heads][width], k [T][kv_heads][width], any
+    strides (slices of one projection, say); pos [T] int32, a row of batch_tables'
+    pos (-1: padding, rows of zeros); freq float64, the angle per position of each
+    pair of elements (base ** (-2 i / rotated), say; None: no rotation; fewer than
+    width / 2: the elements behind are not rotated). Pairs are (i, i + rotated/2),
+    or neighbours if interleaved. q_weight, k_weight [width] of one type, or None.
+    Returns q_out, k_out; they may be q and k. Autograd takes them back to q, k and
+    the weights by norm_rotate_grad."""
+    if torch.is_grad_enabled() and any(
+            t is not None and t.requires_grad for t in (q, k, q_weight, k_weight)):
+        _no_outputs_given("norm_rotate", q_out, k_out)
+        return _NormRotate.apply(q, k, pos, freq, q_weight, k_weight, eps, interleaved, stream)
+    dev = torch.cuda.current_device()
+    r = _rotate(q, k, pos, freq, q_weight, k_weight, eps, interleaved, dev)
+    outs = []
+    for name, t, like in (("q_out", q_out, q), ("k_out", k_out, k)):
+        if t is None:
+            t = q.new_empty(like.shape)
+        else:
+            _step_shape(_step_tensor(t, name, (q.dtype,), 3, dev), name, like.shape)
+        outs.append(t)
+    r = _Rotate(*r, *_strides(q, k, *outs))
+    st = _step_stream(stream, dev, (q, k, pos, freq, q_weight, k_weight, *outs))
+    _check(lib().nopfs_norm_rotate(ctypes.byref(r), q.data_ptr(), k.data_ptr(), pos.data_ptr(),
+                                   _optional(freq), _optional(q_weight), _optional(k_weight),
+                                   outs[0].data_ptr(), outs[1].data_ptr(), st), "nopfs_norm_rotate")
+    return tuple(outs)
+
+
+def norm_rotate_grad(dq_out, dk_out, q, k, pos, freq=None, q_weight=None, k_weight=None, eps=1e-6,
+                     interleaved=False, weights=True, dq=None, dk=None, stream=None):
+    """Gradient of norm_rotate (nopfs_norm_rotate_grad) from its inputs and the
+    gradients of its outputs. Returns dq, dk (given, they may be dq_out and dk_out) and
+    the gradients of the weights, None of a weight that is None, or with weights False."""
+    dev = torch.cuda.current_device()
+    r = _rotate(q, k, pos, freq, q_weight, k_weight, eps, interleaved, dev)
+    grads = []
+    for name, d, t, like in (("q", dq_out, dq, q), ("k", dk_out, dk, k)):
+        _step_shape(_step_tensor(d, f"d{name}_out", (q.dtype,), 3, dev), f"d{name}_out", like.shape)
+        if t is None:
+            t = q.new_empty(like.shape)
+        else:
+            _step_shape(_step_tensor(t, "d" + name, (q.dtype,), 3, dev), "d" + name, like.shape)
+        grads.append(t)
+    grads += [torch.empty_like(w) if weights and w is not None else None for w in (q_weight, k_weight)]
+    r = _Rotate(*r, *_strides(q, k, dq_out, dk_out, grads[0], grads[1]))
+    st = _step_stream(stream, dev, (dq_out, dk_out, q, k, pos, freq, q_weight, k_weight, *grads))
+    scratch = _capturing() and _step_scratch(r, dev, stream, "nopfs_norm_rotate_scratch")  # noqa: F841
+    _check(lib().nopfs_norm_rotate_grad(
+        ctypes.byref(r), dq_out.data_ptr(), dk_out.data_ptr(), q.data_ptr(), k.data_ptr(), pos.data_ptr(),
+        _optional(freq), _optional(q_weight), _optional(k_weight), grads[0].data_ptr(),
+        grads[1].data_ptr(), _optional(grads[2]), _optional(grads[3]), st), "nopfs_norm_rotate_grad")
+    return tuple(grads)
+
+
+SCAN_CHUNK = 16  # NOPFS_SCAN_CHUNK
+
+
+def _scan(x, gate, start, h0, dev):
+    T, channels = _step_tensor(x, "x", _DTYPES, 2, dev).shape
+    _step_shape(_step_tensor(gate, "gate", (x.dtype,), 2, dev), "gate", (T, channels))
+    n = _dense(_step_tensor(start, "start", _I32, 1, dev), "start").shape[0] - 1
+    if n < 0:
+        raise ValueError("start must have an entry before every sample and one behind the last")
+    if h0 is not None:
+        _step_dense(h0, "h0", torch.float32, (n, channels), dev)
+    return T, n, channels, -(-T // SCAN_CHUNK)
+
+
+def _rows_of(t, name, dtype, shape, like, dev):
+    """An output's rows: as given, or new ones."""
+    if t is None:
+        return like.new_empty(shape, dtype=dtype)
+    _step_shape(_step_tensor(t, name, (dtype,), 2, dev), name, shape)
+    return t
+
+
+class _GatedScan(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, gate, start, h0, stream):
+        h, last, carry = gated_scan(x, gate, start, h0, stream=stream)
+        ctx.save_for_backward(x, gate, start, h0, carry)
+        ctx.stream = stream
+        ctx.mark_non_differentiable(carry)
+        ctx.set_materialize_grads(False)
+        return h, last, carry
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dh, dlast, _):
+        if dh is None and dlast is None:
+            return (None,) * 5
+        x, gate, start, h0, carry = ctx.saved_tensors
+        dh = torch.zeros_like(x, memory_format=torch.contiguous_format) if dh is None else _row_gradient(dh)
+        dlast = None if dlast is None else dlast.contiguous()
+        dx, dgate, dh0 = _call_in_backward(ctx.stream, lambda: gated_scan_grad(
+            dh, x, gate, start, carry, h0, dlast, stream=ctx.stream))
+        return dx, dgate, None, dh0, None
+
+
+def gated_scan(x, gate, start, h0=None, keep=True, h=None, last=None, stream=None):
+    """A gated linear recurrence over packed samples (nopfs_gated_scan), for each
+    channel by itself: with a = sigmoid(gate), h_t = a_t h_(t-1) + (1 - a_t) x_t.
+    x and gate [T][channels], any row strides (halves of one projection, say);
+    start [n+1] int32, a row of batch_tables' start; h0 [n][channels] float32, the
+    state before each sample (0 if None). Returns h (as x), last [n][channels]
+    float32, the state behind each sample, and carry, which the gradient starts from
+    (None if keep is False). Samples of one token with h0 are the step of a
+    generation; last may not be h0. Autograd takes h and last back to x, gate and h0
+    by gated_scan_grad."""
+    if torch.is_grad_enabled() and (x.requires_grad or gate.requires_grad
+                                    or h0 is not None and h0.requires_grad):
+        _no_outputs_given("gated_scan", h, last)
+        return _GatedScan.apply(x, gate, start, h0, stream)
+    dev = torch.cuda.current_device()
+    T, n, channels, chunks = _scan(x, gate, start, h0, dev)
+    h = _rows_of(h, "h", x.dtype, (T, channels), x, dev)
+    if last is None:
+        last = x.new_empty((n, channels), dtype=torch.float32)
+    else:
+        _step_dense(last, "last", torch.float32, (n, channels), dev)
+    carry = x.new_empty((chunks, channels), dtype=torch.float32) if keep else None
+    s = _Scan(T, n, channels, _DTYPES[x.dtype], 0, _row_stride(x), _row_stride(gate), _row_stride(h))
+    st = _step_stream(stream, dev, (x, gate, start, h0, h, last, carry))
+    scratch = _capturing() and _step_scratch(s, dev, stream, "nopfs_gated_scan_scratch", 0)  # noqa: F841
+    _check(lib().nopfs_gated_scan(ctypes.byref(s), x.data_ptr(), gate.data_ptr(), start.data_ptr(),
+                                  _optional(h0), h.data_ptr(), last.data_ptr(), _optional(carry), st),
+           "nopfs_gated_scan")
+    return h, last, carry
+
+
+def gated_scan_grad(dh, x, gate, start, carry, h0=None, dlast=None, dx=None, dgate=None, stream=None):
+    """Gradient of gated_scan (nopfs_gated_scan_grad) from its inputs, its carry and
+    the gradients of h and last (None: 0). Returns dx, dgate (as x) and dh0 (None
+    without h0)."""
+    dev = torch.cuda.current_device()
+    T, n, channels, chunks = _scan(x, gate, start, h0, dev)
+    _step_shape(_step_tensor(dh, "dh", (x.dtype,), 2, dev), "dh", (T, channels))
+    _step_dense(carry, "carry", torch.float32, (chunks, channels), dev)
+    if dlast is not None:
+        _step_dense(dlast, "dlast", torch.float32, (n, channels), dev)
+    dx = _rows_of(dx, "dx", x.dtype, (T, channels), x, dev)
+    dgate = _rows_of(dgate, "dgate", x.dtype, (T, channels), x, dev)
+    dh0 = None if h0 is None else torch.empty_like(h0)
+    s = _Scan(T, n, channels, _DTYPES[x.dtype], 0, _row_stride(x), _row_stride(gate), 0,
+              _row_stride(dh), _row_stride(dx), _row_stride(dgate))
+    st = _step_stream(stream, dev, (dh, x, gate, start, carry, h0, dlast, dx, dgate, dh0))
+    scratch = _capturing() and _step_scratch(s, dev, stream, "nopfs_gated_scan_scratch", 1)  # noqa: F841
+    _check(lib().nopfs_gated_scan_grad(
+        ctypes.byref(s), dh.data_ptr(), _optional(dlast), x.data_ptr(), gate.data_ptr(), start.data_ptr(),
+        _optional(h0), carry.data_ptr(), dx.data_ptr(), dgate.data_ptr(), _optional(dh0), st),
+        "nopfs_gated_scan_grad")
+    return dx, dgate, dh0
 
 
 # -- measurement aids -----------------------------------------------------------

@@ -1,0 +1,218 @@
+"""nopfs_gated_scan and its gradient against 64 bits within layer_ref's bounds: the
+types, channels and strides of any alignment, samples of none, one and many tokens,
+states in and out, padding, gates that never forget or always do, non-finite
+neighbours, and the gradient against differences."""
+import math
+
+import pytest
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+
+import layer_ref  # noqa: E402
+from layer_ref import close  # noqa: E402
+from paper_2101_08734_amd import nopfs  # noqa: E402
+
+BF, FP, F32 = torch.bfloat16, torch.float16, torch.float32
+NAMES = {BF: "bf16", FP: "fp16", F32: "fp32"}
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _gpu():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    nopfs.lib()
+    yield
+
+
+def _inputs(lengths, C, dt=BF, tail=0, seed=0, state=True, mean=2.5, spread=1.5):
+    g = torch.Generator().manual_seed(seed)
+    T, n = sum(lengths) + tail, len(lengths)
+    x = torch.randn((T, C), generator=g).to(dt).cuda()
+    gate = (mean + spread * torch.randn((T, C), generator=g)).to(dt).cuda()
+    start = torch.tensor([0] + list(lengths)).cumsum(0).int().cuda()
+    dh = torch.randn((T, C), generator=g).to(dt).cuda()
+    h0 = torch.randn((n, C), generator=g).cuda() if state else None
+    dlast = torch.randn((n, C), generator=g).cuda() if state else None
+    return x, gate, start, h0, dh, dlast
+
+
+def _check(x, gate, start, h0, dh, dlast):
+    h, last, carry = nopfs.gated_scan(x, gate, start, h0)
+    dx, dgate, dh0 = nopfs.gated_scan_grad(dh, x, gate, start, carry, h0, dlast)
+    val, err = layer_ref.scan(x, gate, start.tolist(), h0, dh, dlast)
+    got = dict(h=h, last=last, dx=dx, dgate=dgate, dh0=dh0)
+    for name, t in got.items():
+        if name == "dh0" and h0 is None:
+            assert t is None
+        else:
+            close(name, t, val[name], err[name])
+    again = nopfs.gated_scan(x, gate, start, h0)
+    assert all(torch.equal(a, b) for a, b in zip((h, last, carry), again))
+    again = nopfs.gated_scan_grad(dh, x, gate, start, carry, h0, dlast)
+    assert all(a is b is None or torch.equal(a, b) for a, b in zip((dx, dgate, dh0), again))
+    alone = nopfs.gated_scan(x, gate, start, h0, keep=False)
+    assert alone[2] is None and torch.equal(alone[0], h) and torch.equal(alone[1], last)
+    return h, last, carry, dx, dgate, dh0
+
+
+LENGTHS = {"one": [1], "none": [0], "no sample": [], "short": [1, 2, 0, 3, 1], "chunk": [16, 16, 0, 32],
+           "long": [1_000], "mixed": [300, 0, 1, 17, 255, 256, 0, 129, 1, 640, 0], "tile": [128, 256, 128]}
+
+
+@pytest.mark.parametrize("dt", [BF, FP, F32], ids=NAMES.get)
+@pytest.mark.parametrize("lengths", LENGTHS)
+@pytest.mark.parametrize("state", [False, True])
+def test_samples(dt, lengths, state):
+    _check(*_inputs(LENGTHS[lengths], 40, dt, tail=5, state=state))
+
+
+@pytest.mark.parametrize("T", [1, 2, 15, 16, 17, 31, 32, 33, 127, 128, 129, 255, 256, 257, 511, 513, 1_025, 3_001])
+def test_tokens(T):
+    _check(*_inputs([T], 6, F32, seed=T))
+    _check(*_inputs([T], 6, BF, seed=T, tail=T % 40))
+
+
+@pytest.mark.parametrize("C", [1, 2, 3, 63, 64, 65, 127, 128, 129, 255, 256, 257, 333, 640])
+@pytest.mark.parametrize("dt", [FP, F32], ids=NAMES.get)
+def test_channels(C, dt):
+    _check(*_inputs([150, 0, 41], C, dt, tail=3, seed=C))
+
+
+def test_single_tokens():
+    """A generation's step, from its states, as often as the sample is long."""
+    x, gate, start, h0, *_ = _inputs([50] * 7, 96, BF)
+    whole, last, _ = nopfs.gated_scan(x, gate, start, h0)
+    one = torch.arange(8, dtype=torch.int32, device="cuda")
+    state, other = h0.clone(), torch.empty_like(h0)
+    rows = []
+    for t in range(50):
+        at = torch.arange(7, device="cuda") * 50 + t
+        h, _, none = nopfs.gated_scan(x[at], gate[at], one, state, keep=False, last=other)
+        assert none is None
+        rows.append(h)
+        state, other = other, state
+    val, err = layer_ref.scan(x, gate, start.tolist(), h0)
+    close("h", torch.stack(rows, 1).view(350, 96), val["h"], err["h"])
+    close("last", state, val["last"], err["last"])
+
+
+@pytest.mark.parametrize("n", [1, 31, 32, 33, 130, 1_000])
+def test_many_single_tokens(n):
+    _check(*_inputs([1] * n, 70, BF, seed=n))
+
+
+@pytest.mark.parametrize("mean", [-30.0, -8.0, 0.0, 8.0, 17.0, 90.0])
+@pytest.mark.parametrize("dt", [BF, F32], ids=NAMES.get)
+def test_gates(mean, dt):
+    """From gates that forget at once to gates that keep all."""
+    _check(*_inputs([400, 300], 24, dt, mean=mean, spread=1.0))
+
+
+def test_a_long_memory():
+    """a = 1 - 2^-12 over 20,000 tokens of equal x: h comes to x and stays there."""
+    T, C = 20_000, 8
+    x = torch.full((T, C), 1.7, device="cuda")
+    gate = torch.full((T, C), math.log(4_095.0), device="cuda")
+    start = torch.tensor([0, T], dtype=torch.int32, device="cuda")
+    h, last, _ = nopfs.gated_scan(x, gate, start)
+    val, err = layer_ref.scan(x[:, :1], gate[:, :1], [0, T])
+    close("h", h[:, :1], val["h"], err["h"])
+    assert bool((h == h[:, :1]).all())
+
+
+def test_many_samples_of_none():
+    lengths = [0] * 3_000 + [5] + [0] * 700 + [300] + [0] * 129
+    _check(*_inputs(lengths, 3, BF, tail=2))
+
+
+@pytest.mark.parametrize("bad", [math.nan, math.inf])
+def test_not_finite_stays_in_its_sample(bad):
+    lengths = [40, 100, 0, 60, 300, 20]
+    x, gate, start, h0, dh, dlast = _inputs(lengths, 20, BF, tail=30)
+    want = _check(x, gate, start, h0, dh, dlast)
+    a, b = int(start[4]), int(start[5])
+    x[a + 10] = bad
+    gate[b - 1] = math.nan
+    dh[a + 200] = bad
+    h0[4], dlast[4] = bad, bad
+    for t in (x, gate, dh):  # rows of no sample: not read
+        t[int(start[-1]):] = math.nan
+    h, last, carry = nopfs.gated_scan(x, gate, start, h0)
+    dx, dgate, dh0 = nopfs.gated_scan_grad(dh, x, gate, start, carry, h0, dlast)
+    rows = torch.ones(len(x), dtype=torch.bool)
+    rows[a:b] = False
+    samples = torch.arange(6) != 4
+    for got, ref, mask in ((h, want[0], rows), (last, want[1], samples), (dx, want[3], rows),
+                           (dgate, want[4], rows), (dh0, want[5], samples)):
+        assert torch.equal(got[mask], ref[mask])
+    assert not bool(torch.isfinite(last[4]).any())
+
+
+@pytest.mark.parametrize("dt", [BF, F32], ids=NAMES.get)
+@pytest.mark.parametrize("shift,stride", [(0, 40), (1, 43), (3, 64), (0, 128)])
+def test_strides(dt, shift, stride):
+    """Rows of wider arrays from any element on; what lies between them stays."""
+    x0, gate0, start, h0, dh0_, dlast = _inputs([90, 0, 60], 37, dt, tail=4)
+    want = _check(x0, gate0, start, h0, dh0_, dlast)
+    T = len(x0)
+
+    def strided(like, fill):
+        flat = torch.full((T * stride + 8,), fill, dtype=dt, device="cuda")
+        view = torch.as_strided(flat, (T, 37), (stride, 1), shift)
+        if like is not None:
+            view.copy_(like)
+        return flat, view
+
+    x, gate, dh = (strided(t, math.nan)[1] for t in (x0, gate0, dh0_))
+    (fh, h), (fx, dx), (fg, dgate) = (strided(None, f) for f in (5.0, 6.0, 7.0))
+    _, last, carry = nopfs.gated_scan(x, gate, start, h0, h=h)
+    _, _, dh0 = nopfs.gated_scan_grad(dh, x, gate, start, carry, h0, dlast, dx=dx, dgate=dgate)
+    for a, b in zip((h, last, carry, dx, dgate, dh0), want):
+        assert torch.equal(a, b)
+    held = torch.ones_like(fh, dtype=torch.bool)
+    torch.as_strided(held, (T, 37), (stride, 1), shift).fill_(False)
+    for flat, fill in ((fh, 5.0), (fx, 6.0), (fg, 7.0)):
+        assert bool((flat[held] == fill).all())
+
+
+def test_gradient_against_differences():
+    x, gate, start, h0, dh, dlast = _inputs([30, 0, 7, 40], 5, F32, mean=1.0)
+    _, _, carry = nopfs.gated_scan(x, gate, start, h0)
+    grads = nopfs.gated_scan_grad(dh, x, gate, start, carry, h0, dlast)
+    g = torch.Generator().manual_seed(5)
+    args = [x, gate, h0]
+    moves = [torch.randn(t.shape, generator=g).cuda() for t in args]
+
+    def f(step):
+        a, b, c = (t + step * m for t, m in zip(args, moves))
+        h, last, _ = nopfs.gated_scan(a, b, start, c)
+        return float((h.double() * dh.double()).sum() + (last.double() * dlast.double()).sum())
+
+    step = 2.0**-7
+    diff = (8 * (f(step) - f(-step)) - (f(2 * step) - f(-2 * step))) / (12 * step)
+    want = sum(float((a.double() * m.double()).sum()) for a, m in zip(grads, moves))
+    # values are off by some 60 E (four tokens' memory), the formula by step^4
+    size = 2 * float(dh.abs().sum() + dlast.abs().sum())
+    assert abs(diff - want) <= size * (2 * 60 * 2.0**-24 / step + 30 * step**4)
+
+
+def test_refusals():
+    x, gate, start, h0, dh, dlast = _inputs([3, 2], 8)
+    h, last, carry = nopfs.gated_scan(x, gate, start, h0)
+    for bad in (lambda: nopfs.gated_scan(x, gate.half(), start), lambda: nopfs.gated_scan(x, gate[:4], start),
+                lambda: nopfs.gated_scan(x, gate, start.long()), lambda: nopfs.gated_scan(x, gate, start[:0]),
+                lambda: nopfs.gated_scan(x, gate, start, h0[:1]), lambda: nopfs.gated_scan(x, gate, start, h0.half()),
+                lambda: nopfs.gated_scan(x, gate, start, h=h.float()),
+                lambda: nopfs.gated_scan(x, gate, start, last=last[:1]),
+                lambda: nopfs.gated_scan_grad(dh[:4], x, gate, start, carry),
+                lambda: nopfs.gated_scan_grad(dh, x, gate, start, carry[:0]),
+                lambda: nopfs.gated_scan_grad(dh, x, gate, start, carry, dlast=dlast.half())):
+        with pytest.raises(ValueError):
+            bad()
+    with pytest.raises(TypeError):
+        nopfs.gated_scan(x, gate, start.cpu())
+    for bad in (lambda: nopfs.gated_scan(x, gate, start, h0, last=h0),
+                lambda: nopfs.gated_scan(x[:1].expand(5, 8), gate, start)):
+        with pytest.raises(nopfs.NopfsError):
+            bad()
