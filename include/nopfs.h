@@ -517,7 +517,7 @@ typedef struct nopfs_embed {
   int64_t n_ids;         /* entries of ids: T, or with slot those of the buffer */
   int64_t weight_stride; /* of weight or its gradient, row to row, >= width    */
   int64_t out_stride;    /* of out or its gradient, the same                   */
-  int32_t width;         /* elements of a row, >= 1                            */
+  int32_t width;         /* elements of a row, 1 .. 2^23                       */
   int32_t weight_dtype;  /* of weight and its gradient                         */
   int32_t dtype;         /* of out and its gradient                            */
   int32_t id_bytes;      /* of an entry of ids: 4 (int32) or 8 (int64)         */

@@ -78,7 +78,8 @@ constexpr int kSortTile = 1024;
 struct Sort {
   const uint32_t *key_in, *val_in;  // the pass before (not in the first)
   uint32_t *key, *val;
-  uint32_t* hist;  // [tiles][1 << bits]
+  uint32_t* hist;   // [tiles][1 << bits]
+  uint8_t* named;   // [V]: some token names the row (cleared and set in the first pass)
   int32_t tiles, per_tile, shift, bits;
 };
 
@@ -94,6 +95,9 @@ __global__ void __launch_bounds__(256) te_count(const Embed d, const Sort s) {
   __shared__ uint32_t count[1 << kMostBits];
   const int bins = 1 << s.bits;
   for (int b = threadIdx.x; b < bins; b += 256) count[b] = 0;
+  if (kFirst) {
+    for (int64_t v = int64_t(blockIdx.x) * 256 + threadIdx.x; v < d.V; v += int64_t(gridDim.x) * 256) s.named[v] = 0;
+  }
   __syncthreads();
   const int64_t i0 = int64_t(blockIdx.x) * s.per_tile;
   const int64_t i1 = i0 + s.per_tile < d.T ? i0 + s.per_tile : d.T;
@@ -152,6 +156,7 @@ __global__ void __launch_bounds__(256) te_scatter(const Embed d, const Sort s) {
       for (int w = 0; w < wave; ++w) at += cnt[w][digit];
       s.key[at] = key;
       s.val[at] = kFirst ? uint32_t(i) : s.val_in[i];
+      if (kFirst && key < d.V) s.named[key] = 1;
     }
     __syncthreads();
     if (leads) {
@@ -163,37 +168,155 @@ __global__ void __launch_bounds__(256) te_scatter(const Embed d, const Sort s) {
 }
 
 // ---- sums ------------------------------------------------------------------
-// A row of the embedding by a group of 2^lg lanes: its tokens one after the other.
+// The sorted tokens are cut into pieces of equal size, however many of them share
+// a name, by groups of 2^lg lanes. A name whose tokens lie in one piece has its row
+// written from there; the others leave the sum of each piece's part, and te_join
+// adds those up in order.
+struct Pieces {
+  const uint32_t *key, *val;
+  float *head, *tail;  // [pieces][width]: of the name that goes on from the piece before; into the next
+  int32_t per, n;      // tokens of a piece, pieces
+};
+
+template <class W>
+__device__ __forceinline__ void store_row(const Embed& d, typename W::T* dw, uint32_t v, int32_t c, int some,
+                                          float (&sum)[kVec]) {
+#pragma unroll
+  for (int e = 0; e < kVec; ++e) sum[e] *= d.scale;
+  Pack<W, kVec> o;
+  o.set(sum);
+  typename W::T* p = dw + int64_t(v) * d.weight_stride + c;
+  if (some >= kVec) o.store(p);
+  else o.store_some(p, some);
+}
+
 template <class W, class E>
-__global__ void __launch_bounds__(256) te_sum(const Embed d, const typename E::T* dout, const uint32_t* key,
-                                              const uint32_t* val, typename W::T* dw, int lg) {
+__global__ void __launch_bounds__(256) te_pieces(const Embed d, const Pieces s, const typename E::T* dout,
+                                                 typename W::T* dw, int lg) {
+  constexpr int kDeep = 8;  // rows in flight
   const int lanes = 1 << lg;
-  const int64_t v = int64_t(row_block()) * (256 >> lg) + (threadIdx.x >> lg);
-  if (v >= d.V) return;
-  int64_t lo = 0, hi = d.T;
-  while (lo < hi) {
-    const int64_t mid = (lo + hi) >> 1;
-    if (key[mid] < v) lo = mid + 1;
-    else hi = mid;
-  }
+  const int64_t piece = int64_t(row_block()) * (256 >> lg) + (threadIdx.x >> lg);
+  if (piece >= s.n) return;
+  const int64_t i0 = piece * s.per, i1 = i0 + s.per < d.T ? i0 + s.per : d.T;
+  const uint32_t none = uint32_t(d.V);
+  const uint32_t before = i0 > 0 ? s.key[i0 - 1] : none, behind = i1 < d.T ? s.key[i1] : none;
   for (int32_t c = int32_t(threadIdx.x & (lanes - 1)) * kVec; c < d.width; c += lanes * kVec) {
     const int some = d.width - c;
     float sum[kVec] = {};
-    for (int64_t i = lo; i < d.T && key[i] == v; ++i) {
-      Pack<E, kVec> x;
-      const typename E::T* p = dout + int64_t(val[i]) * d.out_stride + c;
-      if (some >= kVec) x.load(p);
-      else x.load_some(p, some);
+    uint32_t name = s.key[i0];
+    bool from_before = name == before;
+    auto flush = [&](bool goes_on) {
+      if (name >= none) return;
+      if (!from_before && !goes_on) return store_row<W>(d, dw, name, c, some, sum);
+      float* p = (from_before ? s.head : s.tail) + piece * d.width + c;
+      if (some >= kVec) {
 #pragma unroll
-      for (int e = 0; e < kVec; ++e) sum[e] += x.get(e);
+        for (int e = 0; e < kVec; ++e) p[e] = sum[e];
+      } else {
+        for (int e = 0; e < some; ++e) p[e] = sum[e];
+      }
+    };
+    for (int64_t i = i0; i < i1; i += kDeep) {
+      uint32_t key[kDeep], val[kDeep];
+#pragma unroll
+      for (int j = 0; j < kDeep; ++j) {
+        key[j] = i + j < i1 ? s.key[i + j] : none;
+        val[j] = i + j < i1 ? s.val[i + j] : 0;
+      }
+      Pack<E, kVec> x[kDeep];
+#pragma unroll
+      for (int j = 0; j < kDeep; ++j) {
+        x[j].zero();
+        const typename E::T* p = dout + int64_t(val[j]) * d.out_stride + c;
+        if (key[j] < none) {
+          if (some >= kVec) x[j].load(p);
+          else x[j].load_some(p, some);
+        }
+      }
+#pragma unroll
+      for (int j = 0; j < kDeep; ++j) {
+        if (i + j >= i1) break;
+        if (key[j] != name) {
+          flush(false);
+          name = key[j];
+          from_before = false;
+#pragma unroll
+          for (int e = 0; e < kVec; ++e) sum[e] = 0.0f;
+        }
+#pragma unroll
+        for (int e = 0; e < kVec; ++e) sum[e] += x[j].get(e);
+      }
+    }
+    flush(name == behind);
+  }
+}
+
+constexpr int64_t kMostPieces = 8192;
+
+// The names of several pieces: a workgroup adds up the parts of the one that begins
+// in its piece, 256 columns, each wave every fourth part.
+template <class W>
+__global__ void __launch_bounds__(256) te_join(const Embed d, const Pieces s, typename W::T* dw) {
+  constexpr int kCols = 4, kDeep = 8;
+  __shared__ float sums[4][64][kCols];
+  const uint32_t none = uint32_t(d.V);
+  const int64_t piece = blockIdx.x, i0 = piece * s.per, i1 = i0 + s.per;
+  if (i1 >= d.T) return;
+  const uint32_t name = s.key[i1 - 1];
+  if (name >= none || s.key[i1] != name) return;
+  if (i0 > 0 && s.key[i0 - 1] == name) return;
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  int64_t n = 1;  // parts: this piece's and those of the pieces behind it that begin with the name
+  for (;;) {
+    const int64_t at = (piece + n + lane) * s.per;
+    const int more = __popcll(__ballot(at < d.T && s.key[at < d.T ? at : 0] == name));
+    n += more;
+    if (more < 64) break;
+  }
+  const int32_t c = (int32_t(blockIdx.y) * 64 + lane) * kCols;
+  const int some = d.width - c;
+  float sum[kCols] = {};
+  for (int64_t q = wave; q < n; q += 4 * kDeep) {
+    float x[kDeep][kCols];
+#pragma unroll
+    for (int j = 0; j < kDeep; ++j) {
+      const int64_t part = q + 4 * j;
+      const float* p = (part ? s.head : s.tail) + (piece + part) * d.width + c;
+#pragma unroll
+      for (int e = 0; e < kCols; ++e) x[j][e] = part < n && e < some ? p[e] : 0.0f;
     }
 #pragma unroll
-    for (int e = 0; e < kVec; ++e) sum[e] *= d.scale;
-    Pack<W, kVec> o;
-    o.set(sum);
-    typename W::T* p = dw + v * d.weight_stride + c;
-    if (some >= kVec) o.store(p);
-    else o.store_some(p, some);
+    for (int j = 0; j < kDeep; ++j)
+#pragma unroll
+      for (int e = 0; e < kCols; ++e) sum[e] += x[j][e];
+  }
+#pragma unroll
+  for (int e = 0; e < kCols; ++e) sums[wave][lane][e] = sum[e];
+  __syncthreads();
+  if (wave) return;
+#pragma unroll
+  for (int e = 0; e < kCols; ++e) {
+    float t = sum[e];
+    for (int w = 1; w < 4; ++w) t += sums[w][lane][e];
+    if (e < some) dw[int64_t(name) * d.weight_stride + c + e] = typename W::T(t * d.scale);
+  }
+}
+
+// Rows that no token names, kZeroRows by a group of 2^lg lanes.
+constexpr int kZeroRows = 8;
+template <class W>
+__global__ void __launch_bounds__(256) te_zero(const Embed d, const uint8_t* named, typename W::T* dw, int lg) {
+  const int lanes = 1 << lg;
+  const int64_t v0 = (int64_t(row_block()) * (256 >> lg) + (threadIdx.x >> lg)) * kZeroRows;
+  Pack<W, kVec> o;
+  o.zero();
+  for (int64_t v = v0; v < v0 + kZeroRows && v < d.V; ++v) {
+    if (named[v]) continue;
+    for (int32_t c = int32_t(threadIdx.x & (lanes - 1)) * kVec; c < d.width; c += lanes * kVec) {
+      typename W::T* p = dw + v * d.weight_stride + c;
+      if (d.width - c >= kVec) o.store(p);
+      else o.store_some(p, d.width - c);
+    }
   }
 }
 
@@ -207,8 +330,9 @@ int check(const nopfs_embed* p) {
   if ((p->V > 1 && p->weight_stride < p->width) || (p->T > 1 && p->out_stride < p->width))
     return fail(NOPFS_EINVAL, "rows overlap");
   if (p->T > INT32_MAX || p->V > INT32_MAX - 1) return fail(NOPFS_ERANGE, "T must be < 2^31, V <= 2^31 - 2");
-  if (p->width > 1 << 28 || p->weight_stride > 1 << 28 || p->out_stride > 1 << 28)  // byte offsets below 2^63
-    return fail(NOPFS_ERANGE, "width and row strides must be <= 2^28");
+  if (p->width > 1 << 23) return fail(NOPFS_ERANGE, "width must be <= 2^23");
+  if (p->weight_stride > 1 << 28 || p->out_stride > 1 << 28)  // byte offsets below 2^63
+    return fail(NOPFS_ERANGE, "row strides must be <= 2^28");
   return NOPFS_OK;
 }
 
@@ -254,34 +378,51 @@ int embed_grad_impl(const nopfs_embed* p, const void* dout, const void* ids, con
   s.bits = std::max(1, int(ceil_div(bits, passes)));
   s.tiles = int32_t(std::min<int64_t>(128, ceil_div(p->T, kSortTile)));
   s.per_tile = s.tiles ? int32_t(ceil_div(p->T, s.tiles)) : 0;
+  Pieces pc{};
+  pc.per = 32;
+  while (ceil_div(p->T, pc.per) > kMostPieces) pc.per *= 2;
+  pc.n = int32_t(ceil_div(p->T, pc.per));
   Scratch sc(st);
   uint32_t *key[2], *val[2];
-  const size_t n = size_t(std::max<int64_t>(p->T, 1));
+  const size_t n = size_t(std::max<int64_t>(p->T, 1)), parts = size_t(std::max(1, pc.n)) * size_t(p->width);
   for (int i = 0; i < 2; ++i) {
     if ((rc = step_alloc(&sc, &key[i], n)) || (rc = step_alloc(&sc, &val[i], n))) return rc;
   }
-  if ((rc = step_alloc(&sc, &s.hist, size_t(std::max(1, s.tiles)) << s.bits))) return rc;
+  if ((rc = step_alloc(&sc, &s.hist, size_t(std::max(1, s.tiles)) << s.bits)) ||
+      (rc = step_alloc(&sc, &s.named, size_t(p->V))) || (rc = step_alloc(&sc, &pc.head, parts)) ||
+      (rc = step_alloc(&sc, &pc.tail, parts)))
+    return rc;
   int at = 0;
   for (int pass = 0; pass < passes; ++pass, at ^= 1) {
     s.key_in = key[at ^ 1], s.val_in = val[at ^ 1], s.key = key[at], s.val = val[at];
     s.shift = pass * s.bits;
-    const dim3 grid(uint32_t(s.tiles));
+    const dim3 grid(uint32_t(std::max(1, s.tiles)));  // without tokens the first count clears `named`
+    if (pass > 0 && !s.tiles) break;
     rc = pass == 0 ? launch("te_count", te_count<true>, grid, dim3(256), 0, st, d, s)
                    : launch("te_count", te_count<false>, grid, dim3(256), 0, st, d, s);
-    if (rc) return rc;
+    if (rc || !s.tiles) break;
     rc = pass == 0 ? launch("te_scatter", te_scatter<true>, grid, dim3(256), 0, st, d, s)
                    : launch("te_scatter", te_scatter<false>, grid, dim3(256), 0, st, d, s);
-    if (rc) return rc;
+    if (rc) break;
   }
+  if (rc) return rc;
   at ^= 1;
+  pc.key = key[at], pc.val = val[at];
   const int lg = row_lanes(p->width);
-  const int64_t blocks = ceil_div(p->V, 256 >> lg);
   return by_dtype(p->weight_dtype, [&](auto w) {
     return by_dtype(p->dtype, [&](auto e) {
       typedef decltype(w) W;
       typedef decltype(e) E;
-      return launch("te_sum", te_sum<W, E>, row_grid(blocks), dim3(256), 0, st, d,
-                    static_cast<const typename E::T*>(dout), key[at], val[at], static_cast<typename W::T*>(dw), lg);
+      typename W::T* to = static_cast<typename W::T*>(dw);
+      int r = launch("te_zero", te_zero<W>, row_grid(ceil_div(p->V, (256 >> lg) * kZeroRows)), dim3(256), 0, st, d,
+                     s.named, to, lg);
+      if (!r)
+        r = launch("te_pieces", te_pieces<W, E>, row_grid(ceil_div(pc.n, 256 >> lg)), dim3(256), 0, st, d, pc,
+                   static_cast<const typename E::T*>(dout), to, lg);
+      if (!r)
+        r = launch("te_join", te_join<W>, dim3(uint32_t(pc.n), uint32_t(ceil_div(p->width, 256))), dim3(256), 0, st, d,
+                   pc, to);
+      return r;
     });
   });
 }
