@@ -4,10 +4,11 @@
 // from h0 at a sample's first token, and for the gradient, from the last token back,
 //     G_t = dh_t + R_{t+1},  R_t = a_t G_t,  dx_t = k_t G_t,
 //     dgate_t = a_t k_t (h_{t-1} - x_t) G_t.
-// A stretch of tokens is a map h -> A h + B (A the product of the a, 0 from a
-// sample's start on), so the stretches are summed up side by side, their maps are
-// applied one after the other, and each stretch is gone through again from its own
-// first state. Bound by memory.
+// A stretch of tokens is a map h -> A h + B (A the product of the a), or a constant
+// if a sample begins in it. A wave holds 16 tokens of its channels in registers, makes
+// their map, gets the state before them through the maps of the stretches before, and
+// goes through its tokens again from there. Everything is read once and written once.
+// Bound by memory.
 //
 // The states and maps are in 32 bits. A step is taken from the larger share,
 // h + k (x - h) or x + a (h - x), so that its rounding is half a unit of the
@@ -20,19 +21,20 @@ namespace {
 constexpr int kRows = NOPFS_SCAN_CHUNK;  // tokens of a wave
 constexpr int kWaves = 8;
 constexpr int kTile = kRows * kWaves;    // tokens of a workgroup
-constexpr float kReset = -1.0f;          // a map that has lost its state: A where B is all
+constexpr int kWindow = 2 * kWaves;      // chunks that a chunk looks back over
 
 struct Scan {
   int64_t T;
   int32_t n, channels;
-  int32_t tiles;  // of channels
+  int32_t tiles, chunks;  // of channels; of tokens
   int64_t x_stride, gate_stride, h_stride, dh_stride, dx_stride, dgate_stride;
   const void *x, *gate, *dh;
   const int32_t* start;
   const float *h0, *dlast, *carry_in;
   void *h, *dx, *dgate;
   float *last, *carry, *dh0;
-  float *A, *B, *state;  // [chunks][channels]: the chunks' maps, the states before them
+  uint32_t* ticket;
+  uint64_t* slots;  // [chunks][channels]: what a chunk has said so far
 };
 
 // A lane's channels, one word of them.
@@ -58,12 +60,15 @@ __device__ __forceinline__ void load_rows(const void* base, int64_t stride, int6
                                           Pack<E, kChannels<E>> (&v)[kRows]) {
   const typename E::T* p = static_cast<const typename E::T*>(base) + t * stride + col.c;
 #pragma unroll
-  for (int r = 0; r < kRows; ++r) {
-    v[r].zero();
-    if (r < rows) {
-      if (col.n == Cols<E>::kN) v[r].load(p + r * stride);
-      else if (col.n > 0) v[r].load_some(p + r * stride, col.n);
-    }
+  for (int r = 0; r < kRows; ++r) v[r].zero();
+  if (col.n == Cols<E>::kN) {
+#pragma unroll
+    for (int r = 0; r < kRows; ++r)
+      if (r < rows) v[r].load(p + r * stride);
+  } else if (col.n > 0) {
+#pragma unroll
+    for (int r = 0; r < kRows; ++r)
+      if (r < rows) v[r].load_some(p + r * stride, col.n);
   }
 }
 template <class E>
@@ -90,31 +95,31 @@ __device__ __forceinline__ void store_state(float* base, int64_t row, const Scan
     if (i < n) base[row * d.channels + c + i] = v[i];
 }
 
-// The smaller of a and k = 1 - a, in 32 bits of its own, with the gate's sign
-// (negative: it is a).
+// The smaller of a and k = 1 - a, with the gate's sign (negative: it is a). Of
+// gates in 32 bits the exponent's rounding is made up for; those of 16 bits leave
+// it, |gate| units of 2^-24 of the share, far below their own outputs' roundings.
+template <class E>
 __device__ __forceinline__ float share_of(float gate) {
-  const float g = fabsf(gate);
   constexpr float kLog2e = 1.4426950408889634f, kLog2eLow = 1.9259629911266175e-8f, kLn2 = 0.6931471805599453f;
-  const float t = -g * kLog2e;
-  const float low = fmaf(-g, kLog2e, -t) - g * kLog2eLow;  // what t has lost
+  const float g = fabsf(gate), t = -g * kLog2e;
   float e = __builtin_amdgcn_exp2f(t);
-  e = fmaf(e * kLn2, low, e);
-  const float s = 1.0f + e;
-  float r = __builtin_amdgcn_rcpf(s);
-  r = fmaf(r, fmaf(-s, r, 1.0f), r);
-  return copysignf(e * r, gate);
+  if constexpr (sizeof(typename E::T) == 4) {
+    const float low = fmaf(-g, kLog2e, -t) - g * kLog2eLow;  // what t has lost
+    e = fmaf(e * kLn2, low, e);
+  }
+  return copysignf(e * __builtin_amdgcn_rcpf(1.0f + e), gate);
 }
-__device__ __forceinline__ bool is_a(float share) { return __float_as_uint(share) >> 31; }
+__device__ __forceinline__ bool is_a(float share) { return __float_as_int(share) < 0; }
 __device__ __forceinline__ float a_of(float share) { return is_a(share) ? -share : 1.0f - share; }
-__device__ __forceinline__ float k_of(float share) { return is_a(share) ? 1.0f + share : share; }
 __device__ __forceinline__ float step(float share, float h, float x) {
-  const float d = x - h;
-  return is_a(share) ? fmaf(share, d, x) : fmaf(share, d, h);  // x + a (h - x), h + k (x - h)
+  return fmaf(share, x - h, is_a(share) ? x : h);  // x + a (h - x), or h + k (x - h)
 }
-__device__ __forceinline__ float decay(float share, float g) {  // a g
-  return is_a(share) ? -share * g : fmaf(-share, g, g);
+// G's two shares, a G and k G.
+__device__ __forceinline__ void split(float share, float G, float* aG, float* kG) {
+  const float small = fabsf(share) * G, large = G - small;
+  *aG = is_a(share) ? small : large;
+  *kG = is_a(share) ? large : small;
 }
-__device__ __forceinline__ float apply(float A, float B, float h) { return A < 0.0f ? B : fmaf(A, h, B); }
 
 // Where samples begin and end among a workgroup's tokens.
 struct Marks {
@@ -161,130 +166,200 @@ __device__ __forceinline__ uint32_t wave_marks(const int32_t* m) {
   return uint32_t(__ballot(lane < kRows && m[(threadIdx.x >> 6) * kRows + (lane & (kRows - 1))] != 0));
 }
 
-// A wave's map of its rows, forwards.
-template <class E>
-__device__ __forceinline__ void forward_map(const Scan& d, const Pack<E, kChannels<E>> (&x)[kRows],
-                                            const Pack<E, kChannels<E>> (&g)[kRows], int rows, uint32_t first,
-                                            const int32_t* samples, const Cols<E>& col, float (&A)[kChannels<E>],
-                                            float (&B)[kChannels<E>]) {
-  constexpr int kN = kChannels<E>;
-#pragma unroll
-  for (int i = 0; i < kN; ++i) A[i] = 1.0f, B[i] = 0.0f;
-#pragma unroll
-  for (int r = 0; r < kRows; ++r) {
-    if (r >= rows) continue;
-    if (first >> r & 1) {
-#pragma unroll
-      for (int i = 0; i < kN; ++i) A[i] = kReset, B[i] = 0.0f;
-      if (d.h0) load_state<kN>(d.h0, samples[r] - 1, d, col.c, col.n, B);
-    }
-#pragma unroll
-    for (int i = 0; i < kN; ++i) {
-      const float share = share_of(g[r].get(i));
-      B[i] = step(share, B[i], x[r].get(i));
-      A[i] = A[i] < 0.0f ? A[i] : A[i] * a_of(share);
-    }
-  }
+// ---- from chunk to chunk ------------------------------------------------------
+// A chunk's state behind it is B + A times the state before it. Every chunk first
+// says its map (A, B), which takes only its own tokens, and then, when it knows the
+// state before it, the state behind it, which is a map with nothing of what came
+// before. A chunk takes the state behind the kWindow-th chunk before it and applies
+// the maps of those between: so the chain is one wait for every kWindow chunks, and
+// the bits are the same as from chunk to chunk, whatever has been said by when.
+//
+// A slot is one 64-bit word, written and read whole, so it needs no order with
+// others: the upper half is A with its sign bit set (A is in 0 .. 1, or NaN), or
+// kAbsolute; 0: nothing yet. A workgroup draws its chunk from a counter, so all
+// chunks that it waits for have been drawn by workgroups that run or have run.
+constexpr uint32_t kAbsolute = 0xFF800000u;
+
+__device__ __forceinline__ uint64_t slot_map(float A, float B) {
+  return uint64_t(__float_as_uint(A) | 0x80000000u) << 32 | __float_as_uint(B);
+}
+__device__ __forceinline__ uint64_t slot_state(float h) { return uint64_t(kAbsolute) << 32 | __float_as_uint(h); }
+__device__ __forceinline__ float through(uint64_t slot, float h) {
+  const uint32_t code = uint32_t(slot >> 32);
+  const float B = __uint_as_float(uint32_t(slot));
+  return code == kAbsolute ? B : fmaf(__uint_as_float(code & 0x7FFFFFFFu), h, B);
 }
 
-// Grid: chunks by tiles of channels. Each chunk's map.
-template <class E>
-__global__ void __launch_bounds__(64 * kWaves) gs_sums(const Scan d) {
-  constexpr int kN = kChannels<E>;
-  __shared__ Marks marks;
-  __shared__ float As[kWaves][64 * kN], Bs[kWaves][64 * kN];
-  const uint32_t chunk = row_block() / uint32_t(d.tiles), tile = row_block() % uint32_t(d.tiles);
+// The maps of a workgroup's waves; of a wave with a reset, A is not used.
+template <int kN>
+struct Maps {
+  float A[kWaves][64 * kN], B[kWaves][64 * kN];
+  uint32_t reset[kWaves];
+};
+template <int kN>
+__device__ __forceinline__ void keep_map(Maps<kN>* m, bool reset, const float (&A)[kN], const float (&B)[kN]) {
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-  const int64_t t0 = int64_t(chunk) * kTile, total = tokens_of(d);
-  if (t0 >= d.T) return;
-  const Cols<E> col = make_cols<E>(d, tile);
-  const int64_t t = t0 + wave * kRows;
-  const int rows = total <= t ? 0 : total - t < kRows ? int(total - t) : kRows;
-  Pack<E, kN> x[kRows], g[kRows];
-  load_rows<E>(d.x, d.x_stride, t, rows, col, x);
-  load_rows<E>(d.gate, d.gate_stride, t, rows, col, g);
-  make_marks(d, t0, total, &marks);
-  float A[kN], B[kN];
-  forward_map<E>(d, x, g, rows, wave_marks(marks.first), marks.first + wave * kRows, col, A, B);
 #pragma unroll
-  for (int i = 0; i < kN; ++i) As[wave][lane * kN + i] = A[i], Bs[wave][lane * kN + i] = B[i];
-  __syncthreads();
-  if (wave) return;
-  for (int w = 1; w < kWaves; ++w) {
+  for (int i = 0; i < kN; ++i) m->A[wave][i * 64 + lane] = A[i], m->B[wave][i * 64 + lane] = B[i];
+  if (lane == 0) m->reset[wave] = reset;
+}
+template <int kN>
+__device__ __forceinline__ void through_wave(const Maps<kN>& m, int w, float (&h)[kN]) {
+  const int lane = threadIdx.x & 63;
+  const bool reset = m.reset[w];
 #pragma unroll
-    for (int i = 0; i < kN; ++i) {
-      const float a = As[w][lane * kN + i], b = Bs[w][lane * kN + i];
-      B[i] = apply(a, b, B[i]);
-      A[i] = a < 0.0f ? kReset : A[i] < 0.0f ? A[i] : A[i] * a;
-    }
+  for (int i = 0; i < kN; ++i) {
+    const float A = m.A[w][i * 64 + lane], B = m.B[w][i * 64 + lane];
+    h[i] = reset ? B : fmaf(A, h[i], B);
   }
-  store_state<kN>(d.A, chunk, d, col.c, col.n, A);
-  store_state<kN>(d.B, chunk, d, col.c, col.n, B);
 }
 
-// A thread per channel: the states before the chunks (kBack: behind them).
-template <bool kBack>
-__global__ void __launch_bounds__(64) gs_states(const Scan d, int32_t chunks) {
-  const int64_t c = int64_t(blockIdx.x) * 64 + threadIdx.x;
-  if (c >= d.channels) return;
-  float h = 0.0f;
-  for (int32_t j = 0; j < chunks; ++j) {
-    const int64_t at = int64_t(kBack ? chunks - 1 - j : j) * d.channels + c;
-    d.state[at] = h;
-    h = apply(d.A[at], d.B[at], h);
+// The work of a workgroup: (chunk, tile of channels), in the order of the chain.
+template <bool kChain>
+__device__ __forceinline__ uint32_t draw(const Scan& d) {
+  if (!kChain) return row_block();
+  __shared__ uint32_t drawn;
+  if (threadIdx.x == 0) drawn = atomicAdd(d.ticket, 1u);
+  __syncthreads();
+  return drawn;
+}
+
+// The state before chunk number `at` of the chain (kBack: chunk chunks - 1 - at);
+// tells the others the chunk's map and the state behind it. After a barrier behind
+// keep_map. All waves get the state.
+template <bool kBack, int kN>
+__device__ inline void chain(const Scan& d, int32_t at, int32_t c, int n, const Maps<kN>& maps,
+                             uint64_t (&window)[kWindow][64 * kN], float (&h)[kN]) {
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  auto slot = [&](int32_t j) { return d.slots + int64_t(kBack ? d.chunks - 1 - j : j) * d.channels + c; };
+  float A[kN], B[kN];
+  bool reset = false;
+  if (wave == 0) {
+#pragma unroll
+    for (int i = 0; i < kN; ++i) A[i] = 1.0f, B[i] = 0.0f;
+    for (int j = 0; j < kWaves; ++j) {
+      const int w = kBack ? kWaves - 1 - j : j;
+      through_wave<kN>(maps, w, B);
+      reset |= maps.reset[w] != 0;
+#pragma unroll
+      for (int i = 0; i < kN; ++i) A[i] *= maps.A[w][i * 64 + lane];
+    }
+#pragma unroll
+    for (int i = 0; i < kN; ++i)
+      if (i < n)
+        __hip_atomic_store(slot(at) + i, reset ? slot_state(B[i]) : slot_map(A[i], B[i]), __ATOMIC_RELAXED,
+                           __HIP_MEMORY_SCOPE_AGENT);
   }
+  // each wave waits for its chunks of the window: the farthest has to know its state
+  for (int j = wave; j < kWindow; j += kWaves) {
+    const int32_t from = at - 1 - j;
+    if (from < 0) break;
+#pragma unroll
+    for (int i = 0; i < kN; ++i) {
+      uint64_t v = 0;
+      for (;;) {
+        if (i < n) v = __hip_atomic_load(slot(from) + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        const uint32_t code = uint32_t(v >> 32);
+        const bool ready = j == kWindow - 1 ? code == kAbsolute : code != 0;
+        if (__all(i >= n || ready)) break;
+        __builtin_amdgcn_s_sleep(1);
+      }
+      window[j][i * 64 + lane] = v;
+    }
+  }
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < kN; ++i) h[i] = 0.0f;
+  for (int j = at < kWindow ? at - 1 : kWindow - 1; j >= 0; --j) {
+#pragma unroll
+    for (int i = 0; i < kN; ++i) h[i] = through(window[j][i * 64 + lane], h[i]);
+  }
+  if (wave == 0 && !reset) {
+#pragma unroll
+    for (int i = 0; i < kN; ++i)
+      if (i < n)
+        __hip_atomic_store(slot(at) + i, slot_state(fmaf(A[i], h[i], B[i])), __ATOMIC_RELAXED,
+                           __HIP_MEMORY_SCOPE_AGENT);
+  }
+}
+
+// Nothing said, nothing drawn.
+__global__ void __launch_bounds__(256) gs_clear(const Scan d) {
+  const int64_t n = int64_t(d.chunks) * d.channels;
+  for (int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x; i < n; i += int64_t(gridDim.x) * 256) d.slots[i] = 0;
+  if (blockIdx.x == 0 && threadIdx.x == 0) *d.ticket = 0;
 }
 
 // Samples without tokens: their states go through. Workgroups behind the last
 // chunk's, 64 samples by a tile of 64 channels each.
-__device__ inline void empty_samples(const Scan& d, int64_t block, int32_t tiles64, const float* from, float* to) {
-  const int32_t tile = int32_t(block % tiles64);
-  const int32_t c = tile * 64 + int32_t(threadIdx.x & 63);
+__device__ inline void empty_samples(const Scan& d, int64_t block, const float* from, float* to) {
+  const int32_t tiles64 = (d.channels + 63) / 64;
+  const int32_t c = int32_t(block % tiles64) * 64 + int32_t(threadIdx.x & 63);
   const int64_t s0 = block / tiles64 * 64;
   if (c >= d.channels) return;
   for (int64_t s = s0 + (threadIdx.x >> 6); s < s0 + 64 && s < d.n; s += kWaves)
     if (d.start[s] >= d.start[s + 1]) to[s * d.channels + c] = from ? from[s * d.channels + c] : 0.0f;
 }
 
-template <class E>
-__global__ void __launch_bounds__(64 * kWaves) gs_forward(const Scan d, uint32_t blocks) {
+template <class E, bool kChain>
+__global__ void __launch_bounds__(64 * kWaves, 6) gs_forward(const Scan d, uint32_t blocks) {
   constexpr int kN = kChannels<E>;
   __shared__ Marks marks;
-  __shared__ float As[kWaves][64 * kN], Bs[kWaves][64 * kN];
+  __shared__ Maps<kN> maps;
+  __shared__ uint64_t window[kChain ? kWindow : 1][64 * kN];
   if (row_block() >= blocks) {
-    const int32_t tiles64 = (d.channels + 63) / 64;
-    if (d.last) empty_samples(d, row_block() - blocks, tiles64, d.h0, d.last);
+    if (d.last) empty_samples(d, row_block() - blocks, d.h0, d.last);
     return;
   }
-  const uint32_t chunk = row_block() / uint32_t(d.tiles), tile = row_block() % uint32_t(d.tiles);
-  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-  const int64_t t0 = int64_t(chunk) * kTile, total = tokens_of(d);
-  const Cols<E> col = make_cols<E>(d, tile);
-  const int64_t t = t0 + wave * kRows;
+  const uint32_t work = draw<kChain>(d), chunk = work / uint32_t(d.tiles);
+  const int wave = threadIdx.x >> 6;
+  const Cols<E> col = make_cols<E>(d, work % uint32_t(d.tiles));
+  const int64_t t0 = int64_t(chunk) * kTile, t = t0 + wave * kRows;
+  const int there = t >= d.T ? 0 : d.T - t < kRows ? int(d.T - t) : kRows;  // rows; `rows` of them in samples
+  Pack<E, kN> x[kRows];
+  float share[kRows][kN];
+  {
+    Pack<E, kN> g[kRows];
+    load_rows<E>(d.gate, d.gate_stride, t, there, col, g);
+    load_rows<E>(d.x, d.x_stride, t, there, col, x);
+#pragma unroll
+    for (int r = 0; r < kRows; ++r)
+#pragma unroll
+      for (int i = 0; i < kN; ++i) share[r][i] = share_of<E>(g[r].get(i));
+  }
+  const int64_t total = tokens_of(d);
   const int rows = total <= t ? 0 : total - t < kRows ? int(total - t) : kRows;
-  Pack<E, kN> x[kRows], g[kRows];
-  load_rows<E>(d.x, d.x_stride, t, rows, col, x);
-  load_rows<E>(d.gate, d.gate_stride, t, rows, col, g);
-  float h[kN] = {};
-  if (d.state) load_state<kN>(d.state, chunk, d, col.c, col.n, h);
   make_marks(d, t0, total, &marks);
   const uint32_t first = wave_marks(marks.first), end = wave_marks(marks.end);
-  const int32_t* starts = marks.first + wave * kRows;
+  const int32_t *starts = marks.first + wave * kRows, *ends = marks.end + wave * kRows;
   {
     float A[kN], B[kN];
-    forward_map<E>(d, x, g, rows, first, starts, col, A, B);
 #pragma unroll
-    for (int i = 0; i < kN; ++i) As[wave][lane * kN + i] = A[i], Bs[wave][lane * kN + i] = B[i];
+    for (int i = 0; i < kN; ++i) A[i] = 1.0f, B[i] = 0.0f;
+#pragma unroll
+    for (int r = 0; r < kRows; ++r) {
+      if (r >= rows) continue;
+      if (first >> r & 1) {
+#pragma unroll
+        for (int i = 0; i < kN; ++i) B[i] = 0.0f;
+        if (d.h0) load_state<kN>(d.h0, starts[r] - 1, d, col.c, col.n, B);
+      }
+#pragma unroll
+      for (int i = 0; i < kN; ++i) {
+        B[i] = step(share[r][i], B[i], x[r].get(i));
+        A[i] *= a_of(share[r][i]);
+      }
+    }
+    keep_map<kN>(&maps, first != 0, A, B);
   }
   __syncthreads();
-  for (int w = 0; w < wave; ++w) {
-#pragma unroll
-    for (int i = 0; i < kN; ++i) h[i] = apply(As[w][lane * kN + i], Bs[w][lane * kN + i], h[i]);
-  }
+  float h[kN] = {};
+  if constexpr (kChain) chain<false, kN>(d, int32_t(chunk), col.c, col.n, maps, window, h);
+  for (int w = 0; w < wave; ++w) through_wave<kN>(maps, w, h);
   const float none[kN] = {};
 #pragma unroll
   for (int r = 0; r < kRows; ++r) {
-    if (t + r >= d.T) break;
+    if (r >= there) continue;
     if (r >= rows) {
       if (r == 0 && d.carry) store_state<kN>(d.carry, t / kRows, d, col.c, col.n, none);
       store_row<E>(d.h, d.h_stride, t + r, col, none);
@@ -297,106 +372,69 @@ __global__ void __launch_bounds__(64 * kWaves) gs_forward(const Scan d, uint32_t
     }
     if (r == 0 && d.carry) store_state<kN>(d.carry, t / kRows, d, col.c, col.n, h);
 #pragma unroll
-    for (int i = 0; i < kN; ++i) h[i] = step(share_of(g[r].get(i)), h[i], x[r].get(i));
+    for (int i = 0; i < kN; ++i) h[i] = step(share[r][i], h[i], x[r].get(i));
     store_row<E>(d.h, d.h_stride, t + r, col, h);
-    if ((end >> r & 1) && d.last)
-      store_state<kN>(d.last, marks.end[wave * kRows + r] - 1, d, col.c, col.n, h);
+    if ((end >> r & 1) && d.last) store_state<kN>(d.last, ends[r] - 1, d, col.c, col.n, h);
   }
 }
 
-// The map of a wave's rows backwards: R behind its last row to R before its first.
-template <class E>
-__device__ __forceinline__ void backward_map(const Scan& d, const Pack<E, kChannels<E>> (&g)[kRows],
-                                             const Pack<E, kChannels<E>> (&dh)[kRows], int rows, uint32_t end,
-                                             const int32_t* samples, const Cols<E>& col, float (&A)[kChannels<E>],
-                                             float (&B)[kChannels<E>]) {
-  constexpr int kN = kChannels<E>;
-#pragma unroll
-  for (int i = 0; i < kN; ++i) A[i] = 1.0f, B[i] = 0.0f;
-#pragma unroll
-  for (int r = kRows - 1; r >= 0; --r) {
-    if (r >= rows) continue;
-    if (end >> r & 1) {
-#pragma unroll
-      for (int i = 0; i < kN; ++i) A[i] = kReset, B[i] = 0.0f;
-      if (d.dlast) load_state<kN>(d.dlast, samples[r] - 1, d, col.c, col.n, B);
-    }
-#pragma unroll
-    for (int i = 0; i < kN; ++i) {
-      const float share = share_of(g[r].get(i));
-      B[i] = decay(share, dh[r].get(i) + B[i]);
-      A[i] = A[i] < 0.0f ? A[i] : A[i] * a_of(share);
-    }
-  }
-}
-
-template <class E>
-__global__ void __launch_bounds__(64 * kWaves) gs_grad_sums(const Scan d) {
+template <class E, bool kChain>
+__global__ void __launch_bounds__(64 * kWaves, 4) gs_grad(const Scan d, uint32_t blocks) {
   constexpr int kN = kChannels<E>;
   __shared__ Marks marks;
-  __shared__ float As[kWaves][64 * kN], Bs[kWaves][64 * kN];
-  const uint32_t chunk = row_block() / uint32_t(d.tiles), tile = row_block() % uint32_t(d.tiles);
-  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-  const int64_t t0 = int64_t(chunk) * kTile, total = tokens_of(d);
-  if (t0 >= d.T) return;
-  const Cols<E> col = make_cols<E>(d, tile);
-  const int64_t t = t0 + wave * kRows;
-  const int rows = total <= t ? 0 : total - t < kRows ? int(total - t) : kRows;
-  Pack<E, kN> g[kRows], dh[kRows];
-  load_rows<E>(d.gate, d.gate_stride, t, rows, col, g);
-  load_rows<E>(d.dh, d.dh_stride, t, rows, col, dh);
-  make_marks(d, t0, total, &marks);
-  float A[kN], B[kN];
-  backward_map<E>(d, g, dh, rows, wave_marks(marks.end), marks.end + wave * kRows, col, A, B);
-#pragma unroll
-  for (int i = 0; i < kN; ++i) As[wave][lane * kN + i] = A[i], Bs[wave][lane * kN + i] = B[i];
-  __syncthreads();
-  if (wave != kWaves - 1) return;
-  for (int w = kWaves - 2; w >= 0; --w) {
-#pragma unroll
-    for (int i = 0; i < kN; ++i) {
-      const float a = As[w][lane * kN + i], b = Bs[w][lane * kN + i];
-      B[i] = apply(a, b, B[i]);
-      A[i] = a < 0.0f ? kReset : A[i] < 0.0f ? A[i] : A[i] * a;
-    }
-  }
-  store_state<kN>(d.A, chunk, d, col.c, col.n, A);
-  store_state<kN>(d.B, chunk, d, col.c, col.n, B);
-}
-
-template <class E>
-__global__ void __launch_bounds__(64 * kWaves) gs_grad(const Scan d, uint32_t blocks) {
-  constexpr int kN = kChannels<E>;
-  __shared__ Marks marks;
-  __shared__ float As[kWaves][64 * kN], Bs[kWaves][64 * kN];
+  __shared__ Maps<kN> maps;
+  __shared__ uint64_t window[kChain ? kWindow : 1][64 * kN];
   if (row_block() >= blocks) {
-    const int32_t tiles64 = (d.channels + 63) / 64;
-    if (d.dh0) empty_samples(d, row_block() - blocks, tiles64, d.dlast, d.dh0);
+    if (d.dh0) empty_samples(d, row_block() - blocks, d.dlast, d.dh0);
     return;
   }
-  const uint32_t chunk = row_block() / uint32_t(d.tiles), tile = row_block() % uint32_t(d.tiles);
-  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-  const int64_t t0 = int64_t(chunk) * kTile, total = tokens_of(d);
-  const Cols<E> col = make_cols<E>(d, tile);
-  const int64_t t = t0 + wave * kRows;
+  const uint32_t work = draw<kChain>(d);
+  const int32_t at = int32_t(work / uint32_t(d.tiles));
+  const int wave = threadIdx.x >> 6;
+  const Cols<E> col = make_cols<E>(d, work % uint32_t(d.tiles));
+  const int64_t t0 = int64_t(d.chunks - 1 - at) * kTile, t = t0 + wave * kRows;
+  const int there = t >= d.T ? 0 : d.T - t < kRows ? int(d.T - t) : kRows;
+  Pack<E, kN> dh[kRows];
+  float share[kRows][kN], under[kRows][kN];  // under: h_{t-1} - x_t
+  float h[kN] = {};
+  if (there > 0) load_state<kN>(d.carry_in, t / kRows, d, col.c, col.n, h);
+  Pack<E, kN> x[kRows];
+  {
+    Pack<E, kN> g[kRows];
+    load_rows<E>(d.gate, d.gate_stride, t, there, col, g);
+    load_rows<E>(d.dh, d.dh_stride, t, there, col, dh);
+    load_rows<E>(d.x, d.x_stride, t, there, col, x);
+#pragma unroll
+    for (int r = 0; r < kRows; ++r)
+#pragma unroll
+      for (int i = 0; i < kN; ++i) share[r][i] = share_of<E>(g[r].get(i));
+  }
+  const int64_t total = tokens_of(d);
   const int rows = total <= t ? 0 : total - t < kRows ? int(total - t) : kRows;
-  Pack<E, kN> x[kRows], g[kRows], dh[kRows];
-  load_rows<E>(d.x, d.x_stride, t, rows, col, x);
-  load_rows<E>(d.gate, d.gate_stride, t, rows, col, g);
-  load_rows<E>(d.dh, d.dh_stride, t, rows, col, dh);
-  float h[kN] = {}, R[kN] = {};
-  if (rows > 0) load_state<kN>(d.carry_in, t / kRows, d, col.c, col.n, h);
-  if (d.state) load_state<kN>(d.state, chunk, d, col.c, col.n, R);
   make_marks(d, t0, total, &marks);
   const uint32_t first = wave_marks(marks.first), end = wave_marks(marks.end);
   const int32_t *starts = marks.first + wave * kRows, *ends = marks.end + wave * kRows;
   {
-    float A[kN], B[kN];
-    backward_map<E>(d, g, dh, rows, end, ends, col, A, B);
+    float A[kN], R[kN];
 #pragma unroll
-    for (int i = 0; i < kN; ++i) As[wave][lane * kN + i] = A[i], Bs[wave][lane * kN + i] = B[i];
+    for (int i = 0; i < kN; ++i) A[i] = 1.0f, R[i] = 0.0f;
+#pragma unroll
+    for (int r = kRows - 1; r >= 0; --r) {
+      if (r >= rows) continue;
+      if (end >> r & 1) {
+#pragma unroll
+        for (int i = 0; i < kN; ++i) R[i] = 0.0f;
+        if (d.dlast) load_state<kN>(d.dlast, ends[r] - 1, d, col.c, col.n, R);
+      }
+#pragma unroll
+      for (int i = 0; i < kN; ++i) {
+        float kG;
+        split(share[r][i], dh[r].get(i) + R[i], &R[i], &kG);
+        A[i] *= a_of(share[r][i]);
+      }
+    }
+    keep_map<kN>(&maps, end != 0, A, R);
   }
-  float share[kRows][kN], under[kRows][kN];  // under: h_{t-1} - x_t
 #pragma unroll
   for (int r = 0; r < kRows; ++r) {
     if (r >= rows) continue;
@@ -407,19 +445,17 @@ __global__ void __launch_bounds__(64 * kWaves) gs_grad(const Scan d, uint32_t bl
     }
 #pragma unroll
     for (int i = 0; i < kN; ++i) {
-      share[r][i] = share_of(g[r].get(i));
       under[r][i] = h[i] - x[r].get(i);
       h[i] = step(share[r][i], h[i], x[r].get(i));
     }
   }
   __syncthreads();
-  for (int w = kWaves - 1; w > wave; --w) {
-#pragma unroll
-    for (int i = 0; i < kN; ++i) R[i] = apply(As[w][lane * kN + i], Bs[w][lane * kN + i], R[i]);
-  }
+  float R[kN] = {};
+  if constexpr (kChain) chain<true, kN>(d, at, col.c, col.n, maps, window, R);
+  for (int w = kWaves - 1; w > wave; --w) through_wave<kN>(maps, w, R);
 #pragma unroll
   for (int r = kRows - 1; r >= 0; --r) {
-    if (t + r >= d.T) continue;
+    if (r >= there) continue;
     float dx[kN] = {}, dg[kN] = {};
     if (r < rows) {
       if (end >> r & 1) {
@@ -430,9 +466,8 @@ __global__ void __launch_bounds__(64 * kWaves) gs_grad(const Scan d, uint32_t bl
 #pragma unroll
       for (int i = 0; i < kN; ++i) {
         const float G = dh[r].get(i) + R[i];
-        R[i] = decay(share[r][i], G);
-        dx[i] = k_of(share[r][i]) * G;
-        dg[i] = a_of(share[r][i]) * under[r][i] * dx[i];
+        split(share[r][i], G, &R[i], &dx[i]);
+        dg[i] = under[r][i] * (a_of(share[r][i]) * dx[i]);
       }
       if ((first >> r & 1) && d.dh0) store_state<kN>(d.dh0, starts[r] - 1, d, col.c, col.n, R);
     }
@@ -459,33 +494,29 @@ int check(const nopfs_scan* p, bool gradient) {
 // Workgroups: chunks by tiles of channels, and behind them those of the samples
 // without tokens, if a state is asked for.
 struct Grid {
-  int64_t chunks, blocks, all;
+  int64_t blocks, all;
 };
 int make_grid(const nopfs_scan* p, bool states, Scan* d, Grid* g) {
   const int per = 64 * (p->dtype == NOPFS_FP32 ? 1 : 2);
+  d->T = p->T, d->n = p->n, d->channels = p->channels;
+  d->x_stride = p->x_stride, d->gate_stride = p->gate_stride, d->h_stride = p->h_stride;
+  d->dh_stride = p->dh_stride, d->dx_stride = p->dx_stride, d->dgate_stride = p->dgate_stride;
   d->tiles = int32_t(ceil_div(p->channels, per));
-  g->chunks = ceil_div(p->T, kTile);
-  g->blocks = g->chunks * d->tiles;
+  d->chunks = int32_t(ceil_div(p->T, kTile));
+  g->blocks = int64_t(d->chunks) * d->tiles;
   g->all = g->blocks + (states ? ceil_div(p->n, 64) * ceil_div(p->channels, 64) : 0);
   if (g->all > INT32_MAX) return fail(NOPFS_ERANGE, "too many tokens, samples and channels for one call");
   return NOPFS_OK;
 }
 
-int alloc_maps(Scratch* sc, const Grid& g, Scan* d) {
-  if (g.chunks <= 1) return NOPFS_OK;
-  const size_t n = size_t(g.chunks) * size_t(d->channels);
+// What the chunks say to each other, if there are several, with nothing said yet.
+int make_chain(Scratch* sc, Scan* d, hipStream_t st) {
+  if (d->chunks <= 1) return NOPFS_OK;
   int rc;
-  if ((rc = step_alloc(sc, &d->A, n)) || (rc = step_alloc(sc, &d->B, n)) || (rc = step_alloc(sc, &d->state, n)))
-    return rc;
-  return NOPFS_OK;
-}
-
-Scan describe(const nopfs_scan* p) {
-  Scan d{};
-  d.T = p->T, d.n = p->n, d.channels = p->channels;
-  d.x_stride = p->x_stride, d.gate_stride = p->gate_stride, d.h_stride = p->h_stride;
-  d.dh_stride = p->dh_stride, d.dx_stride = p->dx_stride, d.dgate_stride = p->dgate_stride;
-  return d;
+  const size_t n = size_t(d->chunks) * size_t(d->channels);
+  if ((rc = step_alloc(sc, &d->slots, n)) || (rc = step_alloc(sc, &d->ticket, 1))) return rc;
+  return launch("gs_clear", gs_clear, dim3(uint32_t(std::min<int64_t>(ceil_div(int64_t(n), 1024), 4096))), dim3(256),
+                0, st, *d);
 }
 
 int scan_impl(const nopfs_scan* p, const void* x, const void* gate, const int32_t* start, const float* h0, void* h,
@@ -494,23 +525,16 @@ int scan_impl(const nopfs_scan* p, const void* x, const void* gate, const int32_
   if (rc) return rc;
   if (!start || (p->T > 0 && (!x || !gate || !h))) return fail(NOPFS_EINVAL, "x, gate, start and h must be non-NULL");
   if (last && last == h0) return fail(NOPFS_EINVAL, "last must not be h0");
-  Scan d = describe(p);
+  Scan d{};
   d.x = x, d.gate = gate, d.start = start, d.h0 = h0, d.h = h, d.last = last, d.carry = carry;
   Grid g;
   if ((rc = make_grid(p, last != nullptr, &d, &g))) return rc;
   Scratch sc(st);
-  if ((rc = alloc_maps(&sc, g, &d))) return rc;
+  if ((rc = make_chain(&sc, &d, st))) return rc;
   return by_dtype(p->dtype, [&](auto e) {
     typedef decltype(e) E;
-    int r = NOPFS_OK;
-    if (g.chunks > 1) {
-      r = launch("gs_sums", gs_sums<E>, row_grid(g.blocks), dim3(64 * kWaves), 0, st, d);
-      if (!r)
-        r = launch("gs_states", gs_states<false>, dim3(uint32_t(ceil_div(d.channels, 64))), dim3(64), 0, st, d,
-                   int32_t(g.chunks));
-    }
-    if (r) return r;
-    return launch("gs_forward", gs_forward<E>, row_grid(g.all), dim3(64 * kWaves), 0, st, d, uint32_t(g.blocks));
+    return launch("gs_forward", d.chunks > 1 ? gs_forward<E, true> : gs_forward<E, false>, row_grid(g.all),
+                  dim3(64 * kWaves), 0, st, d, uint32_t(g.blocks));
   });
 }
 
@@ -522,24 +546,17 @@ int scan_grad_impl(const nopfs_scan* p, const void* dh, const float* dlast, cons
   if (!start || (p->T > 0 && (!dh || !x || !gate || !carry || !dx || !dgate)))
     return fail(NOPFS_EINVAL, "d_h, x, gate, start, carry, d_x and d_gate must be non-NULL");
   if (dh0 && dh0 == dlast) return fail(NOPFS_EINVAL, "d_h0 must not be d_last");
-  Scan d = describe(p);
+  Scan d{};
   d.dh = dh, d.dlast = dlast, d.x = x, d.gate = gate, d.start = start, d.h0 = h0, d.carry_in = carry;
   d.dx = dx, d.dgate = dgate, d.dh0 = dh0;
   Grid g;
   if ((rc = make_grid(p, dh0 != nullptr, &d, &g))) return rc;
   Scratch sc(st);
-  if ((rc = alloc_maps(&sc, g, &d))) return rc;
+  if ((rc = make_chain(&sc, &d, st))) return rc;
   return by_dtype(p->dtype, [&](auto e) {
     typedef decltype(e) E;
-    int r = NOPFS_OK;
-    if (g.chunks > 1) {
-      r = launch("gs_grad_sums", gs_grad_sums<E>, row_grid(g.blocks), dim3(64 * kWaves), 0, st, d);
-      if (!r)
-        r = launch("gs_states", gs_states<true>, dim3(uint32_t(ceil_div(d.channels, 64))), dim3(64), 0, st, d,
-                   int32_t(g.chunks));
-    }
-    if (r) return r;
-    return launch("gs_grad", gs_grad<E>, row_grid(g.all), dim3(64 * kWaves), 0, st, d, uint32_t(g.blocks));
+    return launch("gs_grad", d.chunks > 1 ? gs_grad<E, true> : gs_grad<E, false>, row_grid(g.all), dim3(64 * kWaves),
+                  0, st, d, uint32_t(g.blocks));
   });
 }
 

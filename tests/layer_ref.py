@@ -145,7 +145,8 @@ def scan(x, gate, start, h0=None, dh=None, dlast=None):
     """h, last (and dx, dgate, dh0) token by token, and bounds.
 
     With s the smaller of a and k: s is off by 6 E (exponential 2, sum and reciprocal
-    3, product 1) and 0 below 2^-126, the larger, 1 - s, by E. A step's rounding is E of its result, E s
+    3, product 1), of gates in 16 bits by 1.3 |gate| E more (the exponent |gate| log2 e
+    is rounded, and so is log2 e), and 0 below 2^-126; the larger, 1 - s, by E. A step's rounding is E of its result, E s
     of the difference in it, and 6 E s of that difference for s. A stretch's map adds
     3 E of A h and 2 E of B for each of its steps. All of it is at most 16 E of what
     the step's magnitudes come to, M_t = a M_(t-1) + k |x_t| and s (|x_t| + M_(t-1)),
@@ -157,6 +158,7 @@ def scan(x, gate, start, h0=None, dh=None, dlast=None):
     z = lambda *s: torch.zeros(s, dtype=F64)  # noqa: E731
     a, k = torch.sigmoid(Gt), torch.sigmoid(-Gt)
     s = torch.minimum(a, k)
+    es = s * (0.0 if dt is torch.float32 else 1.3 * E * Gt.abs())
     val = dict(h=z(T, C), last=z(n, C) if h0 is None else _wide(h0))
     err = dict(h=z(T, C), last=z(n, C))
     before, ebefore, mag = z(T, C), z(T, C), z(T, C)
@@ -169,7 +171,7 @@ def scan(x, gate, start, h0=None, dh=None, dlast=None):
             h = a[t] * h + k[t] * X[t]
             grow = s[t] * (X[t].abs() + M)
             M = a[t] * M + k[t] * X[t].abs()
-            e = a[t] * e + 16 * E * (M + grow) + LEAST * (X[t].abs() + mag[t]) + TINY[torch.float32]
+            e = a[t] * e + 16 * E * (M + grow) + (es[t] + LEAST) * (X[t].abs() + mag[t]) + TINY[torch.float32]
             val["h"][t], err["h"][t] = h, e + u * h.abs() + tiny
         val["last"][i], err["last"][i] = h, e
     if dh is None:
@@ -184,13 +186,13 @@ def scan(x, gate, start, h0=None, dh=None, dlast=None):
             G, eG, NG = D[t] + R, e + E * (D[t].abs() + N), D[t].abs() + N
             diff, p = before[t] - X[t], a[t] * k[t]
             val["dx"][t] = k[t] * G
-            err["dx"][t] = k[t] * (eG + 9 * E * NG) + LEAST * NG + u * (k[t] * G).abs() + tiny
+            err["dx"][t] = k[t] * (eG + 9 * E * NG) + (es[t] + LEAST) * NG + u * (k[t] * G).abs() + tiny
             val["dgate"][t] = p * diff * G
             err["dgate"][t] = (p * (diff.abs() * eG + (ebefore[t] + E * (X[t].abs() + mag[t])) * NG
                                     + 18 * E * diff.abs() * NG)
-                               + LEAST * diff.abs() * NG
+                               + (2 * es[t] + LEAST) * diff.abs() * NG
                                + u * (p * diff * G).abs() + tiny)
             R, N = a[t] * G, a[t] * NG
-            e = a[t] * eG + 16 * E * N + 8 * E * s[t] * NG + LEAST * NG + TINY[torch.float32]
+            e = a[t] * eG + 16 * E * N + 8 * E * s[t] * NG + (es[t] + LEAST) * NG + TINY[torch.float32]
         val["dh0"][i], err["dh0"][i] = R, e
     return val, err
