@@ -21,7 +21,8 @@ namespace {
 constexpr int kRows = NOPFS_SCAN_CHUNK;  // tokens of a wave
 constexpr int kWaves = 8;
 constexpr int kTile = kRows * kWaves;    // tokens of a workgroup
-constexpr int kWindow = 2 * kWaves;      // chunks that a chunk looks back over
+constexpr int kGroup = 16;               // chunks from one known state to the next, a power of two
+constexpr int kLine = 32;                // words of 128 bytes
 
 struct Scan {
   int64_t T;
@@ -33,66 +34,83 @@ struct Scan {
   const float *h0, *dlast, *carry_in;
   void *h, *dx, *dgate;
   float *last, *carry, *dh0;
-  uint32_t* ticket;
-  uint64_t* slots;  // [chunks][channels]: what a chunk has said so far
+  uint32_t* drawn;  // [tiles]: chunks that workgroups have drawn, kLine words apart
+  uint64_t* slots;  // [chunks][tiles][64 kN]: what a chunk has said, of its lanes' first channels, then second
 };
 
 // A lane's channels, one word of them.
 template <class E>
 constexpr int kChannels = sizeof(typename E::T) == 4 ? 1 : 2;
 
+// What a wave shares goes through here, so that the compiler keeps it once and not
+// for every lane, and branches on it instead of masking lanes.
+__device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
+__device__ __forceinline__ int wave_id() { return uniform(int(threadIdx.x >> 6)); }
+
 template <class E>
 struct Cols {
   static constexpr int kN = kChannels<E>;
   int32_t c;  // the first
   int n;      // so many of them are there
+  bool full;  // all of the wave's
 };
 template <class E>
 __device__ __forceinline__ Cols<E> make_cols(const Scan& d, int32_t tile) {
   const int32_t c = (tile * 64 + int32_t(threadIdx.x & 63)) * Cols<E>::kN;
   const int32_t left = d.channels - c;
-  return {c, left < 0 ? 0 : left < Cols<E>::kN ? int(left) : Cols<E>::kN};
+  return {c, left < 0 ? 0 : left < Cols<E>::kN ? int(left) : Cols<E>::kN,
+          int64_t(tile + 1) * 64 * Cols<E>::kN <= d.channels};
 }
 
 // A wave's rows, `rows` of them.
 template <class E>
 __device__ __forceinline__ void load_rows(const void* base, int64_t stride, int64_t t, int rows, const Cols<E>& col,
                                           Pack<E, kChannels<E>> (&v)[kRows]) {
-  const typename E::T* p = static_cast<const typename E::T*>(base) + t * stride + col.c;
+  const typename E::T* p = static_cast<const typename E::T*>(base) + t * stride;
 #pragma unroll
   for (int r = 0; r < kRows; ++r) v[r].zero();
-  if (col.n == Cols<E>::kN) {
+  if (col.full && rows == kRows) {
+#pragma unroll
+    for (int r = 0; r < kRows; ++r) v[r].load(p + r * stride + uint32_t(col.c));
+  } else {
 #pragma unroll
     for (int r = 0; r < kRows; ++r)
-      if (r < rows) v[r].load(p + r * stride);
-  } else if (col.n > 0) {
-#pragma unroll
-    for (int r = 0; r < kRows; ++r)
-      if (r < rows) v[r].load_some(p + r * stride, col.n);
+      if (r < rows) {
+        if (col.n == Cols<E>::kN) v[r].load(p + r * stride + uint32_t(col.c));
+        else if (col.n > 0) v[r].load_some(p + r * stride + uint32_t(col.c), col.n);
+      }
   }
 }
 template <class E>
 __device__ __forceinline__ void store_row(void* base, int64_t stride, int64_t t, const Cols<E>& col,
                                           const float (&v)[kChannels<E>]) {
-  typename E::T* p = static_cast<typename E::T*>(base) + t * stride + col.c;
+  typename E::T* p = static_cast<typename E::T*>(base) + t * stride + uint32_t(col.c);
   Pack<E, kChannels<E>> o;
   o.set(v);
-  if (col.n == Cols<E>::kN) o.store(p);
+  if (col.full) o.store(p);
+  else if (col.n == Cols<E>::kN) o.store(p);
   else if (col.n > 0) o.store_some(p, col.n);
 }
-// A row of the 32-bit arrays of n or chunks rows.
-template <int kN>
-__device__ __forceinline__ void load_state(const float* base, int64_t row, const Scan& d, int32_t c, int n,
-                                           float (&v)[kN]) {
+// A row of the 32-bit arrays, of samples or chunks.
+template <class E>
+__device__ __forceinline__ void load_state(const float* base, int64_t row, const Scan& d, const Cols<E>& col,
+                                           float (&v)[kChannels<E>]) {
+  const float* p = base + row * d.channels + uint32_t(col.c);
 #pragma unroll
-  for (int i = 0; i < kN; ++i) v[i] = i < n ? base[row * d.channels + c + i] : 0.0f;
+  for (int i = 0; i < Cols<E>::kN; ++i) v[i] = col.full || i < col.n ? p[i] : 0.0f;
 }
-template <int kN>
-__device__ __forceinline__ void store_state(float* base, int64_t row, const Scan& d, int32_t c, int n,
-                                            const float (&v)[kN]) {
+template <class E>
+__device__ __forceinline__ void store_state(float* base, int64_t row, const Scan& d, const Cols<E>& col,
+                                            const float (&v)[kChannels<E>]) {
+  float* p = base + row * d.channels + uint32_t(col.c);
+  if (col.full) {
 #pragma unroll
-  for (int i = 0; i < kN; ++i)
-    if (i < n) base[row * d.channels + c + i] = v[i];
+    for (int i = 0; i < Cols<E>::kN; ++i) p[i] = v[i];
+  } else {
+#pragma unroll
+    for (int i = 0; i < Cols<E>::kN; ++i)
+      if (i < col.n) p[i] = v[i];
+  }
 }
 
 // The smaller of a and k = 1 - a, with the gate's sign (negative: it is a). Of
@@ -127,7 +145,7 @@ struct Marks {
 };
 // The tokens that belong to samples.
 __device__ __forceinline__ int64_t tokens_of(const Scan& d) {
-  const int64_t total = d.n > 0 ? d.start[d.n] : 0;
+  const int64_t total = d.n > 0 ? uniform(d.start[d.n]) : 0;
   return total < 0 ? 0 : total < d.T ? total : d.T;
 }
 // The first sample s in [lo, n) with start[s + 1] > t (n - 1 if none), 64 candidates at a time.
@@ -163,21 +181,21 @@ __device__ inline void make_marks(const Scan& d, int64_t t0, int64_t total, Mark
 // Bit r: row r of the wave.
 __device__ __forceinline__ uint32_t wave_marks(const int32_t* m) {
   const int lane = __lane_id();
-  return uint32_t(__ballot(lane < kRows && m[(threadIdx.x >> 6) * kRows + (lane & (kRows - 1))] != 0));
+  return uint32_t(__ballot(lane < kRows && m[wave_id() * kRows + (lane & (kRows - 1))] != 0));
 }
 
 // ---- from chunk to chunk ------------------------------------------------------
-// A chunk's state behind it is B + A times the state before it. Every chunk first
-// says its map (A, B), which takes only its own tokens, and then, when it knows the
-// state before it, the state behind it, which is a map with nothing of what came
-// before. A chunk takes the state behind the kWindow-th chunk before it and applies
-// the maps of those between: so the chain is one wait for every kWindow chunks, and
-// the bits are the same as from chunk to chunk, whatever has been said by when.
+// The state behind a chunk is B + A times the state before it. Every chunk says
+// its map (A, B), which takes only its own tokens; the last of a group of kGroup
+// chunks says, when it knows the state before it, the state behind it instead. A
+// chunk applies the maps of its group before it to the state behind the group
+// before. So the chain is one wait per group, and the order of all roundings is fixed.
 //
 // A slot is one 64-bit word, written and read whole, so it needs no order with
 // others: the upper half is A with its sign bit set (A is in 0 .. 1, or NaN), or
-// kAbsolute; 0: nothing yet. A workgroup draws its chunk from a counter, so all
-// chunks that it waits for have been drawn by workgroups that run or have run.
+// kAbsolute where the lower half is the state whatever came before; 0: nothing yet.
+// A workgroup draws its chunk from its tile's counter, so all chunks that it waits
+// for have been drawn by workgroups that run or have run.
 constexpr uint32_t kAbsolute = 0xFF800000u;
 
 __device__ __forceinline__ uint64_t slot_map(float A, float B) {
@@ -198,7 +216,7 @@ struct Maps {
 };
 template <int kN>
 __device__ __forceinline__ void keep_map(Maps<kN>* m, bool reset, const float (&A)[kN], const float (&B)[kN]) {
-  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  const int wave = wave_id(), lane = threadIdx.x & 63;
 #pragma unroll
   for (int i = 0; i < kN; ++i) m->A[wave][i * 64 + lane] = A[i], m->B[wave][i * 64 + lane] = B[i];
   if (lane == 0) m->reset[wave] = reset;
@@ -206,7 +224,7 @@ __device__ __forceinline__ void keep_map(Maps<kN>* m, bool reset, const float (&
 template <int kN>
 __device__ __forceinline__ void through_wave(const Maps<kN>& m, int w, float (&h)[kN]) {
   const int lane = threadIdx.x & 63;
-  const bool reset = m.reset[w];
+  const bool reset = uniform(m.reset[w]);
 #pragma unroll
   for (int i = 0; i < kN; ++i) {
     const float A = m.A[w][i * 64 + lane], B = m.B[w][i * 64 + lane];
@@ -214,80 +232,85 @@ __device__ __forceinline__ void through_wave(const Maps<kN>& m, int w, float (&h
   }
 }
 
-// The work of a workgroup: (chunk, tile of channels), in the order of the chain.
+// A workgroup's chunk of its tile of channels, in the order of the chain.
 template <bool kChain>
-__device__ __forceinline__ uint32_t draw(const Scan& d) {
-  if (!kChain) return row_block();
+__device__ __forceinline__ int32_t draw(const Scan& d, uint32_t tile) {
+  if (!kChain) return 0;
   __shared__ uint32_t drawn;
-  if (threadIdx.x == 0) drawn = atomicAdd(d.ticket, 1u);
+  if (threadIdx.x == 0) drawn = atomicAdd(d.drawn + tile * kLine, 1u);
   __syncthreads();
-  return drawn;
+  return uniform(int32_t(drawn));
 }
 
+// What the waves of a workgroup leave for each other on the way.
+template <int kN>
+struct Chain {
+  uint64_t said[kGroup][64 * kN];  // the state before the group, then the maps up to this chunk's
+  float state[64 * kN];
+};
+
 // The state before chunk number `at` of the chain (kBack: chunk chunks - 1 - at);
-// tells the others the chunk's map and the state behind it. After a barrier behind
-// keep_map. All waves get the state.
+// tells the others the chunk's map, or the state behind its group. After a barrier
+// behind keep_map. Wave i < kN works on the i-th channels of all lanes, the waves
+// share the waiting, and all get the state.
 template <bool kBack, int kN>
-__device__ inline void chain(const Scan& d, int32_t at, int32_t c, int n, const Maps<kN>& maps,
-                             uint64_t (&window)[kWindow][64 * kN], float (&h)[kN]) {
-  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-  auto slot = [&](int32_t j) { return d.slots + int64_t(kBack ? d.chunks - 1 - j : j) * d.channels + c; };
-  float A[kN], B[kN];
+__device__ inline void chain(const Scan& d, int32_t at, uint32_t tile, const Maps<kN>& maps, Chain<kN>* lds,
+                             float (&h)[kN]) {
+  const int wave = wave_id(), lane = threadIdx.x & 63, mine = wave * 64 + lane;
+  const int pos = at & (kGroup - 1);
+  uint64_t* slots = d.slots + (int64_t(at - pos) * d.tiles + tile) * 64 * kN;  // of the group's first chunk
+  const int64_t next = int64_t(d.tiles) * 64 * kN;
+  float A = 1.0f, B = 0.0f;
   bool reset = false;
-  if (wave == 0) {
+  if (wave < kN) {
 #pragma unroll
-    for (int i = 0; i < kN; ++i) A[i] = 1.0f, B[i] = 0.0f;
     for (int j = 0; j < kWaves; ++j) {
       const int w = kBack ? kWaves - 1 - j : j;
-      through_wave<kN>(maps, w, B);
-      reset |= maps.reset[w] != 0;
-#pragma unroll
-      for (int i = 0; i < kN; ++i) A[i] *= maps.A[w][i * 64 + lane];
+      const bool cut = uniform(maps.reset[w]);
+      const float a = maps.A[w][mine], b = maps.B[w][mine];
+      A *= a;
+      B = cut ? b : fmaf(a, B, b);
+      reset |= cut;
     }
-#pragma unroll
-    for (int i = 0; i < kN; ++i)
-      if (i < n)
-        __hip_atomic_store(slot(at) + i, reset ? slot_state(B[i]) : slot_map(A[i], B[i]), __ATOMIC_RELAXED,
-                           __HIP_MEMORY_SCOPE_AGENT);
+    if (pos < kGroup - 1 || reset)
+      __hip_atomic_store(slots + pos * next + mine, reset ? slot_state(B) : slot_map(A, B), __ATOMIC_RELAXED,
+                         __HIP_MEMORY_SCOPE_AGENT);
   }
-  // each wave waits for its chunks of the window: the farthest has to know its state
-  for (int j = wave; j < kWindow; j += kWaves) {
-    const int32_t from = at - 1 - j;
-    if (from < 0) break;
-#pragma unroll
-    for (int i = 0; i < kN; ++i) {
-      uint64_t v = 0;
+  for (int j = wave; j < (pos + 1) * kN; j += kWaves) {
+    const int from = j / kN, i = j & (kN - 1);  // 0: the chunk before the group
+    uint64_t v = slot_state(0.0f);
+    if (from > 0 || at >= kGroup) {
+      const uint64_t* p = slots + (from - 1) * next + i * 64 + lane;
       for (;;) {
-        if (i < n) v = __hip_atomic_load(slot(from) + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        v = __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
         const uint32_t code = uint32_t(v >> 32);
-        const bool ready = j == kWindow - 1 ? code == kAbsolute : code != 0;
-        if (__all(i >= n || ready)) break;
+        if (__all(from ? code != 0 : code == kAbsolute)) break;
         __builtin_amdgcn_s_sleep(1);
       }
-      window[j][i * 64 + lane] = v;
     }
+    lds->said[from][i * 64 + lane] = v;
+  }
+  __syncthreads();
+  if (wave < kN) {
+    float state = 0.0f;
+#pragma unroll
+    for (int j = 0; j < kGroup; ++j)
+      if (j <= pos) state = through(lds->said[j][mine], state);
+    if (pos == kGroup - 1 && !reset)
+      __hip_atomic_store(slots + pos * next + mine, slot_state(fmaf(A, state, B)), __ATOMIC_RELAXED,
+                         __HIP_MEMORY_SCOPE_AGENT);
+    lds->state[mine] = state;
   }
   __syncthreads();
 #pragma unroll
-  for (int i = 0; i < kN; ++i) h[i] = 0.0f;
-  for (int j = at < kWindow ? at - 1 : kWindow - 1; j >= 0; --j) {
-#pragma unroll
-    for (int i = 0; i < kN; ++i) h[i] = through(window[j][i * 64 + lane], h[i]);
-  }
-  if (wave == 0 && !reset) {
-#pragma unroll
-    for (int i = 0; i < kN; ++i)
-      if (i < n)
-        __hip_atomic_store(slot(at) + i, slot_state(fmaf(A[i], h[i], B[i])), __ATOMIC_RELAXED,
-                           __HIP_MEMORY_SCOPE_AGENT);
-  }
+  for (int i = 0; i < kN; ++i) h[i] = lds->state[i * 64 + lane];
 }
 
 // Nothing said, nothing drawn.
-__global__ void __launch_bounds__(256) gs_clear(const Scan d) {
-  const int64_t n = int64_t(d.chunks) * d.channels;
+__global__ void __launch_bounds__(256) gs_clear(const Scan d, int64_t n) {
   for (int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x; i < n; i += int64_t(gridDim.x) * 256) d.slots[i] = 0;
-  if (blockIdx.x == 0 && threadIdx.x == 0) *d.ticket = 0;
+  for (int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x; i < d.tiles; i += int64_t(gridDim.x) * 256)
+    d.drawn[i * kLine] = 0;
 }
 
 // Samples without tokens: their states go through. Workgroups behind the last
@@ -306,14 +329,15 @@ __global__ void __launch_bounds__(64 * kWaves, 6) gs_forward(const Scan d, uint3
   constexpr int kN = kChannels<E>;
   __shared__ Marks marks;
   __shared__ Maps<kN> maps;
-  __shared__ uint64_t window[kChain ? kWindow : 1][64 * kN];
+  __shared__ std::conditional_t<kChain, Chain<kN>, int> lds;
   if (row_block() >= blocks) {
     if (d.last) empty_samples(d, row_block() - blocks, d.h0, d.last);
     return;
   }
-  const uint32_t work = draw<kChain>(d), chunk = work / uint32_t(d.tiles);
-  const int wave = threadIdx.x >> 6;
-  const Cols<E> col = make_cols<E>(d, work % uint32_t(d.tiles));
+  const uint32_t tile = row_block() % uint32_t(d.tiles);
+  const int32_t chunk = draw<kChain>(d, tile);
+  const int wave = wave_id();
+  const Cols<E> col = make_cols<E>(d, tile);
   const int64_t t0 = int64_t(chunk) * kTile, t = t0 + wave * kRows;
   const int there = t >= d.T ? 0 : d.T - t < kRows ? int(d.T - t) : kRows;  // rows; `rows` of them in samples
   Pack<E, kN> x[kRows];
@@ -342,7 +366,7 @@ __global__ void __launch_bounds__(64 * kWaves, 6) gs_forward(const Scan d, uint3
       if (first >> r & 1) {
 #pragma unroll
         for (int i = 0; i < kN; ++i) B[i] = 0.0f;
-        if (d.h0) load_state<kN>(d.h0, starts[r] - 1, d, col.c, col.n, B);
+        if (d.h0) load_state<E>(d.h0, uniform(starts[r]) - 1, d, col, B);
       }
 #pragma unroll
       for (int i = 0; i < kN; ++i) {
@@ -354,28 +378,71 @@ __global__ void __launch_bounds__(64 * kWaves, 6) gs_forward(const Scan d, uint3
   }
   __syncthreads();
   float h[kN] = {};
-  if constexpr (kChain) chain<false, kN>(d, int32_t(chunk), col.c, col.n, maps, window, h);
+  if constexpr (kChain) chain<false, kN>(d, chunk, tile, maps, &lds, h);
   for (int w = 0; w < wave; ++w) through_wave<kN>(maps, w, h);
   const float none[kN] = {};
 #pragma unroll
   for (int r = 0; r < kRows; ++r) {
     if (r >= there) continue;
     if (r >= rows) {
-      if (r == 0 && d.carry) store_state<kN>(d.carry, t / kRows, d, col.c, col.n, none);
+      if (r == 0 && d.carry) store_state<E>(d.carry, t / kRows, d, col, none);
       store_row<E>(d.h, d.h_stride, t + r, col, none);
       continue;
     }
     if (first >> r & 1) {
 #pragma unroll
       for (int i = 0; i < kN; ++i) h[i] = 0.0f;
-      if (d.h0) load_state<kN>(d.h0, starts[r] - 1, d, col.c, col.n, h);
+      if (d.h0) load_state<E>(d.h0, uniform(starts[r]) - 1, d, col, h);
     }
-    if (r == 0 && d.carry) store_state<kN>(d.carry, t / kRows, d, col.c, col.n, h);
+    if (r == 0 && d.carry) store_state<E>(d.carry, t / kRows, d, col, h);
 #pragma unroll
     for (int i = 0; i < kN; ++i) h[i] = step(share[r][i], h[i], x[r].get(i));
     store_row<E>(d.h, d.h_stride, t + r, col, h);
-    if ((end >> r & 1) && d.last) store_state<kN>(d.last, ends[r] - 1, d, col.c, col.n, h);
+    if ((end >> r & 1) && d.last) store_state<E>(d.last, uniform(ends[r]) - 1, d, col, h);
   }
+}
+
+// Short samples (the next token of a generation, above all): a wave goes through a
+// sample by itself. Sample n stands for the rows behind the last one.
+template <class E>
+__global__ void __launch_bounds__(256) gs_step(const Scan d) {
+  constexpr int kN = kChannels<E>, kDeep = 4;
+  const int64_t work = int64_t(row_block()) * 4 + wave_id();
+  const int64_t s = work / d.tiles;
+  if (s > d.n) return;
+  const Cols<E> col = make_cols<E>(d, int32_t(work % d.tiles));
+  const int64_t total = tokens_of(d);
+  int64_t a = total, b = d.T;
+  float h[kN] = {};
+  if (s < d.n) {
+    a = uniform(d.start[s]), b = uniform(d.start[s + 1]);
+    a = a < 0 ? 0 : a, b = b < total ? b : total;
+    if (d.h0) load_state<E>(d.h0, s, d, col, h);
+  }
+  for (int64_t t = a; t < b; t += kDeep) {
+    Pack<E, kN> x[kDeep], g[kDeep];
+#pragma unroll
+    for (int r = 0; r < kDeep; ++r) {
+      x[r].zero(), g[r].zero();
+      if (s < d.n && t + r < b) {
+        const typename E::T* px = static_cast<const typename E::T*>(d.x) + (t + r) * d.x_stride + uint32_t(col.c);
+        const typename E::T* pg = static_cast<const typename E::T*>(d.gate) + (t + r) * d.gate_stride + uint32_t(col.c);
+        if (col.n == kN) x[r].load(px), g[r].load(pg);
+        else if (col.n > 0) x[r].load_some(px, col.n), g[r].load_some(pg, col.n);
+      }
+    }
+#pragma unroll
+    for (int r = 0; r < kDeep; ++r) {
+      if (t + r >= b) break;
+      if (d.carry && (t + r) % kRows == 0) store_state<E>(d.carry, (t + r) / kRows, d, col, h);
+      if (s < d.n) {
+#pragma unroll
+        for (int i = 0; i < kN; ++i) h[i] = step(share_of<E>(g[r].get(i)), h[i], x[r].get(i));
+      }
+      store_row<E>(d.h, d.h_stride, t + r, col, h);
+    }
+  }
+  if (s < d.n && d.last) store_state<E>(d.last, s, d, col, h);
 }
 
 template <class E, bool kChain>
@@ -383,21 +450,21 @@ __global__ void __launch_bounds__(64 * kWaves, 4) gs_grad(const Scan d, uint32_t
   constexpr int kN = kChannels<E>;
   __shared__ Marks marks;
   __shared__ Maps<kN> maps;
-  __shared__ uint64_t window[kChain ? kWindow : 1][64 * kN];
+  __shared__ std::conditional_t<kChain, Chain<kN>, int> lds;
   if (row_block() >= blocks) {
     if (d.dh0) empty_samples(d, row_block() - blocks, d.dlast, d.dh0);
     return;
   }
-  const uint32_t work = draw<kChain>(d);
-  const int32_t at = int32_t(work / uint32_t(d.tiles));
-  const int wave = threadIdx.x >> 6;
-  const Cols<E> col = make_cols<E>(d, work % uint32_t(d.tiles));
+  const uint32_t tile = row_block() % uint32_t(d.tiles);
+  const int32_t at = draw<kChain>(d, tile);
+  const int wave = wave_id();
+  const Cols<E> col = make_cols<E>(d, tile);
   const int64_t t0 = int64_t(d.chunks - 1 - at) * kTile, t = t0 + wave * kRows;
   const int there = t >= d.T ? 0 : d.T - t < kRows ? int(d.T - t) : kRows;
   Pack<E, kN> dh[kRows];
   float share[kRows][kN], under[kRows][kN];  // under: h_{t-1} - x_t
   float h[kN] = {};
-  if (there > 0) load_state<kN>(d.carry_in, t / kRows, d, col.c, col.n, h);
+  if (there > 0) load_state<E>(d.carry_in, t / kRows, d, col, h);
   Pack<E, kN> x[kRows];
   {
     Pack<E, kN> g[kRows];
@@ -424,7 +491,7 @@ __global__ void __launch_bounds__(64 * kWaves, 4) gs_grad(const Scan d, uint32_t
       if (end >> r & 1) {
 #pragma unroll
         for (int i = 0; i < kN; ++i) R[i] = 0.0f;
-        if (d.dlast) load_state<kN>(d.dlast, ends[r] - 1, d, col.c, col.n, R);
+        if (d.dlast) load_state<E>(d.dlast, uniform(ends[r]) - 1, d, col, R);
       }
 #pragma unroll
       for (int i = 0; i < kN; ++i) {
@@ -441,7 +508,7 @@ __global__ void __launch_bounds__(64 * kWaves, 4) gs_grad(const Scan d, uint32_t
     if (r > 0 && (first >> r & 1)) {
 #pragma unroll
       for (int i = 0; i < kN; ++i) h[i] = 0.0f;
-      if (d.h0) load_state<kN>(d.h0, starts[r] - 1, d, col.c, col.n, h);
+      if (d.h0) load_state<E>(d.h0, uniform(starts[r]) - 1, d, col, h);
     }
 #pragma unroll
     for (int i = 0; i < kN; ++i) {
@@ -451,7 +518,7 @@ __global__ void __launch_bounds__(64 * kWaves, 4) gs_grad(const Scan d, uint32_t
   }
   __syncthreads();
   float R[kN] = {};
-  if constexpr (kChain) chain<true, kN>(d, at, col.c, col.n, maps, window, R);
+  if constexpr (kChain) chain<true, kN>(d, at, tile, maps, &lds, R);
   for (int w = kWaves - 1; w > wave; --w) through_wave<kN>(maps, w, R);
 #pragma unroll
   for (int r = kRows - 1; r >= 0; --r) {
@@ -461,7 +528,7 @@ __global__ void __launch_bounds__(64 * kWaves, 4) gs_grad(const Scan d, uint32_t
       if (end >> r & 1) {
 #pragma unroll
         for (int i = 0; i < kN; ++i) R[i] = 0.0f;
-        if (d.dlast) load_state<kN>(d.dlast, ends[r] - 1, d, col.c, col.n, R);
+        if (d.dlast) load_state<E>(d.dlast, uniform(ends[r]) - 1, d, col, R);
       }
 #pragma unroll
       for (int i = 0; i < kN; ++i) {
@@ -469,7 +536,7 @@ __global__ void __launch_bounds__(64 * kWaves, 4) gs_grad(const Scan d, uint32_t
         split(share[r][i], G, &R[i], &dx[i]);
         dg[i] = under[r][i] * (a_of(share[r][i]) * dx[i]);
       }
-      if ((first >> r & 1) && d.dh0) store_state<kN>(d.dh0, starts[r] - 1, d, col.c, col.n, R);
+      if ((first >> r & 1) && d.dh0) store_state<E>(d.dh0, uniform(starts[r]) - 1, d, col, R);
     }
     store_row<E>(d.dx, d.dx_stride, t + r, col, dx);
     store_row<E>(d.dgate, d.dgate_stride, t + r, col, dg);
@@ -493,11 +560,12 @@ int check(const nopfs_scan* p, bool gradient) {
 
 // Workgroups: chunks by tiles of channels, and behind them those of the samples
 // without tokens, if a state is asked for.
+int tile_channels(int32_t dtype) { return 64 * (dtype == NOPFS_FP32 ? 1 : 2); }
 struct Grid {
   int64_t blocks, all;
 };
 int make_grid(const nopfs_scan* p, bool states, Scan* d, Grid* g) {
-  const int per = 64 * (p->dtype == NOPFS_FP32 ? 1 : 2);
+  const int per = tile_channels(p->dtype);
   d->T = p->T, d->n = p->n, d->channels = p->channels;
   d->x_stride = p->x_stride, d->gate_stride = p->gate_stride, d->h_stride = p->h_stride;
   d->dh_stride = p->dh_stride, d->dx_stride = p->dx_stride, d->dgate_stride = p->dgate_stride;
@@ -510,14 +578,17 @@ int make_grid(const nopfs_scan* p, bool states, Scan* d, Grid* g) {
 }
 
 // What the chunks say to each other, if there are several, with nothing said yet.
-int make_chain(Scratch* sc, Scan* d, hipStream_t st) {
+int make_chain(Scratch* sc, Scan* d, int per, hipStream_t st) {
   if (d->chunks <= 1) return NOPFS_OK;
   int rc;
-  const size_t n = size_t(d->chunks) * size_t(d->channels);
-  if ((rc = step_alloc(sc, &d->slots, n)) || (rc = step_alloc(sc, &d->ticket, 1))) return rc;
+  const size_t n = size_t(d->chunks) * size_t(d->tiles) * size_t(per);
+  if ((rc = step_alloc(sc, &d->slots, n)) || (rc = step_alloc(sc, &d->drawn, size_t(d->tiles) * kLine))) return rc;
   return launch("gs_clear", gs_clear, dim3(uint32_t(std::min<int64_t>(ceil_div(int64_t(n), 1024), 4096))), dim3(256),
-                0, st, *d);
+                0, st, *d, int64_t(n));
 }
+
+// Up to so many tokens, and two a sample, samples go one by one.
+constexpr int64_t kStepTokens = 1024;
 
 int scan_impl(const nopfs_scan* p, const void* x, const void* gate, const int32_t* start, const float* h0, void* h,
               float* last, float* carry, hipStream_t st) {
@@ -529,8 +600,13 @@ int scan_impl(const nopfs_scan* p, const void* x, const void* gate, const int32_
   d.x = x, d.gate = gate, d.start = start, d.h0 = h0, d.h = h, d.last = last, d.carry = carry;
   Grid g;
   if ((rc = make_grid(p, last != nullptr, &d, &g))) return rc;
+  if (p->T <= kStepTokens && p->T <= 2 * int64_t(p->n))
+    return by_dtype(p->dtype, [&](auto e) {
+      return launch("gs_step", gs_step<decltype(e)>, row_grid(ceil_div((int64_t(p->n) + 1) * d.tiles, 4)), dim3(256), 0,
+                    st, d);
+    });
   Scratch sc(st);
-  if ((rc = make_chain(&sc, &d, st))) return rc;
+  if ((rc = make_chain(&sc, &d, tile_channels(p->dtype), st))) return rc;
   return by_dtype(p->dtype, [&](auto e) {
     typedef decltype(e) E;
     return launch("gs_forward", d.chunks > 1 ? gs_forward<E, true> : gs_forward<E, false>, row_grid(g.all),
@@ -552,7 +628,7 @@ int scan_grad_impl(const nopfs_scan* p, const void* dh, const float* dlast, cons
   Grid g;
   if ((rc = make_grid(p, dh0 != nullptr, &d, &g))) return rc;
   Scratch sc(st);
-  if ((rc = make_chain(&sc, &d, st))) return rc;
+  if ((rc = make_chain(&sc, &d, tile_channels(p->dtype), st))) return rc;
   return by_dtype(p->dtype, [&](auto e) {
     typedef decltype(e) E;
     return launch("gs_grad", d.chunks > 1 ? gs_grad<E, true> : gs_grad<E, false>, row_grid(g.all), dim3(64 * kWaves),

@@ -102,6 +102,16 @@ def test_many_single_tokens(n):
     _check(*_inputs([1] * n, 70, BF, seed=n))
 
 
+@pytest.mark.parametrize("lengths", [[0] * 40 + [70] + [0] * 30, [3, 0, 1, 0, 17, 0, 0, 0, 5, 0, 0, 40, 1] + [0] * 40,
+                                     [2] * 512, [2] * 513, [1] * 1_024, [1] * 1_025, [0] * 9],
+                         ids=["one", "mixed", "512", "513", "1024", "1025", "none"])
+@pytest.mark.parametrize("dt,C,tail", [(BF, 130, 0), (F32, 65, 19)])
+def test_few_tokens_a_sample(lengths, dt, C, tail):
+    """Both sides of the rule that goes through samples one by one."""
+    _check(*_inputs(lengths, C, dt, tail=tail))
+    _check(*_inputs(lengths, 3, dt, tail=tail, state=False))
+
+
 @pytest.mark.parametrize("mean", [-30.0, -8.0, 0.0, 8.0, 17.0, 90.0])
 @pytest.mark.parametrize("dt", [BF, F32], ids=NAMES.get)
 def test_gates(mean, dt):
