@@ -108,7 +108,8 @@ __global__ void __launch_bounds__(256) te_count(const Embed d, const Sort s) {
 }
 
 template <bool kFirst>
-__global__ void __launch_bounds__(256) te_scatter(const Embed d, const Sort s) {
+__device__ inline void scatter_tile(const Embed& d, const Sort& s, int32_t tile) {
+  constexpr int kDeep = 16;  // counts in flight
   __shared__ uint32_t base[1 << kMostBits], cnt[4][1 << kMostBits], tmp[65];
   const int bins = 1 << s.bits, wave = threadIdx.x >> 6;
   uint32_t mine[(1 << kMostBits) / 256];  // of the digit, in the tiles before this one
@@ -117,10 +118,15 @@ __global__ void __launch_bounds__(256) te_scatter(const Embed d, const Sort s) {
     const int b = j * 256 + threadIdx.x;
     if (b >= bins) break;
     uint32_t before = 0, all = 0;
-    for (int32_t t = 0; t < s.tiles; ++t) {
-      const uint32_t c = s.hist[int64_t(t) * bins + b];
-      before += t < int32_t(blockIdx.x) ? c : 0;
-      all += c;
+    for (int32_t t = 0; t < s.tiles; t += kDeep) {
+      uint32_t c[kDeep];
+#pragma unroll
+      for (int i = 0; i < kDeep; ++i) c[i] = t + i < s.tiles ? s.hist[int64_t(t + i) * bins + b] : 0;
+#pragma unroll
+      for (int i = 0; i < kDeep; ++i) {
+        before += t + i < tile ? c[i] : 0;
+        all += c[i];
+      }
     }
     mine[j] = before;
     base[b] = all;
@@ -135,7 +141,7 @@ __global__ void __launch_bounds__(256) te_scatter(const Embed d, const Sort s) {
     if (b < bins) base[b] += mine[j];
   }
   __syncthreads();
-  const int64_t i0 = int64_t(blockIdx.x) * s.per_tile;
+  const int64_t i0 = int64_t(tile) * s.per_tile;
   const int64_t i1 = i0 + s.per_tile < d.T ? i0 + s.per_tile : d.T;
   for (int64_t r = i0; r < i1; r += 256) {
     const int64_t i = r + threadIdx.x;
@@ -165,6 +171,37 @@ __global__ void __launch_bounds__(256) te_scatter(const Embed d, const Sort s) {
     }
     __syncthreads();
   }
+}
+
+template <bool kFirst>
+__global__ void __launch_bounds__(256) te_scatter(const Embed d, const Sort s) {
+  scatter_tile<kFirst>(d, s, int32_t(blockIdx.x));
+}
+
+// Rows that no token names, kZeroRows by a group of 2^lg lanes.
+constexpr int kZeroRows = 8;
+template <class W>
+__device__ inline void zero_rows(const Embed& d, const uint8_t* named, typename W::T* dw, int lg, int64_t block) {
+  const int lanes = 1 << lg;
+  const int64_t v0 = (block * (256 >> lg) + (threadIdx.x >> lg)) * kZeroRows;
+  Pack<W, kVec> o;
+  o.zero();
+  for (int64_t v = v0; v < v0 + kZeroRows && v < d.V; ++v) {
+    if (named[v]) continue;
+    for (int32_t c = int32_t(threadIdx.x & (lanes - 1)) * kVec; c < d.width; c += lanes * kVec) {
+      typename W::T* p = dw + v * d.weight_stride + c;
+      if (d.width - c >= kVec) o.store(p);
+      else o.store_some(p, d.width - c);
+    }
+  }
+}
+// The last pass has few workgroups, so the rows without a token go with it. (`named`
+// is whole since the first pass; with one pass alone they go by themselves.)
+template <class W, bool kSort>
+__global__ void __launch_bounds__(256) te_zero(const Embed d, const Sort s, typename W::T* dw, int lg) {
+  const int64_t tiles = kSort ? s.tiles : 0, block = row_block();
+  if (kSort && block < tiles) scatter_tile<false>(d, s, int32_t(block));
+  else zero_rows<W>(d, s.named, dw, lg, block - tiles);
 }
 
 // ---- sums ------------------------------------------------------------------
@@ -302,24 +339,6 @@ __global__ void __launch_bounds__(256) te_join(const Embed d, const Pieces s, ty
   }
 }
 
-// Rows that no token names, kZeroRows by a group of 2^lg lanes.
-constexpr int kZeroRows = 8;
-template <class W>
-__global__ void __launch_bounds__(256) te_zero(const Embed d, const uint8_t* named, typename W::T* dw, int lg) {
-  const int lanes = 1 << lg;
-  const int64_t v0 = (int64_t(row_block()) * (256 >> lg) + (threadIdx.x >> lg)) * kZeroRows;
-  Pack<W, kVec> o;
-  o.zero();
-  for (int64_t v = v0; v < v0 + kZeroRows && v < d.V; ++v) {
-    if (named[v]) continue;
-    for (int32_t c = int32_t(threadIdx.x & (lanes - 1)) * kVec; c < d.width; c += lanes * kVec) {
-      typename W::T* p = dw + v * d.weight_stride + c;
-      if (d.width - c >= kVec) o.store(p);
-      else o.store_some(p, d.width - c);
-    }
-  }
-}
-
 int check(const nopfs_embed* p) {
   if (!p) return fail(NOPFS_EINVAL, "embed is NULL");
   if (p->T < 0 || p->V < 1 || p->width < 1 || p->n_ids < 0)
@@ -343,6 +362,8 @@ Embed describe(const nopfs_embed* p, const void* ids, const int64_t* slot) {
 // Lanes for a row: one vector each, a workgroup at most.
 int row_lanes(int32_t width) { return std::min(8, log2_ceil(ceil_div(width, kVec))); }
 
+constexpr int64_t kManyRows = 4096;
+
 int embed_impl(const nopfs_embed* p, const void* weight, const void* ids, const int64_t* slot, void* out,
                hipStream_t st) {
   const int rc = check(p);
@@ -353,11 +374,13 @@ int embed_impl(const nopfs_embed* p, const void* weight, const void* ids, const 
   const Embed d = describe(p, ids, slot);
   const int lg = row_lanes(p->width);
   const int64_t blocks = ceil_div(p->T, 256 >> lg);
+  const bool several = blocks >= kManyRows;
   return by_dtype(p->weight_dtype, [&](auto w) {
     return by_dtype(p->dtype, [&](auto e) {
       typedef decltype(w) W;
       typedef decltype(e) E;
-      return launch("te_forward", te_forward<W, E, 1>, row_grid(blocks), dim3(256), 0, st, d,
+      return launch("te_forward", several ? te_forward<W, E, 4> : te_forward<W, E, 1>,
+                    row_grid(several ? ceil_div(blocks, 4) : blocks), dim3(256), 0, st, d,
                     static_cast<const typename W::T*>(weight), static_cast<typename E::T*>(out), lg);
     });
   });
@@ -392,38 +415,38 @@ int embed_grad_impl(const nopfs_embed* p, const void* dout, const void* ids, con
       (rc = step_alloc(&sc, &s.named, size_t(p->V))) || (rc = step_alloc(&sc, &pc.head, parts)) ||
       (rc = step_alloc(&sc, &pc.tail, parts)))
     return rc;
-  int at = 0;
-  for (int pass = 0; pass < passes; ++pass, at ^= 1) {
-    s.key_in = key[at ^ 1], s.val_in = val[at ^ 1], s.key = key[at], s.val = val[at];
-    s.shift = pass * s.bits;
-    const dim3 grid(uint32_t(std::max(1, s.tiles)));  // without tokens the first count clears `named`
-    if (pass > 0 && !s.tiles) break;
-    rc = pass == 0 ? launch("te_count", te_count<true>, grid, dim3(256), 0, st, d, s)
-                   : launch("te_count", te_count<false>, grid, dim3(256), 0, st, d, s);
-    if (rc || !s.tiles) break;
-    rc = pass == 0 ? launch("te_scatter", te_scatter<true>, grid, dim3(256), 0, st, d, s)
-                   : launch("te_scatter", te_scatter<false>, grid, dim3(256), 0, st, d, s);
-    if (rc) break;
-  }
-  if (rc) return rc;
-  at ^= 1;
-  pc.key = key[at], pc.val = val[at];
   const int lg = row_lanes(p->width);
+  const int64_t zeros = ceil_div(p->V, (256 >> lg) * kZeroRows);
   return by_dtype(p->weight_dtype, [&](auto w) {
-    return by_dtype(p->dtype, [&](auto e) {
-      typedef decltype(w) W;
+    typedef decltype(w) W;
+    typename W::T* to = static_cast<typename W::T*>(dw);
+    int r = NOPFS_OK, at = 0;
+    for (int pass = 0; pass < passes && !r; ++pass, at ^= 1) {
+      s.key_in = key[at ^ 1], s.val_in = val[at ^ 1], s.key = key[at], s.val = val[at];
+      s.shift = pass * s.bits;
+      const dim3 grid(uint32_t(std::max(1, s.tiles)));  // without tokens the first count clears `named`
+      const dim3 tiles(uint32_t(s.tiles));
+      if (pass == 0) {
+        r = launch("te_count", te_count<true>, grid, dim3(256), 0, st, d, s);
+        if (!r) r = launch("te_scatter", te_scatter<true>, tiles, dim3(256), 0, st, d, s);
+        if (!r && passes == 1) r = launch("te_zero", te_zero<W, false>, row_grid(zeros), dim3(256), 0, st, d, s, to, lg);
+      } else {
+        if (s.tiles) r = launch("te_count", te_count<false>, tiles, dim3(256), 0, st, d, s);
+        if (!r && pass < passes - 1) r = launch("te_scatter", te_scatter<false>, tiles, dim3(256), 0, st, d, s);
+        else if (!r)
+          r = launch("te_zero", te_zero<W, true>, row_grid(s.tiles + zeros), dim3(256), 0, st, d, s, to, lg);
+      }
+    }
+    if (r) return r;
+    pc.key = key[at ^ 1], pc.val = val[at ^ 1];
+    r = by_dtype(p->dtype, [&](auto e) {
       typedef decltype(e) E;
-      typename W::T* to = static_cast<typename W::T*>(dw);
-      int r = launch("te_zero", te_zero<W>, row_grid(ceil_div(p->V, (256 >> lg) * kZeroRows)), dim3(256), 0, st, d,
-                     s.named, to, lg);
-      if (!r)
-        r = launch("te_pieces", te_pieces<W, E>, row_grid(ceil_div(pc.n, 256 >> lg)), dim3(256), 0, st, d, pc,
-                   static_cast<const typename E::T*>(dout), to, lg);
-      if (!r)
-        r = launch("te_join", te_join<W>, dim3(uint32_t(pc.n), uint32_t(ceil_div(p->width, 256))), dim3(256), 0, st, d,
-                   pc, to);
-      return r;
+      return launch("te_pieces", te_pieces<W, E>, row_grid(ceil_div(pc.n, 256 >> lg)), dim3(256), 0, st, d, pc,
+                    static_cast<const typename E::T*>(dout), to, lg);
     });
+    if (r) return r;
+    return launch("te_join", te_join<W>, dim3(uint32_t(pc.n), uint32_t(ceil_div(p->width, 256))), dim3(256), 0, st, d,
+                  pc, to);
   });
 }
 
