@@ -288,7 +288,10 @@ __global__ void __launch_bounds__(256) te_pieces(const Embed d, const Pieces s, 
   }
 }
 
-constexpr int64_t kMostPieces = 8192;
+// Tokens of a piece: 32, fewer (8 at least) while that leaves the chip idle, more where
+// te_join would go over very many pieces. 5,003 tokens by 250 with 32, 16, 8: 28, 16, 10 us;
+// 65,536 by 1,024: 76, 80, 79, and te_join 14, 26, 47.
+constexpr int64_t kMostPieces = 8192, kPieceThreads = 1 << 17;
 
 // The names of several pieces: a workgroup adds up the parts of the one that begins
 // in its piece, 256 columns, each wave every fourth part.
@@ -402,7 +405,9 @@ int embed_grad_impl(const nopfs_embed* p, const void* dout, const void* ids, con
   s.tiles = int32_t(std::min<int64_t>(128, ceil_div(p->T, kSortTile)));
   s.per_tile = s.tiles ? int32_t(ceil_div(p->T, s.tiles)) : 0;
   Pieces pc{};
+  const int lg = row_lanes(p->width);
   pc.per = 32;
+  while (pc.per > 8 && (ceil_div(p->T, pc.per) << lg) < kPieceThreads) pc.per /= 2;
   while (ceil_div(p->T, pc.per) > kMostPieces) pc.per *= 2;
   pc.n = int32_t(ceil_div(p->T, pc.per));
   Scratch sc(st);
@@ -415,7 +420,6 @@ int embed_grad_impl(const nopfs_embed* p, const void* dout, const void* ids, con
       (rc = step_alloc(&sc, &s.named, size_t(p->V))) || (rc = step_alloc(&sc, &pc.head, parts)) ||
       (rc = step_alloc(&sc, &pc.tail, parts)))
     return rc;
-  const int lg = row_lanes(p->width);
   const int64_t zeros = ceil_div(p->V, (256 >> lg) * kZeroRows);
   return by_dtype(p->weight_dtype, [&](auto w) {
     typedef decltype(w) W;

@@ -201,7 +201,7 @@ template <class E, int kLanes>
 __device__ __forceinline__ void grad_heads(const Rotate& d, const Side& side, int32_t heads, int64_t t, bool there,
                                            int part, int parts, const Lane& l, const float (&w)[kVec],
                                            float (&dw)[kVec]) {
-  constexpr int kSlots = 64 / kLanes, kDeep = 2;
+  constexpr int kSlots = 64 / kLanes, kDeep = 4;
   typedef typename E::T T;
   const int slot = (threadIdx.x & 63) / kLanes;
   const T* x = static_cast<const T*>(side.x) + t * side.x_stride[0] + l.e0;
@@ -291,19 +291,28 @@ __global__ void __launch_bounds__(64 * kWaves) nr_grad(const Rotate d, const Sid
   }
 }
 
-// The workgroups' sums, in order: 16 columns by 16 rows of threads.
-__global__ void __launch_bounds__(256) nr_weights(const float* part_sums, int32_t n, int32_t width, int32_t dtype,
-                                                  void* dq, void* dk) {
-  __shared__ float sums[16][17];
+// The workgroups' sums, in order: 16 columns by 64 rows of threads.
+__global__ void __launch_bounds__(1024) nr_weights(const float* part_sums, int32_t n, int32_t width, int32_t dtype,
+                                                   void* dq, void* dk) {
+  constexpr int kDeep = 16;  // in flight
+  __shared__ float sums[64][17];
   const int c = threadIdx.x & 15, row = threadIdx.x >> 4;
   const int col = blockIdx.x * 16 + c;  // 2 width is a multiple of 16
   float s = 0.0f;
-  for (int32_t i = row; i < n; i += 16) s += part_sums[int64_t(i) * 2 * width + col];
+  for (int32_t i = row; i < n; i += 64 * kDeep) {
+    float x[kDeep];
+#pragma unroll
+    for (int j = 0; j < kDeep; ++j)
+      x[j] = i + 64 * j < n ? part_sums[int64_t(i + 64 * j) * 2 * width + col] : 0.0f;
+#pragma unroll
+    for (int j = 0; j < kDeep; ++j) s += x[j];
+  }
   sums[row][c] = s;
   __syncthreads();
   if (row) return;
   s = 0.0f;
-  for (int i = 0; i < 16; ++i) s += sums[i][c];
+#pragma unroll 16
+  for (int i = 0; i < 64; ++i) s += sums[i][c];
   void* to = col < width ? dq : dk;
   const int e = col < width ? col : col - width;
   if (!to) return;
@@ -414,7 +423,7 @@ int rotate_grad_impl(const nopfs_rotate* p, const void* dqo, const void* dko, co
     });
   });
   if (rc || !weights) return rc;
-  return launch("nr_weights", nr_weights, dim3(uint32_t(2 * p->width / 16)), dim3(256), 0, st, sums, int32_t(parts),
+  return launch("nr_weights", nr_weights, dim3(uint32_t(2 * p->width / 16)), dim3(1024), 0, st, sums, int32_t(parts),
                 p->width, p->weight_dtype, dqw, dkw);
 }
 

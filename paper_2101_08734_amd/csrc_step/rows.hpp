@@ -86,11 +86,27 @@ struct Pack {
   }
 };
 
-// The sum over groups of kLanes lanes (a power of two), the same in all of them.
+// The sum over groups of kLanes lanes (a power of two), the same in all of them, in
+// registers: lanes 1 and 2 apart by permutations of four, then mirrors of 8 and 16
+// lanes (whose parts are equal by then), then rows of 16 and halves exchanged.
+template <int kCtrl>
+__device__ __forceinline__ float dpp(float v) {
+  return __uint_as_float(__builtin_amdgcn_update_dpp(0u, __float_as_uint(v), kCtrl, 0xf, 0xf, true));
+}
 template <int kLanes>
 __device__ __forceinline__ float group_sum(float v) {
-#pragma unroll
-  for (int o = kLanes / 2; o; o >>= 1) v += __shfl_xor(v, o);
+  if constexpr (kLanes >= 2) v += dpp<0xB1>(v);    // quad_perm:[1,0,3,2]
+  if constexpr (kLanes >= 4) v += dpp<0x4E>(v);    // quad_perm:[2,3,0,1]
+  if constexpr (kLanes >= 8) v += dpp<0x141>(v);   // row_half_mirror
+  if constexpr (kLanes >= 16) v += dpp<0x140>(v);  // row_mirror
+  if constexpr (kLanes >= 32) {
+    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+  }
+  if constexpr (kLanes >= 64) {
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+  }
   return v;
 }
 
