@@ -29,9 +29,12 @@ struct Pack {
 #pragma unroll
     for (int i = 0; i < kWords; ++i) w[i] = 0;
   }
+  // kOnce: of data that nothing reads again soon
+  template <bool kOnce = false>
   __device__ __forceinline__ void load(const T* p) {
     if constexpr (kWords == 1) {
-      w[0] = *reinterpret_cast<const word_by2*>(p);
+      if constexpr (kOnce) w[0] = __builtin_nontemporal_load(reinterpret_cast<const word_by2*>(p));
+      else w[0] = *reinterpret_cast<const word_by2*>(p);
     } else if constexpr (kWords == 2) {
       const u32x2 v = *reinterpret_cast<const pair_by2*>(p);
       w[0] = v[0], w[1] = v[1];
@@ -68,9 +71,11 @@ struct Pack {
       }
     }
   }
+  template <bool kOnce = false>
   __device__ __forceinline__ void store(T* p) const {
     if constexpr (kWords == 1) {
-      *reinterpret_cast<word_by2*>(p) = w[0];
+      if constexpr (kOnce) __builtin_nontemporal_store(w[0], reinterpret_cast<word_by2*>(p));
+      else *reinterpret_cast<word_by2*>(p) = w[0];
     } else if constexpr (kWords == 2) {
       *reinterpret_cast<pair_by2*>(p) = u32x2{w[0], w[1]};
     } else {

@@ -71,7 +71,7 @@ __device__ __forceinline__ void load_rows(const void* base, int64_t stride, int6
   for (int r = 0; r < kRows; ++r) v[r].zero();
   if (col.full && rows == kRows) {
 #pragma unroll
-    for (int r = 0; r < kRows; ++r) v[r].load(p + r * stride + uint32_t(col.c));
+    for (int r = 0; r < kRows; ++r) v[r].template load<true>(p + r * stride + uint32_t(col.c));
   } else {
 #pragma unroll
     for (int r = 0; r < kRows; ++r)
@@ -87,7 +87,7 @@ __device__ __forceinline__ void store_row(void* base, int64_t stride, int64_t t,
   typename E::T* p = static_cast<typename E::T*>(base) + t * stride + uint32_t(col.c);
   Pack<E, kChannels<E>> o;
   o.set(v);
-  if (col.full) o.store(p);
+  if (col.full) o.template store<true>(p);
   else if (col.n == Cols<E>::kN) o.store(p);
   else if (col.n > 0) o.store_some(p, col.n);
 }
@@ -163,18 +163,17 @@ __device__ inline int32_t sample_of(const Scan& d, int64_t t) {
   return lo;
 }
 // Of tokens t0 .. t0 + kTile - 1, by all threads; ends with a barrier.
-__device__ inline void make_marks(const Scan& d, int64_t t0, int64_t total, Marks* m) {
+__device__ inline void make_marks(const Scan& d, int64_t t0, Marks* m) {
+  const int64_t t1 = t0 + kTile < d.T ? t0 + kTile : d.T;
+  const int32_t s0 = d.n > 0 ? sample_of(d, t0) : 0;
   for (int i = threadIdx.x; i < kTile; i += 64 * kWaves) m->first[i] = m->end[i] = 0;
   __syncthreads();
-  if (t0 < total) {
-    const int64_t t1 = t0 + kTile < total ? t0 + kTile : total;
-    const int32_t s0 = sample_of(d, t0), s1 = sample_of(d, t1 - 1);
-    for (int64_t s = s0 + int64_t(threadIdx.x); s <= s1; s += 64 * kWaves) {
-      const int64_t a = d.start[s], b = d.start[s + 1];
-      if (a >= b) continue;  // no tokens
-      if (a >= t0 && a < t1) m->first[a - t0] = int32_t(s) + 1;
-      if (b > t0 && b <= t1) m->end[b - 1 - t0] = int32_t(s) + 1;
-    }
+  for (int64_t s = s0 + int64_t(threadIdx.x); s < d.n; s += 64 * kWaves) {
+    const int64_t a = d.start[s], b = d.start[s + 1];
+    if (a >= t1) break;
+    if (a >= b) continue;  // no tokens
+    if (a >= t0) m->first[a - t0] = int32_t(s) + 1;
+    if (b > t0 && b <= t1) m->end[b - 1 - t0] = int32_t(s) + 1;
   }
   __syncthreads();
 }
@@ -353,7 +352,7 @@ __global__ void __launch_bounds__(64 * kWaves, 6) gs_forward(const Scan d, uint3
   }
   const int64_t total = tokens_of(d);
   const int rows = total <= t ? 0 : total - t < kRows ? int(total - t) : kRows;
-  make_marks(d, t0, total, &marks);
+  make_marks(d, t0, &marks);
   const uint32_t first = wave_marks(marks.first), end = wave_marks(marks.end);
   const int32_t *starts = marks.first + wave * kRows, *ends = marks.end + wave * kRows;
   {
@@ -478,7 +477,7 @@ __global__ void __launch_bounds__(64 * kWaves, 4) gs_grad(const Scan d, uint32_t
   }
   const int64_t total = tokens_of(d);
   const int rows = total <= t ? 0 : total - t < kRows ? int(total - t) : kRows;
-  make_marks(d, t0, total, &marks);
+  make_marks(d, t0, &marks);
   const uint32_t first = wave_marks(marks.first), end = wave_marks(marks.end);
   const int32_t *starts = marks.first + wave * kRows, *ends = marks.end + wave * kRows;
   {

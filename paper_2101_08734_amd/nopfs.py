@@ -901,14 +901,23 @@ def _rotate(q, k, pos, freq, q_weight, k_weight, eps, interleaved, dev):
     rotated = 0
     if freq is not None:
         rotated = 2 * _dense(_step_tensor(freq, "freq", _F64, 1, dev), "freq").shape[0]
-    kinds = [w.dtype for w in (q_weight, k_weight) if w is not None]
+    kind = None
     for name, w in (("q_weight", q_weight), ("k_weight", k_weight)):
         if w is not None:
             _step_shape(_step_tensor(w, name, _DTYPES, 1, dev), name, (width,))
-    if kinds and kinds[-1] is not kinds[0]:
-        raise ValueError("q_weight and k_weight must be of one type")
+            if kind is not None and w.dtype is not kind:
+                raise ValueError("q_weight and k_weight must be of one type")
+            kind = w.dtype
     return (T, heads, kv_heads, width, rotated, 1 if interleaved else 0, _DTYPES[q.dtype],
-            _DTYPES[kinds[0]] if kinds else 0, eps)
+            0 if kind is None else _DTYPES[kind], eps)
+
+
+def _heads_like(t, name, like, dev):
+    """An output as the heads of `like`: as given, or a new one."""
+    if t is None:
+        return like.new_empty(like.shape)
+    _step_shape(_step_tensor(t, name, (like.dtype,), 3, dev), name, like.shape)
+    return t
 
 
 def _optional(t):
@@ -943,26 +952,22 @@ def norm_rotate(q, k, pos, freq=None, q_weight=None, k_weight=None, eps=1e-6, in
     width / 2: the elements behind are not rotated). Pairs are (i, i + rotated/2),
     or neighbours if interleaved. q_weight, k_weight [width] of one type, or None.
     Returns q_out, k_out; they may be q and k. Autograd takes them back to q, k and
-    the weights by norm_rotate_grad."""
-    if torch.is_grad_enabled() and any(
-            t is not None and t.requires_grad for t in (q, k, q_weight, k_weight)):
+    the weights by norm_rotate_grad; freq is data."""
+    if freq is not None and freq.requires_grad and torch.is_grad_enabled():
+        raise ValueError("norm_rotate has no gradient by freq (detach it)")
+    if (q.requires_grad or k.requires_grad or q_weight is not None and q_weight.requires_grad
+            or k_weight is not None and k_weight.requires_grad) and torch.is_grad_enabled():
         _no_outputs_given("norm_rotate", q_out, k_out)
         return _NormRotate.apply(q, k, pos, freq, q_weight, k_weight, eps, interleaved, stream)
     dev = torch.cuda.current_device()
     r = _rotate(q, k, pos, freq, q_weight, k_weight, eps, interleaved, dev)
-    outs = []
-    for name, t, like in (("q_out", q_out, q), ("k_out", k_out, k)):
-        if t is None:
-            t = q.new_empty(like.shape)
-        else:
-            _step_shape(_step_tensor(t, name, (q.dtype,), 3, dev), name, like.shape)
-        outs.append(t)
-    r = _Rotate(*r, *_strides(q, k, *outs))
-    st = _step_stream(stream, dev, (q, k, pos, freq, q_weight, k_weight, *outs))
+    q_out, k_out = _heads_like(q_out, "q_out", q, dev), _heads_like(k_out, "k_out", k, dev)
+    r = _Rotate(*r, *_strides(q, k, q_out, k_out))
+    st = _step_stream(stream, dev, (q, k, pos, freq, q_weight, k_weight, q_out, k_out))
     _check(lib().nopfs_norm_rotate(ctypes.byref(r), q.data_ptr(), k.data_ptr(), pos.data_ptr(),
                                    _optional(freq), _optional(q_weight), _optional(k_weight),
-                                   outs[0].data_ptr(), outs[1].data_ptr(), st), "nopfs_norm_rotate")
-    return tuple(outs)
+                                   q_out.data_ptr(), k_out.data_ptr(), st), "nopfs_norm_rotate")
+    return q_out, k_out
 
 
 def norm_rotate_grad(dq_out, dk_out, q, k, pos, freq=None, q_weight=None, k_weight=None, eps=1e-6,
@@ -972,23 +977,18 @@ def norm_rotate_grad(dq_out, dk_out, q, k, pos, freq=None, q_weight=None, k_weig
     the gradients of the weights, None of a weight that is None, or with weights False."""
     dev = torch.cuda.current_device()
     r = _rotate(q, k, pos, freq, q_weight, k_weight, eps, interleaved, dev)
-    grads = []
-    for name, d, t, like in (("q", dq_out, dq, q), ("k", dk_out, dk, k)):
-        _step_shape(_step_tensor(d, f"d{name}_out", (q.dtype,), 3, dev), f"d{name}_out", like.shape)
-        if t is None:
-            t = q.new_empty(like.shape)
-        else:
-            _step_shape(_step_tensor(t, "d" + name, (q.dtype,), 3, dev), "d" + name, like.shape)
-        grads.append(t)
-    grads += [torch.empty_like(w) if weights and w is not None else None for w in (q_weight, k_weight)]
-    r = _Rotate(*r, *_strides(q, k, dq_out, dk_out, grads[0], grads[1]))
-    st = _step_stream(stream, dev, (dq_out, dk_out, q, k, pos, freq, q_weight, k_weight, *grads))
+    for name, d, like in (("dq_out", dq_out, q), ("dk_out", dk_out, k)):
+        _step_shape(_step_tensor(d, name, (q.dtype,), 3, dev), name, like.shape)
+    dq, dk = _heads_like(dq, "dq", q, dev), _heads_like(dk, "dk", k, dev)
+    dqw, dkw = (torch.empty_like(w) if weights and w is not None else None for w in (q_weight, k_weight))
+    r = _Rotate(*r, *_strides(q, k, dq_out, dk_out, dq, dk))
+    st = _step_stream(stream, dev, (dq_out, dk_out, q, k, pos, freq, q_weight, k_weight, dq, dk, dqw, dkw))
     scratch = _capturing() and _step_scratch(r, dev, stream, "nopfs_norm_rotate_scratch")  # noqa: F841
     _check(lib().nopfs_norm_rotate_grad(
         ctypes.byref(r), dq_out.data_ptr(), dk_out.data_ptr(), q.data_ptr(), k.data_ptr(), pos.data_ptr(),
-        _optional(freq), _optional(q_weight), _optional(k_weight), grads[0].data_ptr(),
-        grads[1].data_ptr(), _optional(grads[2]), _optional(grads[3]), st), "nopfs_norm_rotate_grad")
-    return tuple(grads)
+        _optional(freq), _optional(q_weight), _optional(k_weight), dq.data_ptr(), dk.data_ptr(),
+        _optional(dqw), _optional(dkw), st), "nopfs_norm_rotate_grad")
+    return dq, dk, dqw, dkw
 
 
 SCAN_CHUNK = 16  # NOPFS_SCAN_CHUNK
@@ -1046,8 +1046,8 @@ def gated_scan(x, gate, start, h0=None, keep=True, h=None, last=None, stream=Non
     (None if keep is False). Samples of one token with h0 are the step of a
     generation; last may not be h0. Autograd takes h and last back to x, gate and h0
     by gated_scan_grad."""
-    if torch.is_grad_enabled() and (x.requires_grad or gate.requires_grad
-                                    or h0 is not None and h0.requires_grad):
+    if (x.requires_grad or gate.requires_grad
+            or h0 is not None and h0.requires_grad) and torch.is_grad_enabled():
         _no_outputs_given("gated_scan", h, last)
         return _GatedScan.apply(x, gate, start, h0, stream)
     dev = torch.cuda.current_device()

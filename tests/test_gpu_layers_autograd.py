@@ -71,6 +71,8 @@ def test_rotate():
         assert torch.equal(qw.grad, want[2]) and torch.equal(kw.grad, want[3])
     with pytest.raises(ValueError, match="given outputs"):
         nopfs.norm_rotate(x[:, :4], x[:, 4:], pos, freq, q_out=torch.empty_like(outs[0]))
+    with pytest.raises(ValueError, match="gradient by freq"):
+        nopfs.norm_rotate(x[:, :4], x[:, 4:], pos, freq.clone().requires_grad_())
 
 
 def test_rotate_of_one_output_or_input():
