@@ -31,6 +31,13 @@ __device__ __forceinline__ int64_t name_of(const Embed& d, int64_t t) {
 
 constexpr int kVec = 8;  // elements per lane and step
 
+// A lane's elements of a row begin at c, its last ones behind the row: they are then
+// the row's last kVec (made and written by two lanes alike), so that rows of any width
+// are read and written in whole vectors. Of less than kVec, `some`.
+__device__ __forceinline__ int32_t in_row(int32_t c, int32_t width) {
+  return c + kVec <= width ? c : width > kVec ? width - kVec : 0;
+}
+
 // Rows by groups of 2^lg lanes, kPer rows of a group at a time.
 template <class W, class E, int kPer>
 __global__ void __launch_bounds__(256) te_forward(const Embed d, const typename W::T* weight, typename E::T* out,
@@ -41,8 +48,9 @@ __global__ void __launch_bounds__(256) te_forward(const Embed d, const typename 
   int64_t id[kPer];
 #pragma unroll
   for (int j = 0; j < kPer; ++j) id[j] = t0 + j < d.T ? name_of(d, t0 + j) : -1;
-  for (int32_t c = int32_t(threadIdx.x & (lanes - 1)) * kVec; c < d.width; c += lanes * kVec) {
-    const int some = d.width - c;
+  const int some = d.width;
+  for (int32_t c0 = int32_t(threadIdx.x & (lanes - 1)) * kVec; c0 < d.width; c0 += lanes * kVec) {
+    const int32_t c = in_row(c0, d.width);
     Pack<W, kVec> w[kPer];
 #pragma unroll
     for (int j = 0; j < kPer; ++j) {
@@ -178,6 +186,100 @@ __global__ void __launch_bounds__(256) te_scatter(const Embed d, const Sort s) {
   scatter_tile<kFirst>(d, s, int32_t(blockIdx.x));
 }
 
+// All of it by one workgroup, for small batches: 8 bits a pass, a wave's keys one
+// after the other in its own counts, so that the waves meet only between the passes.
+constexpr int kSmallKeys = 6;  // of a thread
+constexpr int64_t kSmallSort = 1024 * kSmallKeys, kSmallNames = 1 << 18;
+
+// A wave's lanes go on together from here, behind what all of them have read and
+// written in LDS.
+__device__ __forceinline__ void wave_step() {
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+}
+
+__global__ void __launch_bounds__(1024) te_sort(const Embed d, const Sort s, int passes) {
+  constexpr int kBins = 256, kWaves = 16;
+  __shared__ uint32_t keys[kSmallSort], vals[kSmallSort], base[kBins], tmp[65];
+  __shared__ uint16_t cnt[kWaves][kBins];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, n = int(d.T);
+  const int rounds = (n + 1023) >> 10, first = wave * rounds * 64 + lane;  // the wave's keys: every 64th from here
+  for (int64_t v = tid; v < (d.V + 15) >> 4; v += 1024) reinterpret_cast<u32x4*>(s.named)[v] = u32x4{0, 0, 0, 0};
+  uint32_t key[kSmallKeys], val[kSmallKeys];
+#pragma unroll
+  for (int r = 0; r < kSmallKeys; ++r) {
+    const int i = first + r * 64;
+    key[r] = val[r] = 0;
+    if (r < rounds && i < n) {
+      const int64_t id = name_of(d, i);
+      key[r] = uint32_t(id >= 0 ? id : d.V);
+      val[r] = uint32_t(i);
+    }
+  }
+  for (int pass = 0; pass < passes; ++pass) {
+    const int shift = pass * 8;
+    for (int i = tid; i < kWaves * kBins / 2; i += 1024) reinterpret_cast<uint32_t*>(cnt)[i] = 0;
+    __syncthreads();
+    uint32_t at[kSmallKeys];
+#pragma unroll
+    for (int r = 0; r < kSmallKeys; ++r) {
+      if (r >= rounds) break;
+      const bool in = first + r * 64 < n;
+      const uint32_t digit = key[r] >> shift & (kBins - 1);
+      uint64_t same = __ballot(in);
+#pragma unroll
+      for (int b = 0; b < 8; ++b) {
+        const uint64_t ones = __ballot(digit >> b & 1);
+        same &= digit >> b & 1 ? ones : ~ones;
+      }
+      const uint32_t rank = __popcll(same & lanemask_lt());
+      at[r] = 0;
+      if (in) at[r] = cnt[wave][digit] + rank;  // read by all of the digit before its first lane adds to it
+      wave_step();
+      if (in && rank == 0) cnt[wave][digit] = uint16_t(cnt[wave][digit] + __popcll(same));
+      wave_step();
+    }
+    __syncthreads();
+    if (tid < kBins) {  // a digit's counts before each wave, and in all
+      uint32_t sum = 0;
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w) {
+        const uint32_t c = cnt[w][tid];
+        cnt[w][tid] = uint16_t(sum);
+        sum += c;
+      }
+      base[tid] = sum;
+    }
+    __syncthreads();
+    block_scan_array(base, kBins, tmp);
+#pragma unroll
+    for (int r = 0; r < kSmallKeys; ++r) {
+      if (r < rounds && first + r * 64 < n) {
+        const uint32_t digit = key[r] >> shift & (kBins - 1);
+        const uint32_t to = base[digit] + cnt[wave][digit] + at[r];
+        keys[to] = key[r];
+        vals[to] = val[r];
+      }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int r = 0; r < kSmallKeys; ++r) {
+      const int i = first + r * 64;
+      if (r < rounds && i < n) key[r] = keys[i], val[r] = vals[i];
+    }
+  }
+#pragma unroll
+  for (int r = 0; r < kSmallKeys; ++r) {
+    const int i = first + r * 64;
+    if (r < rounds && i < n) {
+      s.key[i] = key[r];
+      s.val[i] = val[r];
+      if (key[r] < d.V) s.named[key[r]] = 1;  // cleared before the barriers above
+    }
+  }
+}
+
 // Rows that no token names, kZeroRows by a group of 2^lg lanes.
 constexpr int kZeroRows = 8;
 template <class W>
@@ -189,19 +291,19 @@ __device__ inline void zero_rows(const Embed& d, const uint8_t* named, typename 
   for (int64_t v = v0; v < v0 + kZeroRows && v < d.V; ++v) {
     if (named[v]) continue;
     for (int32_t c = int32_t(threadIdx.x & (lanes - 1)) * kVec; c < d.width; c += lanes * kVec) {
-      typename W::T* p = dw + v * d.weight_stride + c;
-      if (d.width - c >= kVec) o.store(p);
-      else o.store_some(p, d.width - c);
+      typename W::T* p = dw + v * d.weight_stride + in_row(c, d.width);
+      if (d.width >= kVec) o.store(p);
+      else o.store_some(p, d.width);
     }
   }
 }
-// The last pass has few workgroups, so the rows without a token go with it. (`named`
-// is whole since the first pass; with one pass alone they go by themselves.)
-template <class W, bool kSort>
-__global__ void __launch_bounds__(256) te_zero(const Embed d, const Sort s, typename W::T* dw, int lg) {
-  const int64_t tiles = kSort ? s.tiles : 0, block = row_block();
-  if (kSort && block < tiles) scatter_tile<false>(d, s, int32_t(block));
-  else zero_rows<W>(d, s.named, dw, lg, block - tiles);
+// The last of several passes has few workgroups, so the rows without a token go with
+// it (`named` is whole since the first); after a single pass they go with te_pieces.
+template <class W>
+__global__ void __launch_bounds__(256) te_scatter_zero(const Embed d, const Sort s, typename W::T* dw, int lg) {
+  const int64_t block = row_block();
+  if (block < s.tiles) scatter_tile<false>(d, s, int32_t(block));
+  else zero_rows<W>(d, s.named, dw, lg, block - s.tiles);
 }
 
 // ---- sums ------------------------------------------------------------------
@@ -229,16 +331,18 @@ __device__ __forceinline__ void store_row(const Embed& d, typename W::T* dw, uin
 
 template <class W, class E>
 __global__ void __launch_bounds__(256) te_pieces(const Embed d, const Pieces s, const typename E::T* dout,
-                                                 typename W::T* dw, int lg) {
+                                                 typename W::T* dw, int lg, uint32_t blocks, const uint8_t* named) {
   constexpr int kDeep = 8;  // rows in flight
+  if (row_block() >= blocks) return zero_rows<W>(d, named, dw, lg, row_block() - blocks);
   const int lanes = 1 << lg;
   const int64_t piece = int64_t(row_block()) * (256 >> lg) + (threadIdx.x >> lg);
   if (piece >= s.n) return;
   const int64_t i0 = piece * s.per, i1 = i0 + s.per < d.T ? i0 + s.per : d.T;
   const uint32_t none = uint32_t(d.V);
   const uint32_t before = i0 > 0 ? s.key[i0 - 1] : none, behind = i1 < d.T ? s.key[i1] : none;
-  for (int32_t c = int32_t(threadIdx.x & (lanes - 1)) * kVec; c < d.width; c += lanes * kVec) {
-    const int some = d.width - c;
+  const int some = d.width;
+  for (int32_t c0 = int32_t(threadIdx.x & (lanes - 1)) * kVec; c0 < d.width; c0 += lanes * kVec) {
+    const int32_t c = in_row(c0, d.width);
     float sum[kVec] = {};
     uint32_t name = s.key[i0];
     bool from_before = name == before;
@@ -294,18 +398,19 @@ __global__ void __launch_bounds__(256) te_pieces(const Embed d, const Pieces s, 
 constexpr int64_t kMostPieces = 8192, kPieceThreads = 1 << 17;
 
 // The names of several pieces: a workgroup adds up the parts of the one that begins
-// in its piece, 256 columns, each wave every fourth part.
+// in its piece, 4 columns a lane. Its 2^(8 - jg) groups of lanes have every so
+// manieth part, so that narrow rows take as many loads at once as wide ones.
 template <class W>
-__global__ void __launch_bounds__(256) te_join(const Embed d, const Pieces s, typename W::T* dw) {
+__global__ void __launch_bounds__(256) te_join(const Embed d, const Pieces s, typename W::T* dw, int jg) {
   constexpr int kCols = 4, kDeep = 8;
-  __shared__ float sums[4][64][kCols];
+  __shared__ float sums[256][kCols + 1];
   const uint32_t none = uint32_t(d.V);
   const int64_t piece = blockIdx.x, i0 = piece * s.per, i1 = i0 + s.per;
   if (i1 >= d.T) return;
   const uint32_t name = s.key[i1 - 1];
   if (name >= none || s.key[i1] != name) return;
   if (i0 > 0 && s.key[i0 - 1] == name) return;
-  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  const int lane = threadIdx.x & 63, group = threadIdx.x >> jg, groups = 256 >> jg;
   int64_t n = 1;  // parts: this piece's and those of the pieces behind it that begin with the name
   for (;;) {
     const int64_t at = (piece + n + lane) * s.per;
@@ -313,14 +418,14 @@ __global__ void __launch_bounds__(256) te_join(const Embed d, const Pieces s, ty
     n += more;
     if (more < 64) break;
   }
-  const int32_t c = (int32_t(blockIdx.y) * 64 + lane) * kCols;
+  const int32_t c = (int32_t(blockIdx.y << jg) + int32_t(threadIdx.x & ((1 << jg) - 1))) * kCols;
   const int some = d.width - c;
   float sum[kCols] = {};
-  for (int64_t q = wave; q < n; q += 4 * kDeep) {
+  for (int64_t q = group; q < n; q += groups * kDeep) {
     float x[kDeep][kCols];
 #pragma unroll
     for (int j = 0; j < kDeep; ++j) {
-      const int64_t part = q + 4 * j;
+      const int64_t part = q + groups * j;
       const float* p = (part ? s.head : s.tail) + (piece + part) * d.width + c;
 #pragma unroll
       for (int e = 0; e < kCols; ++e) x[j][e] = part < n && e < some ? p[e] : 0.0f;
@@ -331,15 +436,16 @@ __global__ void __launch_bounds__(256) te_join(const Embed d, const Pieces s, ty
       for (int e = 0; e < kCols; ++e) sum[e] += x[j][e];
   }
 #pragma unroll
-  for (int e = 0; e < kCols; ++e) sums[wave][lane][e] = sum[e];
+  for (int e = 0; e < kCols; ++e) sums[threadIdx.x][e] = sum[e];
   __syncthreads();
-  if (wave) return;
+  if (group) return;
+  for (int w = 1; w < groups; ++w) {
 #pragma unroll
-  for (int e = 0; e < kCols; ++e) {
-    float t = sum[e];
-    for (int w = 1; w < 4; ++w) t += sums[w][lane][e];
-    if (e < some) dw[int64_t(name) * d.weight_stride + c + e] = typename W::T(t * d.scale);
+    for (int e = 0; e < kCols; ++e) sum[e] += sums[(w << jg) + threadIdx.x][e];
   }
+#pragma unroll
+  for (int e = 0; e < kCols; ++e)
+    if (e < some) dw[int64_t(name) * d.weight_stride + c + e] = typename W::T(sum[e] * d.scale);
 }
 
 int check(const nopfs_embed* p) {
@@ -424,33 +530,42 @@ int embed_grad_impl(const nopfs_embed* p, const void* dout, const void* ids, con
   return by_dtype(p->weight_dtype, [&](auto w) {
     typedef decltype(w) W;
     typename W::T* to = static_cast<typename W::T*>(dw);
+    const bool small = p->T <= kSmallSort && p->V <= kSmallNames;
+    bool zeroed = false;
     int r = NOPFS_OK, at = 0;
-    for (int pass = 0; pass < passes && !r; ++pass, at ^= 1) {
+    if (small) {
+      s.key = key[0], s.val = val[0];
+      r = launch("te_sort", te_sort, dim3(1), dim3(1024), 0, st, d, s, std::max(1, int(ceil_div(bits, 8))));
+      at = 1;
+    }
+    for (int pass = 0; !small && pass < passes && !r; ++pass, at ^= 1) {
       s.key_in = key[at ^ 1], s.val_in = val[at ^ 1], s.key = key[at], s.val = val[at];
       s.shift = pass * s.bits;
-      const dim3 grid(uint32_t(std::max(1, s.tiles)));  // without tokens the first count clears `named`
       const dim3 tiles(uint32_t(s.tiles));
-      if (pass == 0) {
-        r = launch("te_count", te_count<true>, grid, dim3(256), 0, st, d, s);
-        if (!r) r = launch("te_scatter", te_scatter<true>, tiles, dim3(256), 0, st, d, s);
-        if (!r && passes == 1) r = launch("te_zero", te_zero<W, false>, row_grid(zeros), dim3(256), 0, st, d, s, to, lg);
-      } else {
-        if (s.tiles) r = launch("te_count", te_count<false>, tiles, dim3(256), 0, st, d, s);
-        if (!r && pass < passes - 1) r = launch("te_scatter", te_scatter<false>, tiles, dim3(256), 0, st, d, s);
-        else if (!r)
-          r = launch("te_zero", te_zero<W, true>, row_grid(s.tiles + zeros), dim3(256), 0, st, d, s, to, lg);
-      }
+      // without tokens the first count clears `named` all the same
+      r = pass == 0 ? launch("te_count", te_count<true>, dim3(uint32_t(std::max(1, s.tiles))), dim3(256), 0, st, d, s)
+                    : launch("te_count", te_count<false>, tiles, dim3(256), 0, st, d, s);
+      if (r) break;
+      zeroed = pass > 0 && pass == passes - 1;
+      if (zeroed)
+        r = launch("te_scatter_zero", te_scatter_zero<W>, row_grid(s.tiles + zeros), dim3(256), 0, st, d, s, to, lg);
+      else if (pass == 0)
+        r = launch("te_scatter", te_scatter<true>, tiles, dim3(256), 0, st, d, s);
+      else
+        r = launch("te_scatter", te_scatter<false>, tiles, dim3(256), 0, st, d, s);
     }
     if (r) return r;
     pc.key = key[at ^ 1], pc.val = val[at ^ 1];
+    const int64_t blocks = ceil_div(pc.n, 256 >> lg);
     r = by_dtype(p->dtype, [&](auto e) {
       typedef decltype(e) E;
-      return launch("te_pieces", te_pieces<W, E>, row_grid(ceil_div(pc.n, 256 >> lg)), dim3(256), 0, st, d, pc,
-                    static_cast<const typename E::T*>(dout), to, lg);
+      return launch("te_pieces", te_pieces<W, E>, row_grid(blocks + (zeroed ? 0 : zeros)), dim3(256), 0, st, d, pc,
+                    static_cast<const typename E::T*>(dout), to, lg, uint32_t(blocks), s.named);
     });
     if (r) return r;
-    return launch("te_join", te_join<W>, dim3(uint32_t(pc.n), uint32_t(ceil_div(p->width, 256))), dim3(256), 0, st, d,
-                  pc, to);
+    const int jg = std::min(6, log2_ceil(ceil_div(p->width, 4)));
+    return launch("te_join", te_join<W>, dim3(uint32_t(pc.n), uint32_t(ceil_div(p->width, 4 << jg))), dim3(256), 0, st,
+                  d, pc, to, jg);
   });
 }
 

@@ -47,70 +47,62 @@ constexpr int kChannels = sizeof(typename E::T) == 4 ? 1 : 2;
 __device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
 __device__ __forceinline__ int wave_id() { return uniform(int(threadIdx.x >> 6)); }
 
+// A lane's first channel. Lanes behind the last channels stand for the last ones once
+// more (they read, make and write the same), so that no row masks lanes.
 template <class E>
 struct Cols {
   static constexpr int kN = kChannels<E>;
-  int32_t c;  // the first
-  int n;      // so many of them are there
-  bool full;  // all of the wave's
+  uint32_t c;
+  bool one;  // there is one channel alone, where kN is 2
 };
 template <class E>
-__device__ __forceinline__ Cols<E> make_cols(const Scan& d, int32_t tile) {
-  const int32_t c = (tile * 64 + int32_t(threadIdx.x & 63)) * Cols<E>::kN;
-  const int32_t left = d.channels - c;
-  return {c, left < 0 ? 0 : left < Cols<E>::kN ? int(left) : Cols<E>::kN,
-          int64_t(tile + 1) * 64 * Cols<E>::kN <= d.channels};
+__device__ __forceinline__ Cols<E> make_cols(const Scan& d, uint32_t tile) {
+  const uint32_t c = (tile * 64 + (threadIdx.x & 63)) * Cols<E>::kN;
+  const int32_t most = d.channels - Cols<E>::kN;
+  return {most < 0 ? 0 : c < uint32_t(most) ? c : uint32_t(most), most < 0};
 }
 
+template <class E>
+__device__ __forceinline__ void load_row(const void* base, int64_t stride, int64_t t, const Cols<E>& col,
+                                         Pack<E, kChannels<E>>* v) {
+  const typename E::T* p = static_cast<const typename E::T*>(base) + t * stride + col.c;
+  if (col.one) v->load_some(p, 1);
+  else v->template load<true>(p);
+}
 // A wave's rows, `rows` of them.
 template <class E>
 __device__ __forceinline__ void load_rows(const void* base, int64_t stride, int64_t t, int rows, const Cols<E>& col,
                                           Pack<E, kChannels<E>> (&v)[kRows]) {
-  const typename E::T* p = static_cast<const typename E::T*>(base) + t * stride;
 #pragma unroll
-  for (int r = 0; r < kRows; ++r) v[r].zero();
-  if (col.full && rows == kRows) {
-#pragma unroll
-    for (int r = 0; r < kRows; ++r) v[r].template load<true>(p + r * stride + uint32_t(col.c));
-  } else {
-#pragma unroll
-    for (int r = 0; r < kRows; ++r)
-      if (r < rows) {
-        if (col.n == Cols<E>::kN) v[r].load(p + r * stride + uint32_t(col.c));
-        else if (col.n > 0) v[r].load_some(p + r * stride + uint32_t(col.c), col.n);
-      }
+  for (int r = 0; r < kRows; ++r) {
+    v[r].zero();
+    if (r < rows) load_row<E>(base, stride, t + r, col, &v[r]);
   }
 }
 template <class E>
 __device__ __forceinline__ void store_row(void* base, int64_t stride, int64_t t, const Cols<E>& col,
                                           const float (&v)[kChannels<E>]) {
-  typename E::T* p = static_cast<typename E::T*>(base) + t * stride + uint32_t(col.c);
+  typename E::T* p = static_cast<typename E::T*>(base) + t * stride + col.c;
   Pack<E, kChannels<E>> o;
   o.set(v);
-  if (col.full) o.template store<true>(p);
-  else if (col.n == Cols<E>::kN) o.store(p);
-  else if (col.n > 0) o.store_some(p, col.n);
+  if (col.one) o.store_some(p, 1);
+  else o.template store<true>(p);
 }
 // A row of the 32-bit arrays, of samples or chunks.
 template <class E>
 __device__ __forceinline__ void load_state(const float* base, int64_t row, const Scan& d, const Cols<E>& col,
                                            float (&v)[kChannels<E>]) {
-  const float* p = base + row * d.channels + uint32_t(col.c);
+  const float* p = base + row * d.channels + col.c;
 #pragma unroll
-  for (int i = 0; i < Cols<E>::kN; ++i) v[i] = col.full || i < col.n ? p[i] : 0.0f;
+  for (int i = 0; i < Cols<E>::kN; ++i) v[i] = i == 0 || !col.one ? p[i] : 0.0f;
 }
 template <class E>
 __device__ __forceinline__ void store_state(float* base, int64_t row, const Scan& d, const Cols<E>& col,
                                             const float (&v)[kChannels<E>]) {
-  float* p = base + row * d.channels + uint32_t(col.c);
-  if (col.full) {
+  float* p = base + row * d.channels + col.c;
 #pragma unroll
-    for (int i = 0; i < Cols<E>::kN; ++i) p[i] = v[i];
-  } else {
-#pragma unroll
-    for (int i = 0; i < Cols<E>::kN; ++i)
-      if (i < col.n) p[i] = v[i];
-  }
+  for (int i = 0; i < Cols<E>::kN; ++i)
+    if (i == 0 || !col.one) p[i] = v[i];
 }
 
 // The smaller of a and k = 1 - a, with the gate's sign (negative: it is a). Of
@@ -409,7 +401,7 @@ __global__ void __launch_bounds__(256) gs_step(const Scan d) {
   const int64_t work = int64_t(row_block()) * 4 + wave_id();
   const int64_t s = work / d.tiles;
   if (s > d.n) return;
-  const Cols<E> col = make_cols<E>(d, int32_t(work % d.tiles));
+  const Cols<E> col = make_cols<E>(d, uint32_t(work % d.tiles));
   const int64_t total = tokens_of(d);
   int64_t a = total, b = d.T;
   float h[kN] = {};
@@ -424,10 +416,8 @@ __global__ void __launch_bounds__(256) gs_step(const Scan d) {
     for (int r = 0; r < kDeep; ++r) {
       x[r].zero(), g[r].zero();
       if (s < d.n && t + r < b) {
-        const typename E::T* px = static_cast<const typename E::T*>(d.x) + (t + r) * d.x_stride + uint32_t(col.c);
-        const typename E::T* pg = static_cast<const typename E::T*>(d.gate) + (t + r) * d.gate_stride + uint32_t(col.c);
-        if (col.n == kN) x[r].load(px), g[r].load(pg);
-        else if (col.n > 0) x[r].load_some(px, col.n), g[r].load_some(pg, col.n);
+        load_row<E>(d.x, d.x_stride, t + r, col, &x[r]);
+        load_row<E>(d.gate, d.gate_stride, t + r, col, &g[r]);
       }
     }
 #pragma unroll

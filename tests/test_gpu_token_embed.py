@@ -204,3 +204,21 @@ def test_refusals():
     for scale in (math.inf, math.nan):
         with pytest.raises(nopfs.NopfsError):
             nopfs.token_embed(w, ids, scale)
+
+
+@pytest.mark.parametrize("T", [6_143, 6_144, 6_145])
+@pytest.mark.parametrize("V", [200, 70_000, 262_144, 262_145])
+def test_both_sides_of_the_small_sort(T, V):
+    _check(T, V, 5, F32, F32, seed=T + V)
+
+
+@pytest.mark.parametrize("V", [300, 40_000])
+def test_tokens_of_a_name_in_order(V):
+    """Sums are made in the order of the batch: of terms that differ by 2^30, the small
+    ones count only behind the large one's opposite."""
+    for T in (30, 5_000, 20_000):
+        ids = torch.full((T,), V // 2, dtype=torch.int32, device="cuda")
+        d = torch.zeros((T, 8), device="cuda")
+        d[0], d[1], d[2], d[3] = 2.0**30, 1.0, -(2.0**30), 1.0
+        dw = nopfs.token_embed_grad(d, ids, V)
+        assert bool((dw[V // 2] == 1.0).all())
