@@ -5,12 +5,16 @@ token sequences of unequal length, held in blocks of a resident token buffer;
 with each token the sample stores a teacher's top logits. One step of worker 0:
 
   batch_tables        where the tokens of the next batch lie, for all workers
+  token_embed         their rows of the embedding
   packed_attention    one causal attention layer over the packed samples
   topk_distill        loss and gradient against the teacher's top logits
 
-and the gradients go back through packed_attention_grad to the weights.
+and the gradients go back through packed_attention_grad and token_embed_grad to the
+weights. With --mixer rotary the layer's queries and keys are normed and rotated by
+position first (norm_rotate); with --mixer recurrent a gated recurrence (gated_scan)
+stands in attention's place.
 
-Usage: python examples/token_step.py [--steps 40]
+Usage: python examples/token_step.py [--steps 40] [--mixer attention|rotary|recurrent]
 """
 from __future__ import annotations
 
@@ -62,8 +66,9 @@ def _heads(qkv):
 
 
 class Model(torch.nn.Module):
-    def __init__(self):
+    def __init__(self, mixer="attention"):
         super().__init__()
+        self.mixer = mixer
         g = torch.Generator().manual_seed(0)
         dim = HEADS * WIDTH
 
@@ -71,13 +76,27 @@ class Model(torch.nn.Module):
             return torch.nn.Parameter(torch.randn(shape, generator=g) * shape[0] ** -0.5)
 
         self.embed = torch.nn.Parameter(torch.randn((VOCAB, dim), generator=g) * 0.5)
-        self.qkv = weight(dim, (HEADS + 2 * KV_HEADS) * WIDTH)
+        # the recurrence: what it takes in, and the gates of its channels
+        self.qkv = weight(dim, 2 * dim if mixer == "recurrent" else (HEADS + 2 * KV_HEADS) * WIDTH)
         self.out, self.head = weight(dim, dim), weight(dim, VOCAB)
+        if mixer == "rotary":
+            self.q_norm, self.k_norm = (torch.nn.Parameter(torch.ones(WIDTH)) for _ in range(2))
+            freq = 1_000.0 ** (-torch.arange(0, WIDTH, 2, dtype=torch.float64) / WIDTH)
+            self.register_buffer("freq", freq)
 
-    def forward(self, tokens, start):
-        x = self.embed[tokens].bfloat16()
-        qkv = (x @ self.qkv.bfloat16()).view(-1, HEADS + 2 * KV_HEADS, WIDTH)
-        o = Attention.apply(qkv, start)
+    def forward(self, tokens, start, pos=None, slot=None):
+        """tokens [T], or with slot the token buffer that the samples lie in."""
+        x = nopfs.token_embed(self.embed, tokens, slot=slot, dtype=torch.bfloat16)
+        qkv = x @ self.qkv.bfloat16()
+        if self.mixer == "recurrent":
+            dim = x.shape[1]
+            o = nopfs.gated_scan(qkv[:, :dim], qkv[:, dim:], start)[0]
+        elif self.mixer == "rotary":
+            q, k, v = _heads(qkv.view(-1, HEADS + 2 * KV_HEADS, WIDTH))
+            q, k = nopfs.norm_rotate(q, k, pos, self.freq, self.q_norm, self.k_norm)
+            o = nopfs.packed_attention(q, k, v, start)[0]
+        else:
+            o = Attention.apply(qkv.view(-1, HEADS + 2 * KV_HEADS, WIDTH), start)
         return (x + o.reshape(x.shape) @ self.out.bfloat16()) @ self.head.bfloat16()
 
 
@@ -95,7 +114,7 @@ def teacher_entries(tokens, previous):
     return index.int(), logits.half().contiguous()
 
 
-def main(steps=40):
+def main(steps=40, mixer="attention"):
     job = nopfs.Job(F=2_000, E=4, N=4, B=16, drop_last=1, seed=42)
     R = nopfs.access_streams(job)
     gen = torch.Generator(device="cuda").manual_seed(1)
@@ -103,7 +122,7 @@ def main(steps=40):
     blocks = CAP // BLOCK + job.B
     buffer = torch.zeros(job.N * blocks * BLOCK, dtype=torch.int64, device="cuda")
     free = torch.arange(job.N * blocks, dtype=torch.int32, device="cuda").view(job.N, blocks)
-    model = Model().cuda()
+    model = Model(mixer).cuda()
     optimizer = torch.optim.Adam(model.parameters(), lr=1e-2)
     losses, tables = [], None
     for step in range(steps):
@@ -118,7 +137,7 @@ def main(steps=40):
         tokens = torch.where(there, buffer[slot.clamp(min=0)], 0)
         index, teacher = teacher_entries(tokens, torch.where(pos > 0, tokens.roll(1), 0))
         weight = there.float() / there.sum()
-        loss = Distill.apply(model(tokens, start), index, teacher, 1.0, weight)
+        loss = Distill.apply(model(buffer, start, pos, slot), index, teacher, 1.0, weight)
         optimizer.zero_grad()
         loss.backward()
         optimizer.step()
@@ -133,4 +152,6 @@ def main(steps=40):
 if __name__ == "__main__":
     ap = argparse.ArgumentParser(description=__doc__.split("\n")[0])
     ap.add_argument("--steps", type=int, default=40)
-    main(ap.parse_args().steps)
+    ap.add_argument("--mixer", choices=("attention", "rotary", "recurrent"), default="attention")
+    args = ap.parse_args()
+    main(args.steps, args.mixer)
