@@ -91,6 +91,11 @@ struct Sort {
   int32_t tiles, per_tile, shift, bits;
 };
 
+// `named`, 16 rows at a time (its memory ends at a multiple of 256 bytes).
+__device__ __forceinline__ void clear_names(const Embed& d, const Sort& s, int64_t first, int64_t step) {
+  for (int64_t v = first; v < (d.V + 15) >> 4; v += step) reinterpret_cast<u32x4*>(s.named)[v] = u32x4{0, 0, 0, 0};
+}
+
 template <bool kFirst>
 __device__ __forceinline__ uint32_t sort_key(const Embed& d, const Sort& s, int64_t i) {
   if (!kFirst) return s.key_in[i];
@@ -104,7 +109,7 @@ __global__ void __launch_bounds__(256) te_count(const Embed d, const Sort s) {
   const int bins = 1 << s.bits;
   for (int b = threadIdx.x; b < bins; b += 256) count[b] = 0;
   if (kFirst) {
-    for (int64_t v = int64_t(blockIdx.x) * 256 + threadIdx.x; v < d.V; v += int64_t(gridDim.x) * 256) s.named[v] = 0;
+    clear_names(d, s, int64_t(blockIdx.x) * 256 + threadIdx.x, int64_t(gridDim.x) * 256);
   }
   __syncthreads();
   const int64_t i0 = int64_t(blockIdx.x) * s.per_tile;
@@ -168,8 +173,10 @@ __device__ inline void scatter_tile(const Embed& d, const Sort& s, int32_t tile)
     if (in) {
       uint32_t at = base[digit] + rank;
       for (int w = 0; w < wave; ++w) at += cnt[w][digit];
-      s.key[at] = key;
-      s.val[at] = kFirst ? uint32_t(i) : s.val_in[i];
+      if (at < d.T) {  // ids that change under the call leave the counts behind, not the arrays
+        s.key[at] = key;
+        s.val[at] = kFirst ? uint32_t(i) : s.val_in[i];
+      }
       if (kFirst && key < d.V) s.named[key] = 1;
     }
     __syncthreads();
@@ -205,7 +212,7 @@ __global__ void __launch_bounds__(1024) te_sort(const Embed d, const Sort s, int
   __shared__ uint16_t cnt[kWaves][kBins];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, n = int(d.T);
   const int rounds = (n + 1023) >> 10, first = wave * rounds * 64 + lane;  // the wave's keys: every 64th from here
-  for (int64_t v = tid; v < (d.V + 15) >> 4; v += 1024) reinterpret_cast<u32x4*>(s.named)[v] = u32x4{0, 0, 0, 0};
+  clear_names(d, s, tid, 1024);
   uint32_t key[kSmallKeys], val[kSmallKeys];
 #pragma unroll
   for (int r = 0; r < kSmallKeys; ++r) {
@@ -471,7 +478,9 @@ Embed describe(const nopfs_embed* p, const void* ids, const int64_t* slot) {
 // Lanes for a row: one vector each, a workgroup at most.
 int row_lanes(int32_t width) { return std::min(8, log2_ceil(ceil_div(width, kVec))); }
 
-constexpr int64_t kManyRows = 4096;
+// A group has four rows at a time where a row is one step of it, for the loads in flight
+// (16,384 rows of 2,048 in bf16 30 -> 26 us), else one (8,192 of 8,192: 42, with four 45).
+constexpr int32_t kOneStep = 256 * kVec;
 
 int embed_impl(const nopfs_embed* p, const void* weight, const void* ids, const int64_t* slot, void* out,
                hipStream_t st) {
@@ -483,7 +492,7 @@ int embed_impl(const nopfs_embed* p, const void* weight, const void* ids, const 
   const Embed d = describe(p, ids, slot);
   const int lg = row_lanes(p->width);
   const int64_t blocks = ceil_div(p->T, 256 >> lg);
-  const bool several = blocks >= kManyRows;
+  const bool several = p->width <= kOneStep;
   return by_dtype(p->weight_dtype, [&](auto w) {
     return by_dtype(p->dtype, [&](auto e) {
       typedef decltype(w) W;

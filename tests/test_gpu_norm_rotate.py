@@ -122,6 +122,12 @@ def test_nan_stays_in_its_head():
         same = torch.ones(a.shape[:2], dtype=torch.bool)
         same[t, h] = False
         assert torch.equal(a[same], b[same]) and bool(torch.isnan(a[t, h]).any())
+    # 1 / sqrt(inf) is 0: without a rotation the finite elements of such a head are 0
+    for dt in (BF, FP, F32):
+        x = torch.ones((1, 1, 32), dtype=dt, device="cuda")
+        x[0, 0, 3] = -math.inf
+        y = nopfs.norm_rotate(x, x, pos[:1])[0][0, 0]
+        assert bool(torch.isnan(y[3])) and int((y == 0).sum()) == 31
 
 
 @pytest.mark.parametrize("dt,big", [(BF, 1e30), (F32, 1e30), (F32, 2e19), (BF, 3e38), (F32, 3e38)])
