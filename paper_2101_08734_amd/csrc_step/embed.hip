@@ -478,9 +478,11 @@ Embed describe(const nopfs_embed* p, const void* ids, const int64_t* slot) {
 // Lanes for a row: one vector each, a workgroup at most.
 int row_lanes(int32_t width) { return std::min(8, log2_ceil(ceil_div(width, kVec))); }
 
-// A group has four rows at a time where a row is one step of it, for the loads in flight
-// (16,384 rows of 2,048 in bf16 30 -> 26 us), else one (8,192 of 8,192: 42, with four 45).
+// A group has four rows at a time where a row is one step of it and there are enough
+// of them, for the loads in flight (16,384 rows of 2,048 in bf16 30 -> 26 us), else one
+// (8,192 of 8,192: 42, with four 45; 32 of 2,048: 2.5 and 3.6).
 constexpr int32_t kOneStep = 256 * kVec;
+constexpr int64_t kManyRows = 1024;  // workgroups with a row per group
 
 int embed_impl(const nopfs_embed* p, const void* weight, const void* ids, const int64_t* slot, void* out,
                hipStream_t st) {
@@ -492,7 +494,7 @@ int embed_impl(const nopfs_embed* p, const void* weight, const void* ids, const 
   const Embed d = describe(p, ids, slot);
   const int lg = row_lanes(p->width);
   const int64_t blocks = ceil_div(p->T, 256 >> lg);
-  const bool several = p->width <= kOneStep;
+  const bool several = p->width <= kOneStep && blocks >= kManyRows;
   return by_dtype(p->weight_dtype, [&](auto w) {
     return by_dtype(p->dtype, [&](auto e) {
       typedef decltype(w) W;
