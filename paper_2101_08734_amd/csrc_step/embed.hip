@@ -1,9 +1,12 @@
 // nopfs_token_embed and its gradient: the rows of an embedding that the packed
 // tokens name, and the sums of their gradients by name.
 //     out_t = scale W[id_t],   dW_v = scale sum_{t: id_t = v} dout_t
-// Both are bound by memory. The gradient's sums must not depend on the order in
-// which work finishes, so the tokens are sorted by id first (radix sort, stable:
-// a token's rows are added in the order of the batch).
+// Both are bound by memory (16,384 tokens by 2,048 from 32,768 rows, a twelfth of them
+// the most frequent one, bf16: forward 26 us for 108 MB; the gradient's zeros and sums
+// 41 us for 205). The gradient's sums must not depend on the order in which work
+// finishes, so the tokens are sorted by id first (radix sort, stable: a name's rows
+// are added in the order of the batch; 16 us of four dependent launches there).
+// Sums are in 32 bits, rounded once.
 #include "rows.hpp"
 
 namespace nopfs {
@@ -195,6 +198,8 @@ __global__ void __launch_bounds__(256) te_scatter(const Embed d, const Sort s) {
 
 // All of it by one workgroup, for small batches: 8 bits a pass, a wave's keys one
 // after the other in its own counts, so that the waves meet only between the passes.
+// Bound by latency: 5,173 keys of 15 bits 17 us; forward and gradient of that batch
+// (250 elements a row) took 33 us with it and 40 by the passes above.
 constexpr int kSmallKeys = 6;  // of a thread
 constexpr int64_t kSmallSort = 1024 * kSmallKeys, kSmallNames = 1 << 18;
 
@@ -315,7 +320,8 @@ __global__ void __launch_bounds__(256) te_scatter_zero(const Embed d, const Sort
 
 // ---- sums ------------------------------------------------------------------
 // The sorted tokens are cut into pieces of equal size, however many of them share
-// a name, by groups of 2^lg lanes. A name whose tokens lie in one piece has its row
+// a name (a row of the embedding each: 1,114 us where this takes 100), by groups of
+// 2^lg lanes. A name whose tokens lie in one piece has its row
 // written from there; the others leave the sum of each piece's part, and te_join
 // adds those up in order.
 struct Pieces {

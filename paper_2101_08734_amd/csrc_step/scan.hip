@@ -8,7 +8,10 @@
 // if a sample begins in it. A wave holds 16 tokens of its channels in registers, makes
 // their map, gets the state before them through the maps of the stretches before, and
 // goes through its tokens again from there. Everything is read once and written once.
-// Bound by memory.
+// 16,384 tokens by 2,048 channels in bf16: forward 62 us for 215 MB, the gradient 94 for
+// 358; a workgroup loads, makes maps, waits and stores in turn, and registers allow three
+// (the gradient: two) of them on a compute unit. Workgroups of 64 or 256 tokens took 78
+// and 77 us, the gradient 114 and 132.
 //
 // The states and maps are in 32 bits. A step is taken from the larger share,
 // h + k (x - h) or x + a (h - x), so that its rounding is half a unit of the
@@ -181,6 +184,9 @@ __device__ __forceinline__ uint32_t wave_marks(const int32_t* m) {
 // chunks says, when it knows the state before it, the state behind it instead. A
 // chunk applies the maps of its group before it to the state behind the group
 // before. So the chain is one wait per group, and the order of all roundings is fixed.
+// (Groups of 8, 16, 32 chunks: 70, 70, 70 us forward, one sample of 65,536 tokens by
+// 1,024 channels 144, 130, 135. Reading the slots is uncached: where every chunk read
+// those of the 16 before it, 81 and 167.)
 //
 // A slot is one 64-bit word, written and read whole, so it needs no order with
 // others: the upper half is A with its sign bit set (A is in 0 .. 1, or NaN), or
