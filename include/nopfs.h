@@ -627,7 +627,7 @@ int nopfs_gated_scan(const nopfs_scan* s, const void* x, const void* gate, const
  * a_(t+1) G_(t+1) within a sample, d_last[s] in place of the product at its end:
  *   d_x_t = (1 - a_t) G_t,  d_gate_t = a_t (1 - a_t) (h_(t-1) - x_t) G_t,
  *   d_h0[s] = a G of its first token (d_last[s] without tokens).
- *   d_h0: float [n][channels], or NULL.
+ *   d_h0: float [n][channels], or NULL; not d_last itself.
  * Rows from start[n] on get 0. Errors: EINVAL, ERANGE, ENOMEM, EDEVICE. */
 int nopfs_gated_scan_grad(const nopfs_scan* s, const void* d_h, const float* d_last,
                           const void* x, const void* gate, const int32_t* start, const float* h0,

@@ -110,10 +110,11 @@ template <bool kFirst>
 __global__ void __launch_bounds__(256) te_count(const Embed d, const Sort s) {
   __shared__ uint32_t count[1 << kMostBits];
   const int bins = 1 << s.bits;
-  for (int b = threadIdx.x; b < bins; b += 256) count[b] = 0;
   if (kFirst) {
     clear_names(d, s, int64_t(blockIdx.x) * 256 + threadIdx.x, int64_t(gridDim.x) * 256);
+    if (int64_t(blockIdx.x) >= s.tiles) return;  // is here for that alone
   }
+  for (int b = threadIdx.x; b < bins; b += 256) count[b] = 0;
   __syncthreads();
   const int64_t i0 = int64_t(blockIdx.x) * s.per_tile;
   const int64_t i1 = i0 + s.per_tile < d.T ? i0 + s.per_tile : d.T;
@@ -549,6 +550,7 @@ int embed_grad_impl(const nopfs_embed* p, const void* dout, const void* ids, con
     typename W::T* to = static_cast<typename W::T*>(dw);
     const bool small = p->T <= kSmallSort && p->V <= kSmallNames;
     bool zeroed = false;
+    const int32_t clears = int32_t(std::min<int64_t>(256, ceil_div(p->V, 16 * 256 * 4)));
     int r = NOPFS_OK, at = 0;
     if (small) {
       s.key = key[0], s.val = val[0];
@@ -559,8 +561,8 @@ int embed_grad_impl(const nopfs_embed* p, const void* dout, const void* ids, con
       s.key_in = key[at ^ 1], s.val_in = val[at ^ 1], s.key = key[at], s.val = val[at];
       s.shift = pass * s.bits;
       const dim3 tiles(uint32_t(s.tiles));
-      // without tokens the first count clears `named` all the same
-      r = pass == 0 ? launch("te_count", te_count<true>, dim3(uint32_t(std::max(1, s.tiles))), dim3(256), 0, st, d, s)
+      // the first count clears `named` as well, with workgroups of its own for many rows
+      r = pass == 0 ? launch("te_count", te_count<true>, dim3(uint32_t(std::max(s.tiles, clears))), dim3(256), 0, st, d, s)
                     : launch("te_count", te_count<false>, tiles, dim3(256), 0, st, d, s);
       if (r) break;
       zeroed = pass > 0 && pass == passes - 1;

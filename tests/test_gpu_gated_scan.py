@@ -226,3 +226,41 @@ def test_refusals():
                 lambda: nopfs.gated_scan(x[:1].expand(5, 8), gate, start)):
         with pytest.raises(nopfs.NopfsError):
             bad()
+
+
+def test_far_offsets():
+    """Rows whose elements pass 2^31 and their bytes 2^32."""
+    T, stride = 40_000, 2**17
+    x0, gate0, start, h0, dh0_, dlast = _inputs([T - 900, 0, 700], 40, BF, tail=200)
+    want = nopfs.gated_scan(x0, gate0, start, h0)
+    want_g = nopfs.gated_scan_grad(dh0_, x0, gate0, start, want[2], h0, dlast)
+    wide = torch.empty(T * stride, dtype=BF, device="cuda")
+    x, gate, dh, h, dx, dgate = (torch.as_strided(wide, (T, 40), (stride, 1), 64 * i) for i in range(6))
+    for view, t in ((x, x0), (gate, gate0), (dh, dh0_)):
+        view.copy_(t)
+    got = nopfs.gated_scan(x, gate, start, h0, h=h)
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    got = nopfs.gated_scan_grad(dh, x, gate, start, got[2], h0, dlast, dx=dx, dgate=dgate)
+    assert all(torch.equal(a, b) for a, b in zip(got, want_g))
+
+
+def test_more_workgroups_than_one_launch_dimension_holds():
+    """2^20 chunks of 128 tokens and a few of one sample, with a = 1/2: a token is the
+    sum of the 40 before it, weighted by halves (2^-40 of the others is left out)."""
+    T = 2**27 + 300
+    x = torch.randint(-8, 9, (T, 1), device="cuda").to(BF)
+    gate = torch.zeros((T, 1), dtype=BF, device="cuda")
+    start = torch.tensor([0, T], dtype=torch.int32, device="cuda")
+    h, last, _ = nopfs.gated_scan(x, gate, start, keep=False)
+    for a in (0, 2**20 - 64, 2**26, 2**27 - 128, T - 2**20):
+        b, lead = min(T, a + 2**20), min(a, 40)
+        part = x[a - lead:b, 0].double()
+        want = torch.zeros(b - a, dtype=torch.float64, device="cuda")
+        for k in range(41):
+            if k <= lead:
+                want += part[lead - k:len(part) - k] * 0.5 ** (k + 1)
+            else:
+                want[k - lead:] += part[:len(part) - k] * 0.5 ** (k + 1)
+        # the state is off by 16 E of magnitudes up to 8 + 4, twice for what decays, and rounded
+        got = h[a:b, 0].double()
+        assert bool(((got - want).abs() <= 2.0**-8 * want.abs() + 32 * 12 * 2.0**-24 + 8 * 2.0**-40).all()), a

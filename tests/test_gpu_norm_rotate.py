@@ -244,3 +244,31 @@ def test_refusals():
                 lambda: nopfs.norm_rotate(q[:, :1].expand(6, 2, 16), k, pos, freq)):
         with pytest.raises(nopfs.NopfsError):
             bad()
+
+
+def test_far_offsets():
+    """Tokens whose elements pass 2^31 and their bytes 2^32."""
+    T, stride = 40_000, 2**17
+    q0, k0, pos, freq, qw, kw, dq0, dk0 = _inputs(T, 2, 2, 16)
+    wide = torch.empty(T * stride, dtype=BF, device="cuda")
+    views = [torch.as_strided(wide, (T, 2, 16), (stride, 16, 1), 32 * i) for i in range(8)]
+    for view, x in zip(views, (q0, k0, dq0, dk0)):
+        view.copy_(x)
+    q, k, dq, dk, *outs = views
+    want = nopfs.norm_rotate(q0, k0, pos, freq, qw, kw)
+    nopfs.norm_rotate(q, k, pos, freq, qw, kw, q_out=outs[0], k_out=outs[1])
+    assert torch.equal(outs[0], want[0]) and torch.equal(outs[1], want[1])
+    want = nopfs.norm_rotate_grad(dq0, dk0, q0, k0, pos, freq, qw, kw)
+    got = nopfs.norm_rotate_grad(dq, dk, q, k, pos, freq, qw, kw, dq=outs[2], dk=outs[3])
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+def test_more_workgroups_than_one_launch_dimension_holds():
+    T = 4 * 2**20 + 77  # four tokens a workgroup
+    x = torch.randn((T, 2, 8), device="cuda").to(BF)
+    pos = (torch.arange(T, device="cuda") % 1_000 - 1).int()
+    q, k = nopfs.norm_rotate(x[:, :1], x[:, 1:], pos, _freq(8))
+    half = T // 2 // 4 * 4
+    for a, b in ((0, half), (half, T)):
+        want = nopfs.norm_rotate(x[a:b, :1], x[a:b, 1:], pos[a:b], _freq(8))
+        assert torch.equal(q[a:b], want[0]) and torch.equal(k[a:b], want[1])

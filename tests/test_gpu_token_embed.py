@@ -222,3 +222,28 @@ def test_tokens_of_a_name_in_order(V):
         d[0], d[1], d[2], d[3] = 2.0**30, 1.0, -(2.0**30), 1.0
         dw = nopfs.token_embed_grad(d, ids, V)
         assert bool((dw[V // 2] == 1.0).all())
+
+
+@pytest.mark.parametrize("T,V", [(0, 300_000), (3, 2_000_003), (7_000, 1_500_001), (130_000, 900_001)])
+def test_many_more_rows_than_tokens(T, V):
+    ids = _ids(T, V, 7, skew=False)
+    d = torch.randn((T, 8), device="cuda")
+    dw = torch.full((V, 8), math.nan, device="cuda")
+    nopfs.token_embed_grad(d, ids, V, 1.0, dweight=dw)
+    want = torch.zeros((V, 8), dtype=torch.float64, device="cuda").index_add_(0, ids.long(), d.double())
+    mag = torch.zeros((V, 8), dtype=torch.float64, device="cuda").index_add_(0, ids.long(), d.double().abs())
+    # at most 9 tokens a row here: 8 additions in 32 bits
+    assert int(torch.bincount(ids, minlength=1).max()) <= 9
+    assert bool(((dw.double() - want).abs() <= 9 * 2.0**-24 * mag).all())
+
+
+def test_more_workgroups_than_one_launch_dimension_holds():
+    """A row of more than 2,048 elements is a workgroup's: 2^20 of them and a few."""
+    T, V, D = 2**20 + 37, 5, 2_056
+    w = torch.randn((V, D), device="cuda").to(BF)
+    ids = (torch.arange(T, device="cuda") % (V + 1) - 1).int()  # -1: padding
+    out = nopfs.token_embed(w, ids)
+    rows = torch.cat([torch.zeros((1, D), dtype=BF, device="cuda"), w])
+    for a in range(0, T, 2**18):
+        part = ids[a:a + 2**18].long() + 1
+        assert torch.equal(out[a:a + 2**18], rows[part])
