@@ -204,14 +204,6 @@ __global__ void __launch_bounds__(256) te_scatter(const Embed d, const Sort s) {
 constexpr int kSmallKeys = 6;  // of a thread
 constexpr int64_t kSmallSort = 1024 * kSmallKeys, kSmallNames = 1 << 18;
 
-// A wave's lanes go on together from here, behind what all of them have read and
-// written in LDS.
-__device__ __forceinline__ void wave_step() {
-  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-  __builtin_amdgcn_wave_barrier();
-  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-}
-
 __global__ void __launch_bounds__(1024) te_sort(const Embed d, const Sort s, int passes) {
   constexpr int kBins = 256, kWaves = 16;
   __shared__ uint32_t keys[kSmallSort], vals[kSmallSort], base[kBins], tmp[65];

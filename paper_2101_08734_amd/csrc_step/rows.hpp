@@ -115,6 +115,14 @@ __device__ __forceinline__ float group_sum(float v) {
   return v;
 }
 
+// A wave's lanes go on together from here, behind what all of them have read and
+// written in LDS.
+__device__ __forceinline__ void wave_step() {
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+}
+
 // A type's code in the C ABI as a type: f(E()).
 template <class F>
 int by_dtype(int32_t code, F f) {

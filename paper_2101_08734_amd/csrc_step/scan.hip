@@ -38,6 +38,7 @@ struct Scan {
   void *h, *dx, *dgate;
   float *last, *carry, *dh0;
   uint32_t* drawn;  // [tiles]: chunks that workgroups have drawn, kLine words apart
+  int32_t* sample;  // [chunks]: of the chunk's first token
   uint64_t* slots;  // [chunks][tiles][64 kN]: what a chunk has said, of its lanes' first channels, then second
 };
 
@@ -157,20 +158,31 @@ __device__ inline int32_t sample_of(const Scan& d, int64_t t) {
   }
   return lo;
 }
-// Of tokens t0 .. t0 + kTile - 1, by all threads; ends with a barrier.
-__device__ inline void make_marks(const Scan& d, int64_t t0, Marks* m) {
+// Of tokens t0 .. t0 + kTile - 1, by one wave, 64 samples at a time from s0, the first
+// that matters. The first of them are read before the wave's own rows, whose loads
+// theirs would otherwise wait for, and written behind.
+struct Samples {
+  int64_t s;
+  int32_t a, b;  // its tokens
+};
+__device__ __forceinline__ Samples read_samples(const Scan& d, int64_t s0) {
+  const int64_t s = s0 + int64_t(__lane_id());
+  Samples v{s, INT32_MAX, 0};
+  if (s < d.n) v.a = d.start[s], v.b = d.start[s + 1];
+  return v;
+}
+__device__ inline void write_marks(const Scan& d, int64_t t0, Samples v, Marks* m) {
   const int64_t t1 = t0 + kTile < d.T ? t0 + kTile : d.T;
-  const int32_t s0 = d.n > 0 ? sample_of(d, t0) : 0;
-  for (int i = threadIdx.x; i < kTile; i += 64 * kWaves) m->first[i] = m->end[i] = 0;
-  __syncthreads();
-  for (int64_t s = s0 + int64_t(threadIdx.x); s < d.n; s += 64 * kWaves) {
-    const int64_t a = d.start[s], b = d.start[s + 1];
-    if (a >= t1) break;
-    if (a >= b) continue;  // no tokens
-    if (a >= t0) m->first[a - t0] = int32_t(s) + 1;
-    if (b > t0 && b <= t1) m->end[b - 1 - t0] = int32_t(s) + 1;
+  for (int i = __lane_id(); i < kTile; i += 64) m->first[i] = m->end[i] = 0;
+  for (;;) {
+    wave_step();
+    if (v.a < v.b) {  // it has tokens
+      if (v.a >= t0 && v.a < t1) m->first[v.a - t0] = int32_t(v.s) + 1;
+      if (v.b > t0 && v.b <= t1) m->end[v.b - 1 - t0] = int32_t(v.s) + 1;
+    }
+    if (!(__ballot(v.a < t1) >> 63)) break;  // the last of them is behind the chunk, or there is none
+    v = read_samples(d, v.s - __lane_id() + 64);
   }
-  __syncthreads();
 }
 // Bit r: row r of the wave.
 __device__ __forceinline__ uint32_t wave_marks(const int32_t* m) {
@@ -218,14 +230,18 @@ __device__ __forceinline__ void keep_map(Maps<kN>* m, bool reset, const float (&
   for (int i = 0; i < kN; ++i) m->A[wave][i * 64 + lane] = A[i], m->B[wave][i * 64 + lane] = B[i];
   if (lane == 0) m->reset[wave] = reset;
 }
-template <int kN>
-__device__ __forceinline__ void through_wave(const Maps<kN>& m, int w, float (&h)[kN]) {
-  const int lane = threadIdx.x & 63;
-  const bool reset = uniform(m.reset[w]);
+// The state before each wave's rows from that before the workgroup's, in place of the
+// maps' B; by wave i < kN for the i-th channels. kBack: from the last wave on.
+template <bool kBack, int kN>
+__device__ __forceinline__ void spread(Maps<kN>* m, float state) {
+  const int mine = threadIdx.x;
 #pragma unroll
-  for (int i = 0; i < kN; ++i) {
-    const float A = m.A[w][i * 64 + lane], B = m.B[w][i * 64 + lane];
-    h[i] = reset ? B : fmaf(A, h[i], B);
+  for (int j = 0; j < kWaves; ++j) {
+    const int w = kBack ? kWaves - 1 - j : j;
+    const bool cut = uniform(m->reset[w]);
+    const float a = m->A[w][mine], b = m->B[w][mine];
+    m->B[w][mine] = state;
+    state = cut ? b : fmaf(a, state, b);
   }
 }
 
@@ -239,20 +255,18 @@ __device__ __forceinline__ int32_t draw(const Scan& d, uint32_t tile) {
   return uniform(int32_t(drawn));
 }
 
-// What the waves of a workgroup leave for each other on the way.
+// What a chunk has been told: the state before the group, then the maps up to its own.
 template <int kN>
 struct Chain {
-  uint64_t said[kGroup][64 * kN];  // the state before the group, then the maps up to this chunk's
-  float state[64 * kN];
+  uint64_t said[kGroup][64 * kN];
 };
 
 // The state before chunk number `at` of the chain (kBack: chunk chunks - 1 - at);
 // tells the others the chunk's map, or the state behind its group. After a barrier
-// behind keep_map. Wave i < kN works on the i-th channels of all lanes, the waves
-// share the waiting, and all get the state.
+// behind keep_map. Wave i < kN works on the i-th channels of all lanes and gets their
+// state, the waves share the waiting.
 template <bool kBack, int kN>
-__device__ inline void chain(const Scan& d, int32_t at, uint32_t tile, const Maps<kN>& maps, Chain<kN>* lds,
-                             float (&h)[kN]) {
+__device__ inline float chain(const Scan& d, int32_t at, uint32_t tile, const Maps<kN>& maps, Chain<kN>* lds) {
   const int wave = wave_id(), lane = threadIdx.x & 63, mine = wave * 64 + lane;
   const int pos = at & (kGroup - 1);
   uint64_t* slots = d.slots + (int64_t(at - pos) * d.tiles + tile) * 64 * kN;  // of the group's first chunk
@@ -288,26 +302,27 @@ __device__ inline void chain(const Scan& d, int32_t at, uint32_t tile, const Map
     lds->said[from][i * 64 + lane] = v;
   }
   __syncthreads();
+  float state = 0.0f;
   if (wave < kN) {
-    float state = 0.0f;
 #pragma unroll
     for (int j = 0; j < kGroup; ++j)
       if (j <= pos) state = through(lds->said[j][mine], state);
     if (pos == kGroup - 1 && !reset)
       __hip_atomic_store(slots + pos * next + mine, slot_state(fmaf(A, state, B)), __ATOMIC_RELAXED,
                          __HIP_MEMORY_SCOPE_AGENT);
-    lds->state[mine] = state;
   }
-  __syncthreads();
-#pragma unroll
-  for (int i = 0; i < kN; ++i) h[i] = lds->state[i * 64 + lane];
+  return state;
 }
 
-// Nothing said, nothing drawn.
+// Nothing said, nothing drawn; and the sample of each chunk's first token.
 __global__ void __launch_bounds__(256) gs_clear(const Scan d, int64_t n) {
   for (int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x; i < n; i += int64_t(gridDim.x) * 256) d.slots[i] = 0;
   for (int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x; i < d.tiles; i += int64_t(gridDim.x) * 256)
     d.drawn[i * kLine] = 0;
+  for (int64_t c = int64_t(blockIdx.x) * 4 + wave_id(); c < d.chunks; c += int64_t(gridDim.x) * 4) {
+    const int32_t s = d.n > 0 ? sample_of(d, c * kTile) : 0;
+    if ((threadIdx.x & 63) == 0) d.sample[c] = s;
+  }
 }
 
 // Samples without tokens: their states go through. Workgroups behind the last
@@ -336,6 +351,9 @@ __global__ void __launch_bounds__(64 * kWaves, 6) gs_forward(const Scan d, uint3
   const int wave = wave_id();
   const Cols<E> col = make_cols<E>(d, tile);
   const int64_t t0 = int64_t(chunk) * kTile, t = t0 + wave * kRows;
+  const bool marks_them = wave == kWaves - 1;
+  Samples samples{};
+  if (marks_them) samples = read_samples(d, kChain ? uniform(d.sample[chunk]) : d.n > 0 ? sample_of(d, t0) : 0);
   const int there = t >= d.T ? 0 : d.T - t < kRows ? int(d.T - t) : kRows;  // rows; `rows` of them in samples
   Pack<E, kN> x[kRows];
   float share[kRows][kN];
@@ -343,6 +361,7 @@ __global__ void __launch_bounds__(64 * kWaves, 6) gs_forward(const Scan d, uint3
     Pack<E, kN> g[kRows];
     load_rows<E>(d.gate, d.gate_stride, t, there, col, g);
     load_rows<E>(d.x, d.x_stride, t, there, col, x);
+    if (marks_them) write_marks(d, t0, samples, &marks);
 #pragma unroll
     for (int r = 0; r < kRows; ++r)
 #pragma unroll
@@ -350,7 +369,7 @@ __global__ void __launch_bounds__(64 * kWaves, 6) gs_forward(const Scan d, uint3
   }
   const int64_t total = tokens_of(d);
   const int rows = total <= t ? 0 : total - t < kRows ? int(total - t) : kRows;
-  make_marks(d, t0, &marks);
+  __syncthreads();
   const uint32_t first = wave_marks(marks.first), end = wave_marks(marks.end);
   const int32_t *starts = marks.first + wave * kRows, *ends = marks.end + wave * kRows;
   {
@@ -374,9 +393,13 @@ __global__ void __launch_bounds__(64 * kWaves, 6) gs_forward(const Scan d, uint3
     keep_map<kN>(&maps, first != 0, A, B);
   }
   __syncthreads();
-  float h[kN] = {};
-  if constexpr (kChain) chain<false, kN>(d, chunk, tile, maps, &lds, h);
-  for (int w = 0; w < wave; ++w) through_wave<kN>(maps, w, h);
+  float before = 0.0f;
+  if constexpr (kChain) before = chain<false, kN>(d, chunk, tile, maps, &lds);
+  if (wave < kN) spread<false, kN>(&maps, before);
+  __syncthreads();
+  float h[kN];
+#pragma unroll
+  for (int i = 0; i < kN; ++i) h[i] = maps.B[wave][i * 64 + (threadIdx.x & 63)];
   const float none[kN] = {};
 #pragma unroll
   for (int r = 0; r < kRows; ++r) {
@@ -464,6 +487,9 @@ __global__ void __launch_bounds__(64 * kWaves, 4) gs_grad(const Scan d, uint32_t
   const int wave = wave_id();
   const Cols<E> col = make_cols<E>(d, tile);
   const int64_t t0 = int64_t(d.chunks - 1 - at) * kTile, t = t0 + wave * kRows;
+  const bool marks_them = wave == kWaves - 1;
+  Samples samples{};
+  if (marks_them) samples = read_samples(d, kChain ? uniform(d.sample[d.chunks - 1 - at]) : d.n > 0 ? sample_of(d, t0) : 0);
   const int there = t >= d.T ? 0 : d.T - t < kRows ? int(d.T - t) : kRows;
   Pack<E, kN> dh[kRows];
   float share[kRows][kN], under[kRows][kN];  // under: h_{t-1} - x_t
@@ -475,6 +501,7 @@ __global__ void __launch_bounds__(64 * kWaves, 4) gs_grad(const Scan d, uint32_t
     load_rows<E>(d.gate, d.gate_stride, t, there, col, g);
     load_rows<E>(d.dh, d.dh_stride, t, there, col, dh);
     load_rows<E>(d.x, d.x_stride, t, there, col, x);
+    if (marks_them) write_marks(d, t0, samples, &marks);
 #pragma unroll
     for (int r = 0; r < kRows; ++r)
 #pragma unroll
@@ -482,7 +509,7 @@ __global__ void __launch_bounds__(64 * kWaves, 4) gs_grad(const Scan d, uint32_t
   }
   const int64_t total = tokens_of(d);
   const int rows = total <= t ? 0 : total - t < kRows ? int(total - t) : kRows;
-  make_marks(d, t0, &marks);
+  __syncthreads();
   const uint32_t first = wave_marks(marks.first), end = wave_marks(marks.end);
   const int32_t *starts = marks.first + wave * kRows, *ends = marks.end + wave * kRows;
   {
@@ -521,9 +548,13 @@ __global__ void __launch_bounds__(64 * kWaves, 4) gs_grad(const Scan d, uint32_t
     }
   }
   __syncthreads();
-  float R[kN] = {};
-  if constexpr (kChain) chain<true, kN>(d, at, tile, maps, &lds, R);
-  for (int w = kWaves - 1; w > wave; --w) through_wave<kN>(maps, w, R);
+  float behind = 0.0f;
+  if constexpr (kChain) behind = chain<true, kN>(d, at, tile, maps, &lds);
+  if (wave < kN) spread<true, kN>(&maps, behind);
+  __syncthreads();
+  float R[kN];
+#pragma unroll
+  for (int i = 0; i < kN; ++i) R[i] = maps.B[wave][i * 64 + (threadIdx.x & 63)];
 #pragma unroll
   for (int r = kRows - 1; r >= 0; --r) {
     if (r >= there) continue;
@@ -586,7 +617,8 @@ int make_chain(Scratch* sc, Scan* d, int per, hipStream_t st) {
   if (d->chunks <= 1) return NOPFS_OK;
   int rc;
   const size_t n = size_t(d->chunks) * size_t(d->tiles) * size_t(per);
-  if ((rc = step_alloc(sc, &d->slots, n)) || (rc = step_alloc(sc, &d->drawn, size_t(d->tiles) * kLine))) return rc;
+  if ((rc = step_alloc(sc, &d->slots, n)) || (rc = step_alloc(sc, &d->drawn, size_t(d->tiles) * kLine)) ||
+      (rc = step_alloc(sc, &d->sample, size_t(d->chunks)))) return rc;
   return launch("gs_clear", gs_clear, dim3(uint32_t(std::min<int64_t>(ceil_div(int64_t(n), 1024), 4096))), dim3(256),
                 0, st, *d, int64_t(n));
 }
