@@ -617,8 +617,8 @@ typedef struct nopfs_scan {
  *          a sample without tokens), or NULL.
  *   carry: float [ceil(T / NOPFS_SCAN_CHUNK)][channels], the states that the
  *          gradient starts from, or NULL.
- * Rows from start[n] on get h = 0 and are not read. A NaN or infinity reaches no
- * other sample. Errors: EINVAL, ERANGE, ENOMEM, EDEVICE. */
+ * Rows from start[n] on get h = 0, whatever x and gate hold there. A NaN or
+ * infinity reaches no other sample. Differences of x and the state stay below 2^128. Errors: EINVAL, ERANGE, ENOMEM, EDEVICE. */
 int nopfs_gated_scan(const nopfs_scan* s, const void* x, const void* gate, const int32_t* start,
                      const float* h0, void* h, float* last, float* carry, void* hip_stream);
 

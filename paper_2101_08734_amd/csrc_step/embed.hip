@@ -314,9 +314,8 @@ __global__ void __launch_bounds__(256) te_scatter_zero(const Embed d, const Sort
 // ---- sums ------------------------------------------------------------------
 // The sorted tokens are cut into pieces of equal size, however many of them share
 // a name (a row of the embedding each: 1,114 us where this takes 100), by groups of
-// 2^lg lanes. A name whose tokens lie in one piece has its row
-// written from there; the others leave the sum of each piece's part, and te_join
-// adds those up in order.
+// 2^lg lanes. A name whose tokens lie in one piece has its row written from there; the
+// others leave the sum of each piece's part, and te_join adds those up in order.
 struct Pieces {
   const uint32_t *key, *val;
   float *head, *tail;  // [pieces][width]: of the name that goes on from the piece before; into the next
@@ -573,7 +572,7 @@ int embed_grad_impl(const nopfs_embed* p, const void* dout, const void* ids, con
       return launch("te_pieces", te_pieces<W, E>, row_grid(blocks + (zeroed ? 0 : zeros)), dim3(256), 0, st, d, pc,
                     static_cast<const typename E::T*>(dout), to, lg, uint32_t(blocks), s.named);
     });
-    if (r) return r;
+    if (r || pc.n <= 1) return r;  // one piece: no name has parts
     const int jg = std::min(6, log2_ceil(ceil_div(p->width, 4)));
     return launch("te_join", te_join<W>, dim3(uint32_t(pc.n), uint32_t(ceil_div(p->width, 4 << jg))), dim3(256), 0, st,
                   d, pc, to, jg);
