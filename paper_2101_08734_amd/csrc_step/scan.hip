@@ -112,10 +112,15 @@ __device__ __forceinline__ void store_state(float* base, int64_t row, const Scan
 // The smaller of a and k = 1 - a, with the gate's sign (negative: it is a). Of
 // gates in 32 bits the exponent's rounding is made up for; those of 16 bits leave
 // it, |gate| units of 2^-24 of the share, far below their own outputs' roundings.
+// From 88 on the share is 0; t of a much larger gate in 32 bits would be infinite, and
+// so what it has lost.
+constexpr float kMostGate = 128.0f;
 template <class E>
 __device__ __forceinline__ float share_of(float gate) {
   constexpr float kLog2e = 1.4426950408889634f, kLog2eLow = 1.9259629911266175e-8f, kLn2 = 0.6931471805599453f;
-  const float g = fabsf(gate), t = -g * kLog2e;
+  float g = fabsf(gate);
+  if constexpr (sizeof(typename E::T) == 4) g = g > kMostGate ? kMostGate : g;  // NaN stays
+  const float t = -g * kLog2e;
   float e = __builtin_amdgcn_exp2f(t);
   if constexpr (sizeof(typename E::T) == 4) {
     const float low = fmaf(-g, kLog2e, -t) - g * kLog2eLow;  // what t has lost
