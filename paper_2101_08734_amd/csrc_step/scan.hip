@@ -109,24 +109,23 @@ __device__ __forceinline__ void store_state(float* base, int64_t row, const Scan
     if (i == 0 || !col.one) p[i] = v[i];
 }
 
-// The smaller of a and k = 1 - a, with the gate's sign (negative: it is a). Of
-// gates in 32 bits the exponent's rounding is made up for; those of 16 bits leave
-// it, |gate| units of 2^-24 of the share, far below their own outputs' roundings.
-// From 88 on the share is 0; t of a much larger gate in 32 bits would be infinite, and
-// so what it has lost.
+// The smaller of a and k = 1 - a, with the gate's sign (negative: it is a), of gates of
+// any type within 6 units of 2^-24 (the exponential 3, the sum, the reciprocal and the
+// product 1 each): the exponent's rounding is made up for, the reciprocal refined. From
+// 88 on the share is 0; the exponent of a much larger gate in 32 bits, or of an infinite
+// one, would have lost an infinity.
 constexpr float kMostGate = 128.0f;
-template <class E>
 __device__ __forceinline__ float share_of(float gate) {
-  constexpr float kLog2e = 1.4426950408889634f, kLog2eLow = 1.9259629911266175e-8f, kLn2 = 0.6931471805599453f;
+  constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f, kLn2Low = -1.9046543e-9f;
   float g = fabsf(gate);
-  if constexpr (sizeof(typename E::T) == 4) g = g > kMostGate ? kMostGate : g;  // NaN stays
+  g = g > kMostGate ? kMostGate : g;  // NaN stays
   const float t = -g * kLog2e;
   float e = __builtin_amdgcn_exp2f(t);
-  if constexpr (sizeof(typename E::T) == 4) {
-    const float low = fmaf(-g, kLog2e, -t) - g * kLog2eLow;  // what t has lost
-    e = fmaf(e * kLn2, low, e);
-  }
-  return copysignf(e * __builtin_amdgcn_rcpf(1.0f + e), gate);
+  e = fmaf(e, fmaf(-t, kLn2Low, fmaf(-t, kLn2, -g)), e);  // by what t has lost
+  const float sum = 1.0f + e;
+  float r = __builtin_amdgcn_rcpf(sum);
+  r = fmaf(r, fmaf(-sum, r, 1.0f), r);
+  return copysignf(e * r, gate);
 }
 __device__ __forceinline__ bool is_a(float share) { return __float_as_int(share) < 0; }
 __device__ __forceinline__ float a_of(float share) { return is_a(share) ? -share : 1.0f - share; }
@@ -370,7 +369,7 @@ __global__ void __launch_bounds__(64 * kWaves, 6) gs_forward(const Scan d, uint3
 #pragma unroll
     for (int r = 0; r < kRows; ++r)
 #pragma unroll
-      for (int i = 0; i < kN; ++i) share[r][i] = share_of<E>(g[r].get(i));
+      for (int i = 0; i < kN; ++i) share[r][i] = share_of(g[r].get(i));
   }
   const int64_t total = tokens_of(d);
   const int rows = total <= t ? 0 : total - t < kRows ? int(total - t) : kRows;
@@ -447,7 +446,7 @@ __global__ void __launch_bounds__(256) gs_step(const Scan d) {
   auto token = [&](int64_t t, const Pack<E, kN>& x, const Pack<E, kN>& g) {
     if (d.carry && t % kRows == 0) store_state<E>(d.carry, t / kRows, d, col, h);
 #pragma unroll
-    for (int i = 0; i < kN; ++i) h[i] = step(share_of<E>(g.get(i)), h[i], x.get(i));
+    for (int i = 0; i < kN; ++i) h[i] = step(share_of(g.get(i)), h[i], x.get(i));
     store_row<E>(d.h, d.h_stride, t, col, h);
   };
   if (s == d.n) {
@@ -510,7 +509,7 @@ __global__ void __launch_bounds__(64 * kWaves, 4) gs_grad(const Scan d, uint32_t
 #pragma unroll
     for (int r = 0; r < kRows; ++r)
 #pragma unroll
-      for (int i = 0; i < kN; ++i) share[r][i] = share_of<E>(g[r].get(i));
+      for (int i = 0; i < kN; ++i) share[r][i] = share_of(g[r].get(i));
   }
   const int64_t total = tokens_of(d);
   const int rows = total <= t ? 0 : total - t < kRows ? int(total - t) : kRows;

@@ -107,3 +107,20 @@ def test_nan_gates_stay(dt, lengths):
     others[a:b, 7] = False
     for name in ("h", "dx", "dgate"):
         assert torch.equal(got[name][others], want[name][others])
+
+
+@pytest.mark.parametrize("dt", [BF, FP, F32], ids=NAMES.get)
+@pytest.mark.parametrize("n", [300, 1_100])
+def test_shares_to_32_bits(dt, n):
+    """The smaller of a and 1 - a, of gates of any type: 6 E of it (the exponential 3,
+    the sum, the reciprocal and the product 1 each), E for the product with the state or
+    the input; 0 below 2^-126. `last` of single tokens, by themselves and by chunks."""
+    g = torch.Generator().manual_seed(n)
+    gate = (172 * torch.rand((n, 40), generator=g) - 86).to(dt)
+    forgets = gate < 0
+    y = torch.randn((n, 40), generator=g).to(dt)
+    x, h0 = torch.where(forgets, 0, y), torch.where(forgets, y, 0).float()
+    start = torch.arange(n + 1, dtype=torch.int32)
+    last = nopfs.gated_scan(*(t.cuda() for t in (x, gate, start, h0)))[1]
+    val = torch.sigmoid(-gate.double().abs()) * y.double()
+    close("last", last, val, 8 * 2.0**-24 * val.abs() + 2.0**-126 * y.double().abs() + 2.0**-149)
