@@ -14,8 +14,11 @@
 // and 77 us, the gradient 114 and 132.
 //
 // The states and maps are in 32 bits. A step is taken from the larger share,
-// h + k (x - h) or x + a (h - x), so that its rounding is half a unit of the
-// result and a gate near 1 costs no accuracy over many tokens.
+// h + k (x - h) or x + a (h - x), so that its rounding is half a unit of the result; a
+// map likewise, by the smaller of A and 1 - A, each made by such steps, so that a gate
+// near 1 loses nothing to the rounding of a product of its a. What goes from chunk to
+// chunk so has one rounding of the state per chunk of 128 tokens: 25,600 tokens of gate
+// 12.2 (a = 1 - 5e-6) are off by 2e-7, token by token by 1e-6, by products of a by 3e-4.
 #include "rows.hpp"
 
 namespace nopfs {
@@ -132,6 +135,13 @@ __device__ __forceinline__ float a_of(float share) { return is_a(share) ? -share
 __device__ __forceinline__ float step(float share, float h, float x) {
   return fmaf(share, x - h, is_a(share) ? x : h);  // x + a (h - x), or h + k (x - h)
 }
+// A stretch's map: B + A h, with the smaller of A and K = 1 - A as its share. A and K
+// are what the stretch's steps make of 1 among zeros, and of 0 among ones.
+__device__ __forceinline__ float map_share(float A, float K) { return A <= K ? -A : K; }
+__device__ __forceinline__ float apply(float share, float B, float h) {
+  const float y = fmaf(-share, h, B);  // B + A h, or B - K h
+  return is_a(share) ? y : h + y;
+}
 // G's two shares, a G and k G.
 __device__ __forceinline__ void split(float share, float G, float* aG, float* kG) {
   const float small = fabsf(share) * G, large = G - small;
@@ -196,7 +206,7 @@ __device__ __forceinline__ uint32_t wave_marks(const int32_t* m) {
 
 // ---- from chunk to chunk ------------------------------------------------------
 // The state behind a chunk is B + A times the state before it. Every chunk says
-// its map (A, B), which takes only its own tokens; the last of a group of kGroup
+// its map, which takes only its own tokens; the last of a group of kGroup
 // chunks says, when it knows the state before it, the state behind it instead. A
 // chunk applies the maps of its group before it to the state behind the group
 // before. So the chain is one wait per group, and the order of all roundings is fixed.
@@ -205,33 +215,37 @@ __device__ __forceinline__ uint32_t wave_marks(const int32_t* m) {
 // those of the 16 before it, 81 and 167.)
 //
 // A slot is one 64-bit word, written and read whole, so it needs no order with
-// others: the upper half is A with its sign bit set (A is in 0 .. 1, or NaN), or
-// kAbsolute where the lower half is the state whatever came before; 0: nothing yet.
+// others: the upper half is the map's share, or kAbsolute where the lower half is the
+// state whatever came before, or kNothing yet (both infinities, which no share is).
 // A workgroup draws its chunk from its tile's counter, so all chunks that it waits
 // for have been drawn by workgroups that run or have run.
-constexpr uint32_t kAbsolute = 0xFF800000u;
+constexpr uint32_t kAbsolute = 0xFF800000u, kNothing = 0x7F800000u;
 
-__device__ __forceinline__ uint64_t slot_map(float A, float B) {
-  return uint64_t(__float_as_uint(A) | 0x80000000u) << 32 | __float_as_uint(B);
+__device__ __forceinline__ uint64_t slot_map(float share, float B) {
+  return uint64_t(__float_as_uint(share)) << 32 | __float_as_uint(B);
 }
 __device__ __forceinline__ uint64_t slot_state(float h) { return uint64_t(kAbsolute) << 32 | __float_as_uint(h); }
 __device__ __forceinline__ float through(uint64_t slot, float h) {
   const uint32_t code = uint32_t(slot >> 32);
   const float B = __uint_as_float(uint32_t(slot));
-  return code == kAbsolute ? B : fmaf(__uint_as_float(code & 0x7FFFFFFFu), h, B);
+  return code == kAbsolute ? B : apply(__uint_as_float(code), B, h);
 }
 
-// The maps of a workgroup's waves; of a wave with a reset, A is not used.
+// The maps of a workgroup's waves; of a wave with a reset, the share is not used.
 template <int kN>
 struct Maps {
-  float A[kWaves][64 * kN], B[kWaves][64 * kN];
+  float share[kWaves][64 * kN], B[kWaves][64 * kN];
   uint32_t reset[kWaves];
 };
 template <int kN>
-__device__ __forceinline__ void keep_map(Maps<kN>* m, bool reset, const float (&A)[kN], const float (&B)[kN]) {
+__device__ __forceinline__ void keep_map(Maps<kN>* m, bool reset, const float (&A)[kN], const float (&K)[kN],
+                                         const float (&B)[kN]) {
   const int wave = wave_id(), lane = threadIdx.x & 63;
 #pragma unroll
-  for (int i = 0; i < kN; ++i) m->A[wave][i * 64 + lane] = A[i], m->B[wave][i * 64 + lane] = B[i];
+  for (int i = 0; i < kN; ++i) {
+    m->share[wave][i * 64 + lane] = map_share(A[i], K[i]);
+    m->B[wave][i * 64 + lane] = B[i];
+  }
   if (lane == 0) m->reset[wave] = reset;
 }
 // The state before each wave's rows from that before the workgroup's, in place of the
@@ -243,9 +257,9 @@ __device__ __forceinline__ void spread(Maps<kN>* m, float state) {
   for (int j = 0; j < kWaves; ++j) {
     const int w = kBack ? kWaves - 1 - j : j;
     const bool cut = uniform(m->reset[w]);
-    const float a = m->A[w][mine], b = m->B[w][mine];
+    const float share = m->share[w][mine], b = m->B[w][mine];
     m->B[w][mine] = state;
-    state = cut ? b : fmaf(a, state, b);
+    state = cut ? b : apply(share, b, state);
   }
 }
 
@@ -275,21 +289,22 @@ __device__ inline float chain(const Scan& d, int32_t at, uint32_t tile, const Ma
   const int pos = at & (kGroup - 1);
   uint64_t* slots = d.slots + (int64_t(at - pos) * d.tiles + tile) * 64 * kN;  // of the group's first chunk
   const int64_t next = int64_t(d.tiles) * 64 * kN;
-  float A = 1.0f, B = 0.0f;
+  float A = 1.0f, K = 0.0f, B = 0.0f;
   bool reset = false;
   if (wave < kN) {
 #pragma unroll
     for (int j = 0; j < kWaves; ++j) {
       const int w = kBack ? kWaves - 1 - j : j;
       const bool cut = uniform(maps.reset[w]);
-      const float a = maps.A[w][mine], b = maps.B[w][mine];
-      A *= a;
-      B = cut ? b : fmaf(a, B, b);
+      const float share = maps.share[w][mine], b = maps.B[w][mine];
+      A = step(share, A, 0.0f);
+      K = step(share, K, 1.0f);
+      B = cut ? b : apply(share, b, B);
       reset |= cut;
     }
     if (pos < kGroup - 1 || reset)
-      __hip_atomic_store(slots + pos * next + mine, reset ? slot_state(B) : slot_map(A, B), __ATOMIC_RELAXED,
-                         __HIP_MEMORY_SCOPE_AGENT);
+      __hip_atomic_store(slots + pos * next + mine, reset ? slot_state(B) : slot_map(map_share(A, K), B),
+                         __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
   }
   for (int j = wave; j < (pos + 1) * kN; j += kWaves) {
     const int from = j / kN, i = j & (kN - 1);  // 0: the chunk before the group
@@ -299,7 +314,7 @@ __device__ inline float chain(const Scan& d, int32_t at, uint32_t tile, const Ma
       for (;;) {
         v = __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
         const uint32_t code = uint32_t(v >> 32);
-        if (__all(from ? code != 0 : code == kAbsolute)) break;
+        if (__all(from ? code != kNothing : code == kAbsolute)) break;
         __builtin_amdgcn_s_sleep(1);
       }
     }
@@ -312,7 +327,7 @@ __device__ inline float chain(const Scan& d, int32_t at, uint32_t tile, const Ma
     for (int j = 0; j < kGroup; ++j)
       if (j <= pos) state = through(lds->said[j][mine], state);
     if (pos == kGroup - 1 && !reset)
-      __hip_atomic_store(slots + pos * next + mine, slot_state(fmaf(A, state, B)), __ATOMIC_RELAXED,
+      __hip_atomic_store(slots + pos * next + mine, slot_state(apply(map_share(A, K), B, state)), __ATOMIC_RELAXED,
                          __HIP_MEMORY_SCOPE_AGENT);
   }
   return state;
@@ -320,7 +335,8 @@ __device__ inline float chain(const Scan& d, int32_t at, uint32_t tile, const Ma
 
 // Nothing said, nothing drawn; and the sample of each chunk's first token.
 __global__ void __launch_bounds__(256) gs_clear(const Scan d, int64_t n) {
-  for (int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x; i < n; i += int64_t(gridDim.x) * 256) d.slots[i] = 0;
+  for (int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x; i < n; i += int64_t(gridDim.x) * 256)
+    d.slots[i] = uint64_t(kNothing) << 32;
   for (int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x; i < d.tiles; i += int64_t(gridDim.x) * 256)
     d.drawn[i * kLine] = 0;
   for (int64_t c = int64_t(blockIdx.x) * 4 + wave_id(); c < d.chunks; c += int64_t(gridDim.x) * 4) {
@@ -377,9 +393,9 @@ __global__ void __launch_bounds__(64 * kWaves, 6) gs_forward(const Scan d, uint3
   const uint32_t first = wave_marks(marks.first), end = wave_marks(marks.end);
   const int32_t *starts = marks.first + wave * kRows, *ends = marks.end + wave * kRows;
   {
-    float A[kN], B[kN];
+    float A[kN], K[kN], B[kN];
 #pragma unroll
-    for (int i = 0; i < kN; ++i) A[i] = 1.0f, B[i] = 0.0f;
+    for (int i = 0; i < kN; ++i) A[i] = 1.0f, K[i] = B[i] = 0.0f;
 #pragma unroll
     for (int r = 0; r < kRows; ++r) {
       if (r >= rows) continue;
@@ -391,10 +407,11 @@ __global__ void __launch_bounds__(64 * kWaves, 6) gs_forward(const Scan d, uint3
 #pragma unroll
       for (int i = 0; i < kN; ++i) {
         B[i] = step(share[r][i], B[i], x[r].get(i));
-        A[i] *= a_of(share[r][i]);
+        A[i] = step(share[r][i], A[i], 0.0f);
+        K[i] = step(share[r][i], K[i], 1.0f);
       }
     }
-    keep_map<kN>(&maps, first != 0, A, B);
+    keep_map<kN>(&maps, first != 0, A, K, B);
   }
   __syncthreads();
   float before = 0.0f;
@@ -517,9 +534,9 @@ __global__ void __launch_bounds__(64 * kWaves, 4) gs_grad(const Scan d, uint32_t
   const uint32_t first = wave_marks(marks.first), end = wave_marks(marks.end);
   const int32_t *starts = marks.first + wave * kRows, *ends = marks.end + wave * kRows;
   {
-    float A[kN], R[kN];
+    float A[kN], K[kN], R[kN];
 #pragma unroll
-    for (int i = 0; i < kN; ++i) A[i] = 1.0f, R[i] = 0.0f;
+    for (int i = 0; i < kN; ++i) A[i] = 1.0f, K[i] = R[i] = 0.0f;
 #pragma unroll
     for (int r = kRows - 1; r >= 0; --r) {
       if (r >= rows) continue;
@@ -532,10 +549,11 @@ __global__ void __launch_bounds__(64 * kWaves, 4) gs_grad(const Scan d, uint32_t
       for (int i = 0; i < kN; ++i) {
         float kG;
         split(share[r][i], dh[r].get(i) + R[i], &R[i], &kG);
-        A[i] *= a_of(share[r][i]);
+        A[i] = step(share[r][i], A[i], 0.0f);
+        K[i] = step(share[r][i], K[i], 1.0f);
       }
     }
-    keep_map<kN>(&maps, end != 0, A, R);
+    keep_map<kN>(&maps, end != 0, A, K, R);
   }
 #pragma unroll
   for (int r = 0; r < kRows; ++r) {
