@@ -45,7 +45,8 @@ __device__ inline float weight_at(const void* w, int32_t dtype, int i) {
 }
 
 // Sine and cosine of the angles of `tok` tokens from t0, by all threads. An angle
-// in turns is reduced in 64 bits, so that far positions keep 32 bits of theirs.
+// in turns is reduced in 64 bits, so that far positions keep 32 bits of theirs; what its
+// rounding to 32 bits leaves, up to 2^-26 turns, turns them a little further.
 __device__ inline void make_angles(const Rotate& d, int64_t t0, float2 (*cs)[kMostPairs]) {
   const int pairs = d.rotated >> 1;
   for (int i = threadIdx.x; i < d.tok * pairs; i += 64 * kWaves) {
@@ -54,9 +55,10 @@ __device__ inline void make_angles(const Rotate& d, int64_t t0, float2 (*cs)[kMo
     if (p < 0) continue;
     double turns = double(p) * (d.freq[f] * 0.15915494309189533577);
     turns -= rint(turns);
+    const float near = float(turns), rest = float((turns - double(near)) * 6.28318530717958647693);
     float s, c;
-    sincospif(2.0f * float(turns), &s, &c);
-    cs[k][f] = make_float2(c, s);
+    sincospif(2.0f * near, &s, &c);
+    cs[k][f] = make_float2(fmaf(-rest, s, c), fmaf(rest, c, s));
   }
 }
 
