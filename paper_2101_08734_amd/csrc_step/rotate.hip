@@ -212,6 +212,7 @@ __device__ __forceinline__ void grad_heads(const Rotate& d, const Side& side, in
   const T* g = static_cast<const T*>(side.d) + t * side.d_stride[0] + l.e0;
   T* out = static_cast<T*>(side.out) + t * side.out_stride[0] + l.e0;
   const float by_width = 1.0f / float(d.width);
+  float sum[kVec] = {};  // of the token
   for (int32_t h0 = part * kSlots; h0 < heads; h0 += parts * kSlots * kDeep) {
     Pack<E, kVec> v[kDeep], u[kDeep];
 #pragma unroll
@@ -238,7 +239,7 @@ __device__ __forceinline__ void grad_heads(const Rotate& d, const Side& side, in
         float dot = 0.0f;
 #pragma unroll
         for (int e = 0; e < kVec; ++e) {
-          dw[e] += y[e] * z[e];
+          sum[e] += y[e] * z[e];
           y[e] *= w[e];
           dot += y[e] * z[e];
         }
@@ -251,25 +252,37 @@ __device__ __forceinline__ void grad_heads(const Rotate& d, const Side& side, in
       if (l.active && h < heads) o.store(out + h * side.out_stride[1]);
     }
   }
+#pragma unroll
+  for (int e = 0; e < kVec; ++e) dw[e] += sum[e];
 }
 
 // A workgroup has every gridDim.x-th group of tokens; its sums of the weights'
-// gradients go to part[workgroup][2][width].
+// gradients go to part[workgroup][2][width]. A lane's are over a token's heads, of kRun
+// tokens, and of those, so that no long chain of roundings goes through one sum.
+constexpr int kRun = 64;
 template <class E, int kLanes>
 __global__ void __launch_bounds__(64 * kWaves) nr_grad(const Rotate d, const Side q, const Side k, float* part_sums) {
   __shared__ float2 cs[2][kWaves][kMostPairs];
   __shared__ float sums[2][kWaves][64][kVec];
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, mine = d.tok == 1 ? 0 : wave;
   Lane l = make_lane<kLanes>(d);
-  float wq[kVec], wk[kVec], dq[kVec] = {}, dk[kVec] = {};
+  float wq[kVec], wk[kVec], dq[kVec] = {}, dk[kVec] = {}, all_q[kVec] = {}, all_k[kVec] = {};
 #pragma unroll
   for (int e = 0; e < kVec; ++e) {
     wq[e] = l.active ? weight_at(d.q_weight, d.weight_dtype, l.e0 + e) : 0.0f;
     wk[e] = l.active ? weight_at(d.k_weight, d.weight_dtype, l.e0 + e) : 0.0f;
   }
   const int part = d.tok == 1 ? wave : 0, parts = d.tok == 1 ? kWaves : 1;
-  int which = 0;
+  int which = 0, run = 0;
   for (int64_t t0 = int64_t(blockIdx.x) * d.tok; t0 < d.T; t0 += int64_t(gridDim.x) * d.tok, which ^= 1) {
+    if (run++ == kRun) {
+      run = 1;
+#pragma unroll
+      for (int e = 0; e < kVec; ++e) {
+        all_q[e] += dq[e], all_k[e] += dk[e];
+        dq[e] = dk[e] = 0.0f;
+      }
+    }
     make_angles(d, t0, cs[which]);  // the other half may still be read
     __syncthreads();
     const int64_t t = t0 + mine;
@@ -282,24 +295,29 @@ __global__ void __launch_bounds__(64 * kWaves) nr_grad(const Rotate d, const Sid
   if (!part_sums) return;
 #pragma unroll
   for (int e = 0; e < kVec; ++e) {
-    sums[0][wave][lane][e] = dq[e];
-    sums[1][wave][lane][e] = dk[e];
+    sums[0][wave][lane][e] = all_q[e] + dq[e];
+    sums[1][wave][lane][e] = all_k[e] + dk[e];
   }
   __syncthreads();
   for (int i = threadIdx.x; i < 2 * d.width; i += 64 * kWaves) {
     const int side = i >= d.width, e = i - side * d.width;
     float s = 0.0f;
-    for (int w = 0; w < kWaves; ++w)
-      for (int slot = 0; slot < 64 / kLanes; ++slot) s += sums[side][w][slot * kLanes + e / kVec][e & (kVec - 1)];
+    for (int w = 0; w < kWaves; ++w) {
+      float of_wave = 0.0f;
+      for (int slot = 0; slot < 64 / kLanes; ++slot)
+        of_wave += sums[side][w][slot * kLanes + e / kVec][e & (kVec - 1)];
+      s += of_wave;
+    }
     part_sums[int64_t(blockIdx.x) * 2 * d.width + i] = s;
   }
 }
 
-// The workgroups' sums, in order: 16 columns by 64 rows of threads.
+// The workgroups' sums, in a fixed order: 16 columns by 64 rows of threads, then the
+// four rows of a wave, and the waves four by four.
 __global__ void __launch_bounds__(1024) nr_weights(const float* part_sums, int32_t n, int32_t width, int32_t dtype,
                                                    void* dq, void* dk) {
   constexpr int kDeep = 16;  // in flight
-  __shared__ float sums[64][17];
+  __shared__ float sums[16][17];
   const int c = threadIdx.x & 15, row = threadIdx.x >> 4;
   const int col = blockIdx.x * 16 + c;  // 2 width is a multiple of 16
   float s = 0.0f;
@@ -311,12 +329,14 @@ __global__ void __launch_bounds__(1024) nr_weights(const float* part_sums, int32
 #pragma unroll
     for (int j = 0; j < kDeep; ++j) s += x[j];
   }
-  sums[row][c] = s;
+  s += __shfl_xor(s, 16);
+  s += __shfl_xor(s, 32);
+  if ((row & 3) == 0) sums[row >> 2][c] = s;
   __syncthreads();
   if (row) return;
   s = 0.0f;
-#pragma unroll 16
-  for (int i = 0; i < 64; ++i) s += sums[i][c];
+#pragma unroll
+  for (int i = 0; i < 16; i += 4) s += (sums[i][c] + sums[i + 1][c]) + (sums[i + 2][c] + sums[i + 3][c]);
   void* to = col < width ? dq : dk;
   const int e = col < width ? col : col - width;
   if (!to) return;

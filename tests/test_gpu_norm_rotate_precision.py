@@ -58,3 +58,34 @@ def test_angles_close_to_a_quarter_turn(T, interleaved):
         close("dx a", t[:, :, a], r * (cos - r * dot),
               bound(cos) + r * ((2 * er + 10 * E + W * E) * r * (cos.abs() * r).sum(2, keepdim=True) / W
                                 + r * r * (far.amax() + 2 * math.pi * 2.0**-26 * 2 * E)))
+
+
+def test_sums_of_the_weights_gradients():
+    """65,536 tokens of 64 heads whose terms are z = 1 times a gradient of 1 in the first
+    tokens' first heads and of E in all others, which a sum of 1 does not see one by one. A
+    lane adds up 16 heads of a token, 16 tokens, 4 lanes of a wave, 4 waves, 16 parts, and
+    10 more: 70 E of the terms' sum, 4 E for z and the products. One chain of a lane's 256
+    terms would lose 255 E."""
+    T, H, W = 65_536, 64, 64
+    x = torch.ones((T, H, W), dtype=torch.bfloat16, device="cuda")
+    d = torch.full_like(x, E)
+    d[:4_096, :4] = 1.0
+    w = torch.ones(W, device="cuda")
+    pos = torch.zeros(T, dtype=torch.int32, device="cuda")
+    dqw, dkw = nopfs.norm_rotate_grad(d, d, x, x, pos, None, w, w, eps=2.0**-60)[2:]
+    want = torch.full((W,), 4_096 * 4 + (T * H - 4_096 * 4) * E, dtype=F64)
+    for got in (dqw, dkw):
+        close("dw", got, want, 1.01 * 75 * E * want)
+
+
+@pytest.mark.parametrize("T", [4_095, 4_096 * 64, 4_096 * 64 + 1, 4_096 * 65, 600_001])
+def test_sums_over_many_tokens(T):
+    """Every token is in the sums once, in runs of any length: whole numbers, exactly."""
+    x = torch.ones((T, 1, 8), dtype=torch.bfloat16, device="cuda")
+    d = (torch.arange(T, device="cuda") % 7 - 3).bfloat16()[:, None, None].expand(T, 1, 8).contiguous()
+    w = torch.ones(8, device="cuda")
+    pos = torch.zeros(T, dtype=torch.int32, device="cuda")
+    pos[5::11] = -1
+    dqw, dkw = nopfs.norm_rotate_grad(d, d, x, x, pos, None, w, w, eps=2.0**-60)[2:]
+    want = d[pos >= 0].double().sum((0, 1))
+    assert torch.equal(dqw.double(), want) and torch.equal(dkw.double(), want)
