@@ -534,6 +534,10 @@ typedef struct nopfs_embed {
  * No scratch. Errors: EINVAL, ERANGE, EDEVICE. */
 int nopfs_token_embed(const nopfs_embed* e, const void* weight, const void* ids,
                       const int64_t* slot, void* out, void* hip_stream);
+/* The same, and names: int32 [T], each id_t (-1: padding). As ids of the gradient
+ * (id_bytes 4, n_ids T, no slot) they stand for ids and slot, which may change then. */
+int nopfs_token_embed_names(const nopfs_embed* e, const void* weight, const void* ids,
+                            const int64_t* slot, void* out, int32_t* names, void* hip_stream);
 
 /* The gradient of weight, all of it: d_weight[v] = scale times the sum of d_out[t]
  * over the t with id_t = v in 32 bits, in an order that the ids alone decide,

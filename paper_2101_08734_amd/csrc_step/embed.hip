@@ -41,16 +41,22 @@ __device__ __forceinline__ int32_t in_row(int32_t c, int32_t width) {
   return c + kVec <= width ? c : width > kVec ? width - kVec : 0;
 }
 
-// Rows by groups of 2^lg lanes, kPer rows of a group at a time.
+// Rows by groups of 2^lg lanes, kPer rows of a group at a time. `names`, if given, gets
+// what each token names.
 template <class W, class E, int kPer>
 __global__ void __launch_bounds__(256) te_forward(const Embed d, const typename W::T* weight, typename E::T* out,
-                                                  int lg) {
+                                                  int32_t* names, int lg) {
   const int lanes = 1 << lg;
   const int64_t t0 = (int64_t(row_block()) * (256 >> lg) + (threadIdx.x >> lg)) * kPer;
   if (t0 >= d.T) return;
   int64_t id[kPer];
 #pragma unroll
   for (int j = 0; j < kPer; ++j) id[j] = t0 + j < d.T ? name_of(d, t0 + j) : -1;
+  if (names && (threadIdx.x & (lanes - 1)) == 0) {
+#pragma unroll
+    for (int j = 0; j < kPer; ++j)
+      if (t0 + j < d.T) names[t0 + j] = int32_t(id[j]);
+  }
   const int some = d.width;
   for (int32_t c0 = int32_t(threadIdx.x & (lanes - 1)) * kVec; c0 < d.width; c0 += lanes * kVec) {
     const int32_t c = in_row(c0, d.width);
@@ -483,7 +489,7 @@ constexpr int32_t kOneStep = 256 * kVec;
 constexpr int64_t kManyRows = 1024;  // workgroups with a row per group
 
 int embed_impl(const nopfs_embed* p, const void* weight, const void* ids, const int64_t* slot, void* out,
-               hipStream_t st) {
+               int32_t* names, hipStream_t st) {
   const int rc = check(p);
   if (rc) return rc;
   if (p->T == 0) return NOPFS_OK;
@@ -499,7 +505,7 @@ int embed_impl(const nopfs_embed* p, const void* weight, const void* ids, const 
       typedef decltype(e) E;
       return launch("te_forward", several ? te_forward<W, E, 4> : te_forward<W, E, 1>,
                     row_grid(several ? ceil_div(blocks, 4) : blocks), dim3(256), 0, st, d,
-                    static_cast<const typename W::T*>(weight), static_cast<typename E::T*>(out), lg);
+                    static_cast<const typename W::T*>(weight), static_cast<typename E::T*>(out), names, lg);
     });
   });
 }
@@ -587,7 +593,17 @@ using namespace nopfs;
 extern "C" int nopfs_token_embed(const nopfs_embed* e, const void* weight, const void* ids, const int64_t* slot,
                                  void* out, void* hip_stream) {
   try {
-    return embed_impl(e, weight, ids, slot, out, static_cast<hipStream_t>(hip_stream));
+    return embed_impl(e, weight, ids, slot, out, nullptr, static_cast<hipStream_t>(hip_stream));
+  } catch (...) {
+    return fail(NOPFS_EDEVICE, "unexpected host exception");
+  }
+}
+
+extern "C" int nopfs_token_embed_names(const nopfs_embed* e, const void* weight, const void* ids, const int64_t* slot,
+                                       void* out, int32_t* names, void* hip_stream) {
+  try {
+    if (e && e->T > 0 && !names) return fail(NOPFS_EINVAL, "names must be non-NULL");
+    return embed_impl(e, weight, ids, slot, out, names, static_cast<hipStream_t>(hip_stream));
   } catch (...) {
     return fail(NOPFS_EDEVICE, "unexpected host exception");
   }

@@ -159,6 +159,7 @@ def lib() -> ctypes.CDLL:
             "nopfs_packed_attention_grad": [ctypes.POINTER(_Attention)] + [P] * 11,
             "nopfs_topk_distill": [ctypes.POINTER(_Distill)] + [P] * 7,
             "nopfs_token_embed": [ctypes.POINTER(_Embed)] + [P] * 5,
+            "nopfs_token_embed_names": [ctypes.POINTER(_Embed)] + [P] * 6,
             "nopfs_token_embed_grad": [ctypes.POINTER(_Embed)] + [P] * 5,
             "nopfs_token_embed_scratch": [ctypes.POINTER(_Embed), P],
             "nopfs_norm_rotate": [ctypes.POINTER(_Rotate)] + [P] * 9,
@@ -193,7 +194,7 @@ EXPORTED = ("nopfs_stream_shape", "nopfs_access_streams", "nopfs_access_streams_
             "nopfs_staging_schedule", "nopfs_fetch_model", "nopfs_buffer_sim", "nopfs_policy_sim",
             "nopfs_batch_tables", "nopfs_packed_attention", "nopfs_packed_attention_grad",
             "nopfs_batch_tables_scratch", "nopfs_packed_attention_scratch",
-            "nopfs_topk_distill", "nopfs_token_embed", "nopfs_token_embed_grad",
+            "nopfs_topk_distill", "nopfs_token_embed", "nopfs_token_embed_names", "nopfs_token_embed_grad",
             "nopfs_token_embed_scratch", "nopfs_norm_rotate", "nopfs_norm_rotate_grad",
             "nopfs_norm_rotate_scratch", "nopfs_gated_scan", "nopfs_gated_scan_grad",
             "nopfs_gated_scan_scratch", "nopfs_strerror",
@@ -824,17 +825,20 @@ def _float_types(dtype):
 class _TokenEmbed(torch.autograd.Function):
     @staticmethod
     def forward(ctx, weight, ids, scale, slot, dtype, stream):
-        ctx.save_for_backward(ids, *(() if slot is None else (slot,)))
+        # what the tokens name, not ids and slot: the token buffer and its tables go on
+        # to the next batch while this one's gradient is to come
+        out, names = _token_embed(weight, ids, scale, slot, dtype, None, True, stream)
+        ctx.save_for_backward(names)
         ctx.rows, ctx.dtype, ctx.scale, ctx.stream = weight.shape[0], weight.dtype, scale, stream
-        return token_embed(weight, ids, scale, slot, dtype, stream=stream)
+        return out
 
     @staticmethod
     @torch.autograd.function.once_differentiable
     def backward(ctx, dout):
-        ids, *slot = ctx.saved_tensors
+        names, = ctx.saved_tensors
         dout = _row_gradient(dout)
         dweight = _call_in_backward(ctx.stream, lambda: token_embed_grad(
-            dout, ids, ctx.rows, ctx.scale, slot[0] if slot else None, ctx.dtype, stream=ctx.stream))
+            dout, names, ctx.rows, ctx.scale, None, ctx.dtype, stream=ctx.stream))
         return dweight, None, None, None, None, None
 
 
@@ -844,10 +848,16 @@ def token_embed(weight, ids, scale=1.0, slot=None, dtype=None, out=None, stream=
     int64 (a row of batch_tables' slot) ids is a token buffer, and token t is
     ids[slot[t]]. Slots and ids out of range, -1 among them, are padding: rows of
     zeros. Returns [T][width] of `dtype` (weight's unless given). Autograd takes it
-    back to weight by token_embed_grad."""
+    back to weight by token_embed_grad, from what the tokens named in this call: ids
+    and slot may change before the backward pass."""
     if weight.requires_grad and torch.is_grad_enabled():
         _no_outputs_given("token_embed", out)
         return _TokenEmbed.apply(weight, ids, scale, slot, dtype, stream)
+    return _token_embed(weight, ids, scale, slot, dtype, out, False, stream)[0]
+
+
+def _token_embed(weight, ids, scale, slot, dtype, out, names, stream):
+    """The rows, and if asked for what the tokens name, int32 (-1: padding)."""
     dev = torch.cuda.current_device()
     V, width = _step_tensor(weight, "weight", _DTYPES, 2, dev).shape
     n_ids, T = _tokens(ids, slot, dev)
@@ -858,11 +868,15 @@ def token_embed(weight, ids, scale=1.0, slot=None, dtype=None, out=None, stream=
         _step_shape(_step_tensor(out, "out", types, 2, dev), "out", (T, width))
     e = _Embed(T, V, n_ids, _row_stride(weight), _row_stride(out), width, _DTYPES[weight.dtype],
                _DTYPES[out.dtype], ids.element_size(), scale)
-    st = _step_stream(stream, dev, (weight, ids, slot, out))
-    _check(lib().nopfs_token_embed(ctypes.byref(e), weight.data_ptr(), ids.data_ptr(),
-                                   None if slot is None else slot.data_ptr(), out.data_ptr(), st),
-           "nopfs_token_embed")
-    return out
+    names = ids.new_empty(T, dtype=torch.int32) if names else None
+    st = _step_stream(stream, dev, (weight, ids, slot, out, names))
+    args = (ctypes.byref(e), weight.data_ptr(), ids.data_ptr(), None if slot is None else slot.data_ptr(),
+            out.data_ptr())
+    if names is None:
+        _check(lib().nopfs_token_embed(*args, st), "nopfs_token_embed")
+    else:
+        _check(lib().nopfs_token_embed_names(*args, names.data_ptr(), st), "nopfs_token_embed_names")
+    return out, names
 
 
 def token_embed_grad(dout, ids, rows: int, scale=1.0, slot=None, dtype=None, dweight=None,
