@@ -12,6 +12,7 @@ import os
 from dataclasses import dataclass
 
 import torch  # loads the HIP runtime before the library does
+from torch.autograd import forward_ad
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(HERE, "libnopfs.so")
@@ -606,6 +607,15 @@ def _no_outputs_given(name, *outputs):
                          "requires a gradient (detach it, or call under torch.no_grad())")
 
 
+def _no_tangents(name, *inputs):
+    """Refuses inputs with forward-mode derivatives, which the kernels would drop."""
+    if getattr(forward_ad, "_current_level", 0) < 0:  # none anywhere
+        return
+    if any(isinstance(t, torch.Tensor) and forward_ad.unpack_dual(t).tangent is not None for t in inputs):
+        raise ValueError(f"{name} has no forward-mode derivative (autograd takes its outputs back, "
+                         "or call it with the primals)")
+
+
 def _call_in_backward(stream, call):
     """A call that the forward pass made on `stream`, behind what the backward
     pass has on its own stream and before what follows there."""
@@ -678,6 +688,7 @@ def packed_attention(q, k, v, start, scale=None, o=None, lse=None, stream=None):
     start [n+1] int32, a row of batch_tables' start. Returns o (as q) and lse
     [heads][T] float32. scale: 1/sqrt(width) unless given. Autograd takes o back to
     q, k and v by packed_attention_grad."""
+    _no_tangents("packed_attention", q, k, v)
     if (q.requires_grad or k.requires_grad or v.requires_grad) and torch.is_grad_enabled():
         _no_outputs_given("packed_attention", o, lse)
         return _PackedAttention.apply(q, k, v, start, scale, stream)
@@ -706,6 +717,7 @@ def packed_attention_grad(do, q, k, v, o, lse, start, scale=None, dq=None, dk=No
     """Gradient of packed_attention (nopfs_packed_attention_grad) from its
     outputs and the gradient `do` of o. Returns dq, dk, dv (as q, k, v; slices
     of one preallocated array, say), which autograd does not differentiate again."""
+    _no_tangents("packed_attention_grad", do, q, k, v, o, lse)
     dev = torch.cuda.current_device()
     a = _attention(q, k, v, start, scale, dev)
     same = (q.dtype,)
@@ -761,6 +773,7 @@ def topk_distill(logits, index, teacher, tau=1.0, weight=None, grad=True, loss=N
     by the logits (in their type; dlogits may be logits itself). Autograd takes the
     loss back to the logits by that gradient; with grad False the loss is outside
     its graph. Teacher and weight are data and may not require gradients."""
+    _no_tangents("topk_distill", logits, teacher, weight)
     if teacher.requires_grad or weight is not None and weight.requires_grad:
         if torch.is_grad_enabled():
             raise ValueError("topk_distill has no gradient by teacher and weight (detach them)")
@@ -850,6 +863,7 @@ def token_embed(weight, ids, scale=1.0, slot=None, dtype=None, out=None, stream=
     zeros. Returns [T][width] of `dtype` (weight's unless given). Autograd takes it
     back to weight by token_embed_grad, from what the tokens named in this call: ids
     and slot may change before the backward pass."""
+    _no_tangents("token_embed", weight)
     if weight.requires_grad and torch.is_grad_enabled():
         _no_outputs_given("token_embed", out)
         return _TokenEmbed.apply(weight, ids, scale, slot, dtype, stream)
@@ -884,6 +898,7 @@ def token_embed_grad(dout, ids, rows: int, scale=1.0, slot=None, dtype=None, dwe
     """Gradient of token_embed by its weight of `rows` rows (nopfs_token_embed_grad),
     from `dout` [T][width], the gradient of its output. Returns all of it,
     [rows][width] of `dtype` (dout's unless given)."""
+    _no_tangents("token_embed_grad", dout)
     dev = torch.cuda.current_device()
     n_ids, T = _tokens(ids, slot, dev)
     width = _step_tensor(dout, "dout", _DTYPES, 2, dev).shape[1]
@@ -967,6 +982,7 @@ def norm_rotate(q, k, pos, freq=None, q_weight=None, k_weight=None, eps=1e-6, in
     or neighbours if interleaved. q_weight, k_weight [width] of one type, or None.
     Returns q_out, k_out; they may be q and k. Autograd takes them back to q, k and
     the weights by norm_rotate_grad; freq is data."""
+    _no_tangents("norm_rotate", q, k, freq, q_weight, k_weight)
     if freq is not None and freq.requires_grad and torch.is_grad_enabled():
         raise ValueError("norm_rotate has no gradient by freq (detach it)")
     if (q.requires_grad or k.requires_grad or q_weight is not None and q_weight.requires_grad
@@ -989,6 +1005,7 @@ def norm_rotate_grad(dq_out, dk_out, q, k, pos, freq=None, q_weight=None, k_weig
     """Gradient of norm_rotate (nopfs_norm_rotate_grad) from its inputs and the
     gradients of its outputs. Returns dq, dk (given, they may be dq_out and dk_out) and
     the gradients of the weights, None of a weight that is None, or with weights False."""
+    _no_tangents("norm_rotate_grad", dq_out, dk_out, q, k, freq, q_weight, k_weight)
     dev = torch.cuda.current_device()
     r = _rotate(q, k, pos, freq, q_weight, k_weight, eps, interleaved, dev)
     for name, d, like in (("dq_out", dq_out, q), ("dk_out", dk_out, k)):
@@ -1060,6 +1077,7 @@ def gated_scan(x, gate, start, h0=None, keep=True, h=None, last=None, stream=Non
     (None if keep is False). Samples of one token with h0 are the step of a
     generation; last may not be h0. Autograd takes h and last back to x, gate and h0
     by gated_scan_grad."""
+    _no_tangents("gated_scan", x, gate, h0)
     if (x.requires_grad or gate.requires_grad
             or h0 is not None and h0.requires_grad) and torch.is_grad_enabled():
         _no_outputs_given("gated_scan", h, last)
@@ -1085,6 +1103,7 @@ def gated_scan_grad(dh, x, gate, start, carry, h0=None, dlast=None, dx=None, dga
     """Gradient of gated_scan (nopfs_gated_scan_grad) from its inputs, its carry and
     the gradients of h and last (None: 0). Returns dx, dgate (as x) and dh0 (None
     without h0)."""
+    _no_tangents("gated_scan_grad", dh, x, gate, carry, h0, dlast)
     dev = torch.cuda.current_device()
     T, n, channels, chunks = _scan(x, gate, start, h0, dev)
     _step_shape(_step_tensor(dh, "dh", (x.dtype,), 2, dev), "dh", (T, channels))
