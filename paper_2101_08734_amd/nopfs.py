@@ -1081,7 +1081,8 @@ def gated_scan(x, gate, start, h0=None, keep=True, h=None, last=None, stream=Non
     if (x.requires_grad or gate.requires_grad
             or h0 is not None and h0.requires_grad) and torch.is_grad_enabled():
         _no_outputs_given("gated_scan", h, last)
-        return _GatedScan.apply(x, gate, start, h0, stream)
+        h, last, carry = _GatedScan.apply(x, gate, start, h0, stream)
+        return h, last, carry if keep else None
     dev = torch.cuda.current_device()
     T, n, channels, chunks = _scan(x, gate, start, h0, dev)
     h = _rows_of(h, "h", x.dtype, (T, channels), x, dev)
