@@ -13,6 +13,7 @@ from dataclasses import dataclass
 
 import torch  # loads the HIP runtime before the library does
 from torch.autograd import forward_ad
+from torch.autograd.graph import increment_version
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(HERE, "libnopfs.so")
@@ -513,6 +514,14 @@ def _step_dense(t, name, dtype, shape, device):
     return _dense(t, name)
 
 
+def _written(*given):
+    """Tells autograd that a call has written these tensors of its caller's: a backward
+    pass that has one saved as it was before is then refused instead of wrong."""
+    given = [t for t in given if t is not None]
+    if given:
+        increment_version(given)
+
+
 # The current stream's handle without the object around it, which takes 1 us to
 # make, a tenth of a small call.
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
@@ -581,7 +590,7 @@ def batch_tables(ids, tokens, free, block: int, width: int, cap: int, out=None, 
         raise ValueError(f"free must have {G} rows")
     if not (0 < block < 2**31 and 0 < width < 2**31 and 0 <= cap < 2**31):
         raise ValueError("block and width must be positive, cap not negative, all below 2^31")
-    o = dict(out) if out else {}
+    o, given = dict(out) if out else {}, []
     for name, shape, dt in (("start", (G, n + 1), torch.int32), ("table", (G, n, width), torch.int32),
                             ("slot", (G, cap), torch.int64), ("row", (G, cap), torch.int32),
                             ("pos", (G, cap), torch.int32), ("used", (G, 3), torch.int32)):
@@ -589,7 +598,7 @@ def batch_tables(ids, tokens, free, block: int, width: int, cap: int, out=None, 
         if t is None:
             o[name] = lead.new_empty(shape, dtype=dt)
         else:
-            _step_dense(t, name, dt, shape, dev)
+            given.append(_step_dense(t, name, dt, shape, dev))
     b = _Batch(F, _row_stride(lead), _row_stride(free), G, n, free.shape[1], block, width, cap)
     st = _step_stream(stream, dev, (ids, tokens, free, *o.values()))
     scratch = _capturing() and _step_scratch(  # noqa: F841 held until the call is enqueued
@@ -598,6 +607,7 @@ def batch_tables(ids, tokens, free, block: int, width: int, cap: int, out=None, 
         ctypes.byref(b), None if ids is None else ids.data_ptr(), tokens.data_ptr(),
         free.data_ptr(), o["start"].data_ptr(), o["table"].data_ptr(), o["slot"].data_ptr(),
         o["row"].data_ptr(), o["pos"].data_ptr(), o["used"].data_ptr(), st), "nopfs_batch_tables")
+    _written(*given)
     return o
 
 
@@ -693,6 +703,7 @@ def packed_attention(q, k, v, start, scale=None, o=None, lse=None, stream=None):
         _no_outputs_given("packed_attention", o, lse)
         return _PackedAttention.apply(q, k, v, start, scale, stream)
     dev = torch.cuda.current_device()
+    given = (o, lse)
     a = _attention(q, k, v, start, scale, dev)
     if o is None:
         o = q.new_empty(q.shape)
@@ -709,6 +720,7 @@ def packed_attention(q, k, v, start, scale=None, o=None, lse=None, stream=None):
     _check(lib().nopfs_packed_attention(ctypes.byref(a), q.data_ptr(), k.data_ptr(), v.data_ptr(),
                                         start.data_ptr(), o.data_ptr(), lse.data_ptr(), st),
            "nopfs_packed_attention")
+    _written(*given)
     return o, lse
 
 
@@ -719,6 +731,7 @@ def packed_attention_grad(do, q, k, v, o, lse, start, scale=None, dq=None, dk=No
     of one preallocated array, say), which autograd does not differentiate again."""
     _no_tangents("packed_attention_grad", do, q, k, v, o, lse)
     dev = torch.cuda.current_device()
+    given = (dq, dk, dv)
     a = _attention(q, k, v, start, scale, dev)
     same = (q.dtype,)
     for name, t in (("do", do), ("o", o)):
@@ -740,6 +753,7 @@ def packed_attention_grad(do, q, k, v, o, lse, start, scale=None, dq=None, dk=No
         ctypes.byref(a), do.data_ptr(), q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(),
         lse.data_ptr(), start.data_ptr(), dq.data_ptr(), dk.data_ptr(), dv.data_ptr(), st),
         "nopfs_packed_attention_grad")
+    _written(*given)
     return dq, dk, dv
 
 
@@ -781,6 +795,7 @@ def topk_distill(logits, index, teacher, tau=1.0, weight=None, grad=True, loss=N
         _no_outputs_given("topk_distill", loss, dlogits)
         return _TopkDistill.apply(logits, index, teacher, tau, weight, stream)
     dev = torch.cuda.current_device()
+    given = (loss, dlogits if grad else None)
     T, V = _step_tensor(logits, "logits", _DTYPES, 2, dev).shape
     K = _step_tensor(index, "index", _I32, 2, dev).shape[1]
     _step_shape(index, "index", (T, K))
@@ -805,6 +820,7 @@ def topk_distill(logits, index, teacher, tau=1.0, weight=None, grad=True, loss=N
         ctypes.byref(d), logits.data_ptr(), index.data_ptr(), teacher.data_ptr(),
         None if weight is None else weight.data_ptr(), loss.data_ptr(),
         None if dlogits is None else dlogits.data_ptr(), st), "nopfs_topk_distill")
+    _written(*given)
     return loss, dlogits
 
 
@@ -873,6 +889,7 @@ def token_embed(weight, ids, scale=1.0, slot=None, dtype=None, out=None, stream=
 def _token_embed(weight, ids, scale, slot, dtype, out, names, stream):
     """The rows, and if asked for what the tokens name, int32 (-1: padding)."""
     dev = torch.cuda.current_device()
+    given = (out,)
     V, width = _step_tensor(weight, "weight", _DTYPES, 2, dev).shape
     n_ids, T = _tokens(ids, slot, dev)
     types = _float_types(dtype)
@@ -890,6 +907,7 @@ def _token_embed(weight, ids, scale, slot, dtype, out, names, stream):
         _check(lib().nopfs_token_embed(*args, st), "nopfs_token_embed")
     else:
         _check(lib().nopfs_token_embed_names(*args, names.data_ptr(), st), "nopfs_token_embed_names")
+    _written(*given)
     return out, names
 
 
@@ -900,6 +918,7 @@ def token_embed_grad(dout, ids, rows: int, scale=1.0, slot=None, dtype=None, dwe
     [rows][width] of `dtype` (dout's unless given)."""
     _no_tangents("token_embed_grad", dout)
     dev = torch.cuda.current_device()
+    given = (dweight,)
     n_ids, T = _tokens(ids, slot, dev)
     width = _step_tensor(dout, "dout", _DTYPES, 2, dev).shape[1]
     _step_shape(dout, "dout", (T, width))
@@ -917,6 +936,7 @@ def token_embed_grad(dout, ids, rows: int, scale=1.0, slot=None, dtype=None, dwe
     _check(lib().nopfs_token_embed_grad(ctypes.byref(e), dout.data_ptr(), ids.data_ptr(),
                                         None if slot is None else slot.data_ptr(),
                                         dweight.data_ptr(), st), "nopfs_token_embed_grad")
+    _written(*given)
     return dweight
 
 
@@ -990,6 +1010,7 @@ def norm_rotate(q, k, pos, freq=None, q_weight=None, k_weight=None, eps=1e-6, in
         _no_outputs_given("norm_rotate", q_out, k_out)
         return _NormRotate.apply(q, k, pos, freq, q_weight, k_weight, eps, interleaved, stream)
     dev = torch.cuda.current_device()
+    given = (q_out, k_out)
     r = _rotate(q, k, pos, freq, q_weight, k_weight, eps, interleaved, dev)
     q_out, k_out = _heads_like(q_out, "q_out", q, dev), _heads_like(k_out, "k_out", k, dev)
     r = _Rotate(*r, *_strides(q, k, q_out, k_out))
@@ -997,6 +1018,7 @@ def norm_rotate(q, k, pos, freq=None, q_weight=None, k_weight=None, eps=1e-6, in
     _check(lib().nopfs_norm_rotate(ctypes.byref(r), q.data_ptr(), k.data_ptr(), pos.data_ptr(),
                                    _optional(freq), _optional(q_weight), _optional(k_weight),
                                    q_out.data_ptr(), k_out.data_ptr(), st), "nopfs_norm_rotate")
+    _written(*given)
     return q_out, k_out
 
 
@@ -1007,6 +1029,7 @@ def norm_rotate_grad(dq_out, dk_out, q, k, pos, freq=None, q_weight=None, k_weig
     the gradients of the weights, None of a weight that is None, or with weights False."""
     _no_tangents("norm_rotate_grad", dq_out, dk_out, q, k, freq, q_weight, k_weight)
     dev = torch.cuda.current_device()
+    given = (dq, dk)
     r = _rotate(q, k, pos, freq, q_weight, k_weight, eps, interleaved, dev)
     for name, d, like in (("dq_out", dq_out, q), ("dk_out", dk_out, k)):
         _step_shape(_step_tensor(d, name, (q.dtype,), 3, dev), name, like.shape)
@@ -1019,6 +1042,7 @@ def norm_rotate_grad(dq_out, dk_out, q, k, pos, freq=None, q_weight=None, k_weig
         ctypes.byref(r), dq_out.data_ptr(), dk_out.data_ptr(), q.data_ptr(), k.data_ptr(), pos.data_ptr(),
         _optional(freq), _optional(q_weight), _optional(k_weight), dq.data_ptr(), dk.data_ptr(),
         _optional(dqw), _optional(dkw), st), "nopfs_norm_rotate_grad")
+    _written(*given)
     return dq, dk, dqw, dkw
 
 
@@ -1084,6 +1108,7 @@ def gated_scan(x, gate, start, h0=None, keep=True, h=None, last=None, stream=Non
         h, last, carry = _GatedScan.apply(x, gate, start, h0, stream)
         return h, last, carry if keep else None
     dev = torch.cuda.current_device()
+    given = (h, last)
     T, n, channels, chunks = _scan(x, gate, start, h0, dev)
     h = _rows_of(h, "h", x.dtype, (T, channels), x, dev)
     if last is None:
@@ -1097,6 +1122,7 @@ def gated_scan(x, gate, start, h0=None, keep=True, h=None, last=None, stream=Non
     _check(lib().nopfs_gated_scan(ctypes.byref(s), x.data_ptr(), gate.data_ptr(), start.data_ptr(),
                                   _optional(h0), h.data_ptr(), last.data_ptr(), _optional(carry), st),
            "nopfs_gated_scan")
+    _written(*given)
     return h, last, carry
 
 
@@ -1106,6 +1132,7 @@ def gated_scan_grad(dh, x, gate, start, carry, h0=None, dlast=None, dx=None, dga
     without h0)."""
     _no_tangents("gated_scan_grad", dh, x, gate, carry, h0, dlast)
     dev = torch.cuda.current_device()
+    given = (dx, dgate)
     T, n, channels, chunks = _scan(x, gate, start, h0, dev)
     _step_shape(_step_tensor(dh, "dh", (x.dtype,), 2, dev), "dh", (T, channels))
     _step_dense(carry, "carry", torch.float32, (chunks, channels), dev)
@@ -1122,6 +1149,7 @@ def gated_scan_grad(dh, x, gate, start, carry, h0=None, dlast=None, dx=None, dga
         ctypes.byref(s), dh.data_ptr(), _optional(dlast), x.data_ptr(), gate.data_ptr(), start.data_ptr(),
         _optional(h0), carry.data_ptr(), dx.data_ptr(), dgate.data_ptr(), _optional(dh0), st),
         "nopfs_gated_scan_grad")
+    _written(*given)
     return dx, dgate, dh0
 
 
