@@ -4,9 +4,10 @@
 // Both are bound by memory (16,384 tokens by 2,048 from 32,768 rows, a twelfth of them
 // the most frequent one, bf16: forward 26 us for 108 MB; the gradient's zeros and sums
 // 41 us for 205). The gradient's sums must not depend on the order in which work
-// finishes, so the tokens are sorted by id first (radix sort, stable: a name's rows
-// are added in the order of the batch; 16 us of four dependent launches there).
-// Sums are in 32 bits, rounded once.
+// finishes, so the tokens are sorted by id first (radix sort, stable; 16 us of four
+// dependent launches there) and added in an order that the ids alone decide: as in the
+// batch within a piece of the sorted tokens, then the pieces' parts of a name. Sums are
+// in 32 bits, rounded once.
 #include "rows.hpp"
 
 namespace nopfs {
@@ -321,7 +322,7 @@ __global__ void __launch_bounds__(256) te_scatter_zero(const Embed d, const Sort
 // The sorted tokens are cut into pieces of equal size, however many of them share
 // a name (a row of the embedding each: 1,114 us where this takes 100), by groups of
 // 2^lg lanes. A name whose tokens lie in one piece has its row written from there; the
-// others leave the sum of each piece's part, and te_join adds those up in order.
+// others leave the sum of each piece's part, and te_join adds those up.
 struct Pieces {
   const uint32_t *key, *val;
   float *head, *tail;  // [pieces][width]: of the name that goes on from the piece before; into the next
@@ -409,8 +410,9 @@ __global__ void __launch_bounds__(256) te_pieces(const Embed d, const Pieces s, 
 constexpr int64_t kMostPieces = 8192, kPieceThreads = 1 << 17;
 
 // The names of several pieces: a workgroup adds up the parts of the one that begins
-// in its piece, 4 columns a lane. Its 2^(8 - jg) groups of lanes have every so
-// manieth part, so that narrow rows take as many loads at once as wide ones.
+// in its piece, 4 columns a lane. Each of its 2^(8 - jg) groups of lanes adds every so
+// manieth part, in order, so that narrow rows take as many loads at once as wide ones,
+// and the first adds the groups' sums, in order.
 template <class W>
 __global__ void __launch_bounds__(256) te_join(const Embed d, const Pieces s, typename W::T* dw, int jg) {
   constexpr int kCols = 4, kDeep = 8;
