@@ -375,6 +375,8 @@ __global__ void __launch_bounds__(256) te_pieces(const Embed d, const Pieces s, 
       for (int j = 0; j < kDeep; ++j) {
         key[j] = i + j < i1 ? s.key[i + j] : none;
         val[j] = i + j < i1 ? s.val[i + j] : 0;
+        // ids that changed under the call have left places that no token was written to
+        val[j] = val[j] < d.T ? val[j] : 0;
       }
       Pack<E, kVec> x[kDeep];
 #pragma unroll
