@@ -15,8 +15,8 @@
 //
 // The states and maps are in 32 bits. A step is taken from the larger share,
 // h + k (x - h) or x + a (h - x), so that its rounding is half a unit of the result; a
-// map likewise, by the smaller of A and 1 - A, each made by such steps, so that a gate
-// near 1 loses nothing to the rounding of a product of its a. What goes from chunk to
+// map likewise, by the smaller of A and 1 - A, each summed up from the steps' shares, so
+// that a gate near 1 loses nothing to the rounding of a product of its a. What goes from chunk to
 // chunk so has one rounding of the state per chunk of 128 tokens: 25,600 tokens of gate
 // 12.2 (a = 1 - 5e-6) are off by 2e-7, token by token by 1e-6, by products of a by 3e-4.
 #include "rows.hpp"
@@ -135,12 +135,17 @@ __device__ __forceinline__ float a_of(float share) { return is_a(share) ? -share
 __device__ __forceinline__ float step(float share, float h, float x) {
   return fmaf(share, x - h, is_a(share) ? x : h);  // x + a (h - x), or h + k (x - h)
 }
-// A stretch's map: B + A h, with the smaller of A and K = 1 - A as its share. A and K
-// are what the stretch's steps make of 1 among zeros, and of 0 among ones.
-__device__ __forceinline__ float map_share(float A, float K) { return A <= K ? -A : K; }
+// A stretch's map: B + A h, with the smaller of A and K = 1 - A as its share. A is what
+// the stretch's steps make of 1 among zeros, K the sum of what they take from it. K is
+// so only where no step's share is an a; of others A is at most a half and its
+// rounding, and K not used.
+__device__ __forceinline__ void more(float share, float* A, float* K) {
+  *K = fmaf(share, *A, *K);
+  *A = step(share, *A, 0.0f);
+}
+__device__ __forceinline__ float map_share(float A, float K) { return A <= 0.5625f ? -A : K; }
 __device__ __forceinline__ float apply(float share, float B, float h) {
-  const float y = fmaf(-share, h, B);  // B + A h, or B - K h
-  return is_a(share) ? y : h + y;
+  return fmaf(-share, h, B) + (is_a(share) ? 0.0f : h);  // B + A h, or h + (B - K h)
 }
 // G's two shares, a G and k G.
 __device__ __forceinline__ void split(float share, float G, float* aG, float* kG) {
@@ -297,8 +302,7 @@ __device__ inline float chain(const Scan& d, int32_t at, uint32_t tile, const Ma
       const int w = kBack ? kWaves - 1 - j : j;
       const bool cut = uniform(maps.reset[w]);
       const float share = maps.share[w][mine], b = maps.B[w][mine];
-      A = step(share, A, 0.0f);
-      K = step(share, K, 1.0f);
+      more(share, &A, &K);
       B = cut ? b : apply(share, b, B);
       reset |= cut;
     }
@@ -407,8 +411,7 @@ __global__ void __launch_bounds__(64 * kWaves, 6) gs_forward(const Scan d, uint3
 #pragma unroll
       for (int i = 0; i < kN; ++i) {
         B[i] = step(share[r][i], B[i], x[r].get(i));
-        A[i] = step(share[r][i], A[i], 0.0f);
-        K[i] = step(share[r][i], K[i], 1.0f);
+        more(share[r][i], &A[i], &K[i]);
       }
     }
     keep_map<kN>(&maps, first != 0, A, K, B);
@@ -549,8 +552,7 @@ __global__ void __launch_bounds__(64 * kWaves, 4) gs_grad(const Scan d, uint32_t
       for (int i = 0; i < kN; ++i) {
         float kG;
         split(share[r][i], dh[r].get(i) + R[i], &R[i], &kG);
-        A[i] = step(share[r][i], A[i], 0.0f);
-        K[i] = step(share[r][i], K[i], 1.0f);
+        more(share[r][i], &A[i], &K[i]);
       }
     }
     keep_map<kN>(&maps, end != 0, A, K, R);
