@@ -614,7 +614,8 @@ typedef struct nopfs_scan {
 /* With a = 1 / (1 + exp(-gate)), sample s of tokens start[s]..start[s+1]-1 has
  *   h_t = a_t h_(t-1) + (1 - a_t) x_t
  * from h0[s] (or 0) before its first token. The state is held in 32 bits, as are
- * a and 1 - a (0 below 2^-126); h is rounded from it.
+ * a and 1 - a (0 below 2^-126; of an infinite gate one of them is 0); h is rounded
+ * from it.
  *   start: int32 [n+1], as for nopfs_packed_attention.
  *   h0:    float [n][channels], or NULL for 0.
  *   last:  float [n][channels], the state behind each sample's last token (h0 of
@@ -622,7 +623,9 @@ typedef struct nopfs_scan {
  *   carry: float [ceil(T / NOPFS_SCAN_CHUNK)][channels], the states that the
  *          gradient starts from, or NULL.
  * Rows from start[n] on get h = 0, whatever x and gate hold there. A NaN or
- * infinity reaches no other sample. Differences of x and the state stay below 2^128. Errors: EINVAL, ERANGE, ENOMEM, EDEVICE. */
+ * infinity reaches no other sample; an infinite x or state may be NaN from the next
+ * token on, as differences of x and the state are taken, which are to stay below
+ * 2^128. Errors: EINVAL, ERANGE, ENOMEM, EDEVICE. */
 int nopfs_gated_scan(const nopfs_scan* s, const void* x, const void* gate, const int32_t* start,
                      const float* h0, void* h, float* last, float* carry, void* hip_stream);
 

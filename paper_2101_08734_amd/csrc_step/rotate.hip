@@ -6,10 +6,13 @@
 // and back, with g the gradient turned by the opposite angles:
 //     dx = r (g w - z mean(g w z)),   dw = sum g z
 // Bound by memory: a head is read once and written once (the gradient reads the
-// input and the output's gradient): 65,536 tokens, 32 on 8 heads of 128 in bf16 259 us,
-// 5.2 TB/s, the rate of a large copy; 16,384 tokens, 16 on 4 heads 43 us, the gradient
-// 57 and 5 for the weights, with vector units at 57-59%. Statistics, angles and sums are
-// in 32 bits or more; outputs are rounded once.
+// input and the output's gradient): 65,536 tokens, 32 on 8 heads of 128 in bf16 258 us a
+// call, 5.2 TB/s, the rate of a large copy (271 us, 4.95 TB/s, in a kernel trace); 16,384
+// tokens, 16 on 4 heads 44 us, the gradient 59 and 5 for the weights, with vector units at
+// 57-61%; the same in fp32 63 us, 5.3 TB/s, and 106, 4.7. Few or narrow heads leave lanes
+// idle, as a wave has a token: 90,000 tokens of one query and one key head of 64 in bf16 67
+// and 75 us, 0.7 and 0.9 TB/s. Statistics, angles and sums are in 32 bits or more; outputs
+// are rounded once.
 #include "rows.hpp"
 
 namespace nopfs {

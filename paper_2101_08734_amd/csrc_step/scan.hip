@@ -8,10 +8,11 @@
 // if a sample begins in it. A wave holds 16 tokens of its channels in registers, makes
 // their map, gets the state before them through the maps of the stretches before, and
 // goes through its tokens again from there. Everything is read once and written once.
-// 16,384 tokens by 2,048 channels in bf16: forward 60 us for 215 MB, the gradient 95 for
-// 358; a workgroup loads, makes maps, waits and stores in turn, and registers allow three
-// (the gradient: two) of them on a compute unit. Workgroups of 64 or 256 tokens took 78
-// and 77 us, the gradient 114 and 132.
+// 16,384 tokens by 2,048 channels in bf16: forward 64 us for 215 MB, the gradient 102 for
+// 364; a workgroup loads, makes maps, waits and stores in turn beside vector units at 49
+// and 43%, and there are three of them on a compute unit (70 registers a lane), of the
+// gradient two (128, and 6 more in memory). Workgroups of 64 or 256 tokens took 78 and 77
+// us where these took 70, the gradient 114 and 132 to 108.
 //
 // The states and maps are in 32 bits. A step is taken from the larger share,
 // h + k (x - h) or x + a (h - x), so that its rounding is half a unit of the result; a
@@ -648,8 +649,9 @@ int make_chain(Scratch* sc, Scan* d, int per, hipStream_t st) {
 }
 
 // Up to so many tokens, and two a sample, samples go one by one. Of 2,048 channels (bf16)
-// 32, 256, 1,024 samples of one token took 10.8, 10.8, 11.0 us, by chunks 13.0, 19.1, 21.2
-// (4,096: 36.7 and 35.3); where one sample has all 1,024 tokens, 235 and 17.
+// 32, 256, 1,024 samples of one token took 10.9, 10.9, 11.3 us, by chunks 13.0, 19.8, 21.9
+// (4,096: 31.8 and 36.4); where one sample has all 1,024 tokens, 260 and 17, which is why
+// there is no more of it.
 constexpr int64_t kStepTokens = 1024;
 
 int scan_impl(const nopfs_scan* p, const void* x, const void* gate, const int32_t* start, const float* h0, void* h,
