@@ -17,9 +17,10 @@
 // The states and maps are in 32 bits. A step is taken from the larger share,
 // h + k (x - h) or x + a (h - x), so that its rounding is half a unit of the result; a
 // map likewise, by the smaller of A and 1 - A, each summed up from the steps' shares, so
-// that a gate near 1 loses nothing to the rounding of a product of its a. What goes from chunk to
-// chunk so has one rounding of the state per chunk of 128 tokens: 25,600 tokens of gate
-// 12.2 (a = 1 - 5e-6) are off by 2e-7, token by token by 1e-6, by products of a by 3e-4.
+// that a gate near 1 loses nothing to the rounding of a product of its a. What goes from
+// chunk to chunk so has one rounding of the state per chunk of 128 tokens: 25,600 tokens
+// of gate 12.2 (a = 1 - 5e-6) are off by 2e-7, token by token by 1e-6, by products of
+// rounded a by 3e-4.
 #include "rows.hpp"
 
 namespace nopfs {
